@@ -33,6 +33,14 @@ inline bool hip_failed(hipError_t e) {
     return true;
 }
 
+}  // namespace
+
+namespace pgcm {
+bool hip_noted(hipError_t e) { return hip_failed(e); }  // for the library's other files
+}  // namespace pgcm
+
+namespace {
+
 #define PGCM_HIP(call)                             \
     do {                                           \
         if (hip_failed(call)) return PGCM_ERR_HIP; \

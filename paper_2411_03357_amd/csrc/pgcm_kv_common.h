@@ -1,0 +1,152 @@
+// What the operators on KV blocks share: the two 16-bit types, argument checks and the workspace.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <vector>
+
+#include "../../include/pgcm.h"
+#include "../../include/pgcm_kv.h"
+
+namespace pgcm {
+// for pgcm_last_hip_error; true if e is an error
+bool hip_noted(hipError_t e);
+}  // namespace pgcm
+
+// A workspace: counters, zero between calls, and scratch that means nothing between calls.
+struct pgcm_kv {
+    struct Memory {
+        uint8_t* at = nullptr;
+        size_t bytes = 0;
+    };
+    int device = 0;
+    Memory counters, scratch;
+    std::vector<void*> outgrown;  // a captured graph may still name them
+};
+
+namespace pgcm_kv_impl {
+
+constexpr uint32_t kPiece = 16;  // tokens of a matrix-core tile: a block is a whole number of pieces
+constexpr uint32_t kMaxHeadDim = 256;
+constexpr uint32_t kMaxHeads = 65535;
+constexpr uint32_t kTileTokens = 128;  // tokens that a workgroup of attention takes at a step
+
+// At least so many bytes of zeroed counters and of scratch.
+int kv_ensure(pgcm_kv* kv, size_t counters, size_t scratch, hipStream_t stream);
+
+inline bool aligned(const void* p, const int64_t a = 0, const int64_t b = 0, const int64_t c = 0) {
+    return ((uintptr_t)p & 15) == 0 && ((a | b | c) & 7) == 0;
+}
+
+inline int check_shape(uint32_t kv_heads, uint32_t head_dim, uint32_t block_tokens) {
+    if (kv_heads == 0 || kv_heads > kMaxHeads || head_dim == 0 || head_dim % 8 != 0 || head_dim > kMaxHeadDim ||
+        block_tokens == 0 || block_tokens % kPiece != 0 || block_tokens > 4096)
+        return PGCM_ERR_ARG;
+    return PGCM_OK;
+}
+
+// Sizes of a call on a batch of requests.  What kernels count in 32 bits stays below 2^31: blocks of all rows,
+// and tiles of attention for each head.
+inline int check_sizes(uint32_t requests, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint32_t block_tokens,
+                       uint32_t row_blocks) {
+    if (const int rc = check_shape(kv_heads, head_dim, block_tokens)) return rc;
+    if (heads == 0 || heads > kMaxHeads || heads % kv_heads != 0) return PGCM_ERR_ARG;
+    if ((uint64_t)row_blocks * block_tokens > 0x7FFFFFFFull) return PGCM_ERR_ARG;
+    const uint64_t groups = kv_heads * (uint64_t)((heads / kv_heads + kPiece - 1) / kPiece);
+    const uint64_t tiles = ((uint64_t)row_blocks * block_tokens + kTileTokens - 1) / kTileTokens;
+    if (requests != 0 && (groups * requests > 0x7FFFFFFFull || tiles * groups > 0x7FFFFFFFull / requests ||
+                          (uint64_t)row_blocks * kv_heads > 0x7FFFFFFFull / requests))
+        return PGCM_ERR_ARG;
+    return PGCM_OK;
+}
+
+inline int check_cache(const pgcm_kv_cache* c) {
+    if (c == nullptr || c->k == nullptr || c->v == nullptr || c->half > PGCM_KV_BF16 || c->reserved != 0 ||
+        c->blocks == 0 || c->blocks > 0x7FFFFFFFu)
+        return PGCM_ERR_ARG;
+    if (const int rc = check_shape(c->kv_heads, c->head_dim, c->block_tokens)) return rc;
+    if (!aligned(c->k, c->k_block, c->k_token, c->k_head) || !aligned(c->v, c->v_block, c->v_token, c->v_head))
+        return PGCM_ERR_ALIGN;
+    return PGCM_OK;
+}
+
+// ---- workspace
+struct Room {
+    size_t counters, scratch;
+};
+inline size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Attention: a counter for each request and group of up to sixteen query heads of one kv head; two partial results
+// for each workgroup; and, for weights, log-sums of heads and of each piece of a row.
+constexpr uint32_t kAttendGroups = 512;  // workgroups of a launch, at most
+inline size_t partial_floats(uint32_t head_dim) { return 16 * (size_t)(head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 32; }
+inline Room attend_room(uint32_t requests, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint64_t row_pieces) {
+    const size_t groups = kv_heads * (size_t)((heads / kv_heads + kPiece - 1) / kPiece);
+    return Room{4 * groups * requests, whole_lines(4 * partial_floats(head_dim) * 2 * kAttendGroups) +
+                                           whole_lines(4 * (size_t)requests * heads) +
+                                           4 * (size_t)requests * heads * row_pieces};
+}
+
+// Selection: a counter for each request and kv head; a key for each of its blocks.
+inline Room select_room(uint32_t requests, uint32_t kv_heads, uint32_t row_blocks) {
+    return Room{4 * (size_t)requests * kv_heads, 4 * (size_t)requests * kv_heads * row_blocks};
+}
+
+// ---- device side
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+struct F16 {
+    typedef _Float16 one;
+    typedef f16x8 eight;
+    static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+struct Bf16 {
+    typedef __bf16 one;
+    typedef bf16x8 eight;
+    static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+
+template <class H>
+__device__ __forceinline__ typename H::eight as_eight(uint4 x) {
+    return __builtin_bit_cast(typename H::eight, x);
+}
+template <class H>
+__device__ __forceinline__ uint4 as_words(typename H::eight x) {
+    return __builtin_bit_cast(uint4, x);
+}
+
+// Four-byte and eight-byte words that other workgroups of the launch read: written through to where every XCD
+// sees them, and read from there.  (A device-scope fence would write back or drop a whole L2.)
+template <class T>
+__device__ __forceinline__ void put_shared(T* at, T v) {
+    __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class T>
+__device__ __forceinline__ T get_shared(const T* at) {
+    return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// All of this wavefront's stores have arrived there.
+__device__ __forceinline__ void stores_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Whether the calling workgroup is the last of `of` to arrive; the counter is left zero then.  What the others put
+// before arriving can be got afterwards.  All threads call it; *word is in LDS.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* counter, uint32_t of, uint32_t* word) {
+    stores_arrived();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before + 1 == of) put_shared(counter, 0u);
+        *word = before + 1 == of;
+    }
+    __syncthreads();
+    return *word != 0;
+}
+
+}  // namespace pgcm_kv_impl
