@@ -40,25 +40,6 @@ __device__ __forceinline__ uint32_t tiles_of(const AttendArgs& a, uint32_t reque
     return (walked(a, a.lens[request]) + kTileTokens - 1) / kTileTokens;
 }
 
-// inclusive sum over the wavefront
-__device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t lane) {
-#pragma unroll
-    for (uint32_t d = 1; d < 64; d *= 2) {
-        const uint32_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
-}
-
-__device__ __forceinline__ float over_pieces_max(float x) {  // lanes 16 and 32 apart hold the same head
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float over_pieces_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-
 __device__ __forceinline__ float exp2_from(float x, float top) {  // 0 for x = -inf, whatever the top
     return __builtin_amdgcn_exp2f(x - (top == -INFINITY ? 0.f : top));
 }
@@ -165,7 +146,7 @@ struct Walk {
         float most = s[0];
 #pragma unroll
         for (uint32_t j = 1; j < 8; ++j) most = fmaxf(most, s[j]);
-        most = over_pieces_max(most);
+        most = over_rows_max(most);
         if (__any(most > top)) {
             const float now = fmaxf(most, top), keep = exp2_from(top, now);
             top = now;
@@ -243,11 +224,12 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     const uint32_t per_request = a.kv_heads * a.group_tiles;
 
     // The tiles of all items, in the order of requests and heads, in equal spans: this workgroup's is [from, to).
-    uint32_t all = 0;
+    uint32_t all = 0, tiles = 0, upto = 0;   // those of up to 64 requests, and of all before and with them
     for (uint32_t b0 = 0; b0 < a.requests; b0 += 64) {
         const uint32_t b = b0 + lane;
-        const uint32_t tiles = b < a.requests ? tiles_of(a, b) : 0;
-        all += __shfl(scan(tiles, lane), 63);
+        tiles = b < a.requests ? tiles_of(a, b) : 0;
+        upto = all + scan(tiles);
+        all = __builtin_amdgcn_readlane(upto, 63);
         // requests without tokens are answered here
         uint64_t empty = __ballot(b < a.requests && tiles == 0 && b % gridDim.x == blockIdx.x);
         for (; empty != 0; empty &= empty - 1) {
@@ -272,17 +254,19 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     // the request that the span begins in, and its first tile
     uint32_t request = 0, before = 0;
     for (uint32_t b0 = 0, sum = 0; b0 < a.requests; b0 += 64) {
-        const uint32_t b = b0 + lane;
-        const uint32_t tiles = b < a.requests ? tiles_of(a, b) : 0;
-        const uint32_t upto = sum + scan(tiles, lane);
+        if (a.requests > 64) {
+            const uint32_t b = b0 + lane;
+            tiles = b < a.requests ? tiles_of(a, b) : 0;
+            upto = sum + scan(tiles);
+        }
         const uint64_t past = __ballot(upto * per_request > from);
         if (past != 0) {
             const uint32_t at = __builtin_ctzll(past);
             request = b0 + at;
-            before = __shfl(upto - tiles, at) * per_request;
+            before = __builtin_amdgcn_readlane(upto - tiles, at) * per_request;
             break;
         }
-        sum = __shfl(upto, 63);
+        sum = __builtin_amdgcn_readlane(upto, 63);
     }
     request = __builtin_amdgcn_readfirstlane(request);
     before = __builtin_amdgcn_readfirstlane(before);
@@ -363,8 +347,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
             if (tile < tile_to) load_keys(b0, b1, in0, in1);   // under way while the weights are made
             walk.weigh(s);
             if (a.piece_lse != nullptr) {
-                const float w0 = over_pieces_sum((s[0] + s[1]) + (s[2] + s[3]));
-                const float w1 = over_pieces_sum((s[4] + s[5]) + (s[6] + s[7]));
+                const float w0 = over_rows_sum((s[0] + s[1]) + (s[2] + s[3]));
+                const float w1 = over_rows_sum((s[4] + s[5]) + (s[6] + s[7]));
                 if (g == 0 && i < heads) {
                     const uint32_t per_row = a.row_blocks * (a.block_tokens / kPiece);
                     float* to_row = a.piece_lse + ((size_t)request * a.kv_heads * a.group + first_head + i) * per_row +
@@ -383,7 +367,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
         }
 
         // The wavefronts' results as one.  A lane holds, of head i, channels kRun (4 g + r) + t.
-        walk.total = over_pieces_sum(walk.total);
+        walk.total = over_rows_sum(walk.total);
         __syncthreads();
         if (i < heads) {
 #pragma unroll
@@ -512,10 +496,17 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(AttendArgs a, const f
         const uint32_t pieces = (tokens + kPiece - 1) / kPiece, per_row = a.row_blocks * per_block;
         const float* at = a.piece_lse + (size_t)request * heads * per_row + j * per_block;
         const float* of = a.head_lse + (size_t)request * heads;
-        for (uint32_t h = heads * wave / kWaves; h < heads * (wave + 1) / kWaves; ++h)
-            for (uint32_t p = 0; p < pieces; ++p) {
-                const float x = at[(size_t)h * per_row + p];
-                sum += exp2_from(x, of[h]);
+        const uint32_t to = heads * (wave + 1) / kWaves;
+        for (uint32_t p = 0; p < pieces; ++p)
+            for (uint32_t h = heads * wave / kWaves; h < to; h += 8) {   // eight heads' loads under way together
+                float x[8], y[8];
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) {
+                    x[e] = h + e < to ? at[(size_t)(h + e) * per_row + p] : -INFINITY;
+                    y[e] = h + e < to ? of[h + e] : 0.f;
+                }
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) sum += exp2_from(x[e], y[e]);
             }
     }
     quarter[wave][lane] = sum;

@@ -86,12 +86,7 @@ __device__ __forceinline__ Chosen choose(Key key, uint32_t n, uint32_t want, Cho
             mine[e] = shared.bins[kBins - 1 - (threadIdx.x * kEach + e)];
             sum += mine[e];
         }
-        uint32_t upto = sum;
-#pragma unroll
-        for (uint32_t d = 1; d < 64; d *= 2) {
-            const uint32_t y = __shfl_up(upto, d);
-            if (lane >= d) upto += y;
-        }
+        const uint32_t upto = scan(sum);
         if (lane == 63) shared.able[wave] = upto;
         __syncthreads();
         uint32_t before = upto - sum;
@@ -172,36 +167,43 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     uint32_t want = asked <= 0 ? 0u : (uint32_t)asked;
     if (want > a.most) want = a.most;
     const uint32_t n = blocks > a.last ? blocks - a.last : 0;   // the last ones stay
-    auto made = [&](uint32_t i) {
-        if (i < a.first || (uint32_t)row[i] >= a.blocks) return kNever;
-        const float w = weights[i];
-        return w == w ? ~ordered(w) : 1u;
+    auto made = [&](uint32_t i, int32_t block, float w) {
+        return i < a.first || (uint32_t)block >= a.blocks ? kNever : w == w ? ~ordered(w) : 1u;
     };
     auto run = [&](auto key) {
         const Chosen c = choose(key, n, want, shared);
         put_in_order(key, n, c, shared, [&](uint32_t i, uint32_t place, bool chosen) {
-            const int32_t block = row[i];
-            if (chosen) {
-                victims[place] = (int32_t)i;
-                if (victim_blocks != nullptr) victim_blocks[place] = block;
-            }
-            if (row_out != nullptr) row_out[i] = chosen ? -1 : block;
+            if (!chosen) return;
+            victims[place] = (int32_t)i;
+            if (victim_blocks != nullptr) victim_blocks[place] = row[i];
+            if (row_out != nullptr) row_out[i] = -1;   // (a table that is changed in place: the last look at it)
         });
         for (uint32_t i = c.count + threadIdx.x; i < a.most; i += kThreads) {
             victims[i] = -1;
             if (victim_blocks != nullptr) victim_blocks[i] = -1;
         }
     };
-    if (n <= kLdsKeys) {
-        for (uint32_t i = threadIdx.x; i < n; i += kThreads) keys[i] = made(i);
-        __syncthreads();
-        run([&](uint32_t i) { return keys[i]; });
-    } else {
-        // (a table that is changed in place is read for the last time where it is written)
-        run(made);
+    const bool copied = row_out != nullptr && row_out != row;
+    // eight of a thread's places at once: their loads are under way together
+    for (uint32_t i0 = threadIdx.x; i0 < a.row_blocks; i0 += 8 * kThreads) {
+        int32_t block[8];
+        float w[8];
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) {
+            const uint32_t i = i0 + e * kThreads;
+            block[e] = i < a.row_blocks ? row[i] : -1;
+            w[e] = i < n ? weights[i] : 0.f;
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) {
+            const uint32_t i = i0 + e * kThreads;
+            if (i < n && i < kLdsKeys) keys[i] = made(i, block[e], w[e]);
+            if (i < a.row_blocks && copied) row_out[i] = block[e];
+        }
     }
-    if (row_out != nullptr)
-        for (uint32_t i = n + threadIdx.x; i < a.row_blocks; i += kThreads) row_out[i] = row[i];
+    __syncthreads();
+    if (n <= kLdsKeys) run([&](uint32_t i) { return keys[i]; });
+    else run([&](uint32_t i) { return made(i, row[i], weights[i]); });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -252,8 +254,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
                 if (!(fabsf(x[c]) < INFINITY)) x[c] = 0.f;
                 most = fmaxf(most, fabsf(x[c]));
             }
-#pragma unroll
-            for (uint32_t l = 1; l < 64; l *= 2) most = fmaxf(most, __shfl_xor(most, l));
+            most = over_rows_max(row_max(most));
             const bool small = !(most >= 1e-30f);
             const float by = small ? 0.f : 127.f / most;
 #pragma unroll
@@ -300,8 +301,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
                     const uint32_t b = 16 * s + 4 * g + r;
                     float score = (float)sum[r] * __shfl(scale, b) * qs;
                     if (i >= heads) score = -INFINITY;
-#pragma unroll
-                    for (uint32_t l = 1; l < 16; l *= 2) score = fmaxf(score, __shfl_xor(score, l));
+                    score = row_max(score);
                     if (i == 0 && j0 + b < to) {
                         uint32_t* key = &keys[j0 + b - from];
                         const uint32_t now = ordered(score);
@@ -332,7 +332,14 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
     if (parts > 1 && !last_to_arrive(a.arrived + list, parts, &last)) return;
     if (blocks <= kLdsKeys) {
         if (parts > 1)
-            for (uint32_t j = threadIdx.x; j < blocks; j += kThreads) keys[j] = get_shared(row_keys + j);
+            for (uint32_t j0 = threadIdx.x; j0 < blocks; j0 += 8 * kThreads) {   // eight loads under way together
+                uint32_t k[8];
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) k[e] = j0 + e * kThreads < blocks ? get_shared(row_keys + j0 + e * kThreads) : 0;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e)
+                    if (j0 + e * kThreads < blocks) keys[j0 + e * kThreads] = k[e];
+            }
         __syncthreads();
         run([&](uint32_t j) { return keys[j]; });
     } else {

@@ -122,6 +122,53 @@ __device__ __forceinline__ uint4 as_words(typename H::eight x) {
     return __builtin_bit_cast(uint4, x);
 }
 
+// Over the sixteen lanes of a row, and over the four rows: each lane gets the result.
+template <uint32_t kPattern>
+__device__ __forceinline__ float from_lane(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), kPattern, 0xF, 0xF, true));
+}
+constexpr uint32_t kPairs = 0xB1, kQuads = 0x4E, kMirrorEight = 0x141, kMirrorRow = 0x140;  // DPP: lanes 1, 2 apart; mirrored
+__device__ __forceinline__ float row_max(float x) {
+    x = fmaxf(x, from_lane<kPairs>(x));
+    x = fmaxf(x, from_lane<kQuads>(x));
+    x = fmaxf(x, from_lane<kMirrorEight>(x));
+    return fmaxf(x, from_lane<kMirrorRow>(x));
+}
+struct Two {
+    float a, b;
+};
+// of rows 0 and 1, 2 and 3: the first, the second of the pair; of both pairs of rows: the first, the second
+__device__ __forceinline__ Two of_row_pairs(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t a = y[0], b = y[1];   // (the builtin below does not take elements of a vector)
+    return Two{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ __forceinline__ Two of_halves(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a = y[0], b = y[1];   // (the builtin below does not take elements of a vector)
+    return Two{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ __forceinline__ float over_rows_max(float x) {
+    const Two p = of_row_pairs(x), h = of_halves(fmaxf(p.a, p.b));
+    return fmaxf(h.a, h.b);
+}
+__device__ __forceinline__ float over_rows_sum(float x) {
+    const Two p = of_row_pairs(x), h = of_halves(p.a + p.b);
+    return h.a + h.b;
+}
+// inclusive sums over the wavefront: in rows, then the rows before
+__device__ __forceinline__ uint32_t scan(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);  // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2 and 3
+    return x;
+}
+
 // Four-byte and eight-byte words that other workgroups of the launch read: written through to where every XCD
 // sees them, and read from there.  (A device-scope fence would write back or drop a whole L2.)
 template <class T>

@@ -48,6 +48,7 @@ class _Evict(C.Structure):
 
 
 _bound = None
+_marshal = None     # native marshalling (csrc/marshal.cpp), bound to _bound
 
 
 def _lib():
@@ -66,8 +67,21 @@ def _lib():
         for name in KV_EXPORTS:
             if name != "pgcm_kv_destroy":
                 getattr(lib, name).restype = C.c_int
+        from . import _marshal as m
+        m.kv_bind(*[C.cast(getattr(lib, "pgcm_kv_" + n), _vp).value
+                    for n in ("append", "attend", "summarize", "select", "evict")],
+                  torch.float16, torch.bfloat16, torch.int8, torch.int32, torch.int64, torch.float32)
+        global _marshal
+        _marshal = m
         _bound = lib
     return _bound
+
+
+def _native():
+    """the calls' native marshalling; like the batch calls', it leaves anything unusual, by returning None, to the code
+    here, which says what is wrong"""
+    _lib()
+    return _marshal
 
 
 def _ptr(t, what, dtype, shape, contiguous=True):
@@ -130,13 +144,14 @@ class KVWorkspace:
             pass
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _workspaces = {}    # (device, stream handle) -> KVWorkspace, of calls that name none
 _workspaces_lock = threading.Lock()
 
 
 def kv_workspace(stream=None) -> KVWorkspace:
     """the workspace that calls on this stream use unless they are given one"""
-    key = (torch.cuda.current_device(), _stream_handle(stream))
+    key = (_device(), _stream_handle(stream))
     got = _workspaces.get(key)
     if got is None:
         with _workspaces_lock:
@@ -158,6 +173,15 @@ def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=N
     """pgcm_kv_append: q, q_out [tokens, heads, head_dim] (or None: keys and values alone), k, v [tokens, kv_heads,
     head_dim], of the cache's type with contiguous channels; positions int32, slots int64 [tokens]; weights [head_dim]; rope
     float32 [positions, rope_dim], cosines then sines.  positions may be None if rope is."""
+    if not k.is_cuda:
+        raise ValueError("k must be a CUDA tensor")
+    h = _stream_handle(stream)
+    status = (_marshal or _native()).kv_append(cache._at, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope,
+                                               1 if adjacent else 0, h)
+    if status is not None:
+        if status:
+            _check(status)
+        return
     n, kv, d, half = k.shape[0], cache.kv_heads, cache.head_dim, cache.dtype
     heads = 0 if q is None else q.shape[1]
     a = _Append(n, heads)
@@ -179,7 +203,7 @@ def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=N
         a.rope = _ptr(rope, "rope", torch.float32, rope.shape)
         a.rope_positions, a.rope_dim = rope.shape
         a.adjacent = 1 if adjacent else 0
-    _check(_lib().pgcm_kv_append(cache._at, C.addressof(a), _stream_handle(stream)))
+    _check(_lib().pgcm_kv_append(cache._at, C.addressof(a), h))
 
 
 def kv_attend(cache, q, tables, lens, out, lse=None, scale=None, selected=None, weights=None, kept=None, decay=1.0,
@@ -187,12 +211,23 @@ def kv_attend(cache, q, tables, lens, out, lse=None, scale=None, selected=None, 
     """pgcm_kv_attend: q, out [requests, heads, head_dim] of the cache's type; tables int32 [requests, row_blocks]; lens
     int32 [requests]; lse float32 [requests, heads]; selected int32 [requests, kv_heads, keep]; weights, kept float32
     [requests, row_blocks].  scale: 1 / sqrt(head_dim) if None."""
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    h = _stream_handle(stream)
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    space = (workspace or kv_workspace(h))._h
+    status = (_marshal or _native()).kv_attend(space, cache._at, q, tables, lens, out, lse, scale, selected, weights, kept,
+                                               decay, h)
+    if status is not None:
+        if status:
+            _check(status)
+        return
     n, row, tables_at, lens_at = _rows(tables, lens)
     d, half = cache.head_dim, cache.dtype
     heads = q.shape[1]
-    h = _stream_handle(stream)
     a = _Attend(n, heads, _ptr(q, "q", half, (n, heads, d), False), *_strides(q), tables_at, *_strides(tables), row,
-                d ** -0.5 if scale is None else scale, lens_at)
+                scale, lens_at)
     a.out = _ptr(out, "out", half, (n, heads, d), False)
     a.out_request, a.out_head = _strides(out)
     if lse is not None:
@@ -204,42 +239,68 @@ def kv_attend(cache, q, tables, lens, out, lse=None, scale=None, selected=None, 
         a.weights, a.decay = _ptr(weights, "weights", torch.float32, (n, row)), decay
     if kept is not None:
         a.kept = _ptr(kept, "kept", torch.float32, (n, row))
-    _check(_lib().pgcm_kv_attend((workspace or kv_workspace(h))._h, cache._at, C.addressof(a), h))
+    _check(_lib().pgcm_kv_attend(space, cache._at, C.addressof(a), h))
 
 
 def kv_summarize(cache, blocks, counts, bounds, scales, entries=None, stream=None):
     """pgcm_kv_summarize: blocks, counts, entries int32 [n]; bounds int8 [entries, kv_heads, 2, head_dim]; scales float32
     [entries, kv_heads]"""
+    if not blocks.is_cuda:
+        raise ValueError("blocks must be a CUDA tensor")
+    h = _stream_handle(stream)
+    status = (_marshal or _native()).kv_summarize(cache._at, blocks, counts, bounds, scales, entries, h)
+    if status is not None:
+        if status:
+            _check(status)
+        return
     n, m = blocks.shape[0], bounds.shape[0]
     _check(_lib().pgcm_kv_summarize(
         cache._at, n, _ptr(blocks, "blocks", torch.int32, (n,)), _ptr(counts, "counts", torch.int32, (n,)),
         None if entries is None else _ptr(entries, "entries", torch.int32, (n,)), m,
         _ptr(bounds, "bounds", torch.int8, (m, cache.kv_heads, 2, cache.head_dim)),
-        _ptr(scales, "scales", torch.float32, (m, cache.kv_heads)), _stream_handle(stream)))
+        _ptr(scales, "scales", torch.float32, (m, cache.kv_heads)), h))
 
 
 def kv_select(q, tables, lens, bounds, scales, block_tokens, selected, counts=None, first=0, last=1, workspace=None,
               stream=None):
     """pgcm_kv_select: q [requests, heads, head_dim] float16 or bfloat16; tables int32 [requests, row_blocks] of entries of
     bounds; selected int32 [requests, kv_heads, keep]; counts int32 [requests, kv_heads]"""
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    h = _stream_handle(stream)
+    space = (workspace or kv_workspace(h))._h
+    status = (_marshal or _native()).kv_select(space, _HALVES.get(q.dtype, 0), q, tables, lens, bounds, scales, block_tokens,
+                                               selected, counts, first, last, h)
+    if status is not None:
+        if status:
+            _check(status)
+        return
     n, row, tables_at, lens_at = _rows(tables, lens)
     if q.dtype not in _HALVES or bounds.dim() != 4:
         raise ValueError("q must be float16 or bfloat16, bounds [entries, kv_heads, 2, head_dim]")
     m, kv, _, d = bounds.shape
     heads, keep = q.shape[1], selected.shape[-1]
-    h = _stream_handle(stream)
     a = _Select(n, heads, kv, d, _HALVES[q.dtype], block_tokens, _ptr(q, "q", q.dtype, (n, heads, d), False), *_strides(q),
                 tables_at, *_strides(tables), row, m, lens_at,
                 _ptr(bounds, "bounds", torch.int8, (m, kv, 2, d)), _ptr(scales, "scales", torch.float32, (m, kv)), keep, first,
                 last, _ptr(selected, "selected", torch.int32, (n, kv, keep)),
                 None if counts is None else _ptr(counts, "counts", torch.int32, (n, kv)))
-    _check(_lib().pgcm_kv_select((workspace or kv_workspace(h))._h, C.addressof(a), h))
+    _check(_lib().pgcm_kv_select(space, C.addressof(a), h))
 
 
 def kv_evict(weights, tables, lens, block_tokens, evict, victims, victim_blocks=None, tables_out=None, first=0, last=1,
              blocks=0x7FFFFFFF, stream=None):
     """pgcm_kv_evict: weights float32, tables and tables_out int32 [requests, row_blocks]; evict int32 [requests]; victims,
     victim_blocks int32 [requests, most].  blocks: of the pool; table entries outside [0, blocks) are not on the device."""
+    if not weights.is_cuda:
+        raise ValueError("weights must be a CUDA tensor")
+    h = _stream_handle(stream)
+    status = (_marshal or _native()).kv_evict(weights, tables, lens, block_tokens, evict, victims, victim_blocks, tables_out,
+                                              first, last, blocks, h)
+    if status is not None:
+        if status:
+            _check(status)
+        return
     n, row, tables_at, lens_at = _rows(tables, lens)
     most = victims.shape[-1]
     a = _Evict(n, row, block_tokens, blocks, _ptr(weights, "weights", torch.float32, (n, row)), tables_at, *_strides(tables),
@@ -250,4 +311,4 @@ def kv_evict(weights, tables, lens, block_tokens, evict, victims, victim_blocks=
     if tables_out is not None:
         a.tables_out = _ptr(tables_out, "tables_out", torch.int32, (n, row), False)
         a.table_out_row, = _strides(tables_out)
-    _check(_lib().pgcm_kv_evict(C.addressof(a), _stream_handle(stream)))
+    _check(_lib().pgcm_kv_evict(C.addressof(a), h))
