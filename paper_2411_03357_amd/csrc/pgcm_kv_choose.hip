@@ -5,9 +5,8 @@
 namespace pgcm_kv_impl {
 namespace {
 
-constexpr uint32_t kThreads = 512;
-constexpr uint32_t kWaves = kThreads / 64;
-constexpr uint32_t kLdsKeys = 16384;  // rows of more are read from memory at each look
+constexpr uint32_t kMostThreads = 1024;
+constexpr uint32_t kHeld = 16;        // keys that a lane holds in registers; longer rows are read from memory at each look
 constexpr uint32_t kBins = 2048;
 constexpr uint32_t kNever = 0, kAlways = 0xFFFFFFFFu;  // keys of what cannot be chosen, and of what is chosen before all others
 
@@ -17,9 +16,47 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
 
+// A row of n keys: each wavefront has an equal part of it, 64 keys a step.  each(f): f(i, key of i, step) step by step
+// for all lanes together, kNever beyond the row.
+template <uint32_t kThreads>
+struct Part {
+    uint32_t first, steps;
+    __device__ __forceinline__ explicit Part(uint32_t n) {
+        steps = (n + kThreads - 1) / kThreads;
+        first = threadIdx.x / 64 * 64 * steps + threadIdx.x % 64;
+    }
+};
+template <uint32_t kThreads>
+struct HeldKeys {
+    Part<kThreads> part;
+    uint32_t key[kHeld];
+    __device__ __forceinline__ explicit HeldKeys(uint32_t n) : part(n) {}
+    static bool __device__ __forceinline__ holds(uint32_t n) { return n <= kHeld * kThreads; }
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+        for (uint32_t s = 0; s < kHeld; ++s)
+            if (s < part.steps) f(part.first + 64 * s, key[s], s);
+    }
+};
+template <uint32_t kThreads, class Read>
+struct ReadKeys {
+    Part<kThreads> part;
+    uint32_t n;
+    Read read;
+    __device__ __forceinline__ ReadKeys(uint32_t n, Read read) : part(n), n(n), read(read) {}
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+        for (uint32_t s = 0; s < part.steps; ++s) {
+            const uint32_t i = part.first + 64 * s;
+            f(i, i < n ? read(i) : kNever, s);
+        }
+    }
+};
+
 struct ChooseShared {
     uint32_t bins[kBins];
-    uint32_t able[kWaves], always[kWaves], least[kWaves], most[kWaves];
+    uint32_t able[kMostThreads / 64], always[kMostThreads / 64], least[kMostThreads / 64], most[kMostThreads / 64];
     uint32_t bin, in_bin, need;
 };
 
@@ -28,38 +65,38 @@ struct Chosen {
     uint32_t above, equal, of_equal, count;
 };
 
-// The `want` largest of keys key(0) ... key(n - 1).  All threads call it.
-template <class Key>
-__device__ __forceinline__ Chosen choose(Key key, uint32_t n, uint32_t want, ChooseShared& shared) {
+// The sum of the figures of the wavefronts before this one.
+template <uint32_t kWaves>
+__device__ __forceinline__ uint32_t of_waves_before(const uint32_t* figures) {
+    const uint32_t lane = threadIdx.x % 64;
+    return over_wave(lane < threadIdx.x / 64 ? figures[lane] : 0u, [](uint32_t a, uint32_t b) { return a + b; });
+}
+
+// The `want` largest keys.  All threads call it.
+template <uint32_t kThreads, class Keys>
+__device__ __forceinline__ Chosen choose(const Keys& keys, uint32_t want, ChooseShared& shared) {
+    constexpr uint32_t kWaves = kThreads / 64;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const auto less = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
+    const auto more = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
     uint32_t able = 0, always = 0, least = kAlways, most = 0;
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        const uint32_t k = key(i);
-        able += k != kNever;
-        always += k == kAlways;
-        if (k != kNever && k != kAlways) {
-            least = k < least ? k : least;
-            most = k > most ? k : most;
-        }
-    }
-#pragma unroll
-    for (uint32_t l = 1; l < 64; l *= 2) {
-        able += __shfl_xor(able, l);
-        always += __shfl_xor(always, l);
-        const uint32_t x = __shfl_xor(least, l), y = __shfl_xor(most, l);
-        least = x < least ? x : least;
-        most = y > most ? y : most;
-    }
-    __syncthreads();
+    keys.each([&](uint32_t, uint32_t k, uint32_t) {
+        able += __builtin_popcountll(__ballot(k != kNever));
+        always += __builtin_popcountll(__ballot(k == kAlways));
+        const bool between = k != kNever && k != kAlways;
+        least = less(least, between ? k : kAlways);
+        most = more(most, between ? k : 0u);
+    });
+    least = over_wave(least, less);
+    most = over_wave(most, more);
+    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) shared.bins[b] = 0;
     if (lane == 0) shared.able[wave] = able, shared.always[wave] = always, shared.least[wave] = least, shared.most[wave] = most;
     __syncthreads();
-    able = always = most = 0, least = kAlways;
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        able += shared.able[w], always += shared.always[w];
-        least = shared.least[w] < least ? shared.least[w] : least;
-        most = shared.most[w] > most ? shared.most[w] : most;
-    }
+    // (a wavefront's figures in a lane each: sixteen wavefronts that read all of them one by one keep LDS busy for 0.5 us)
+    const bool has = lane < kWaves;
+    const auto plus = [](uint32_t a, uint32_t b) { return a + b; };
+    able = over_wave(has ? shared.able[lane] : 0u, plus), always = over_wave(has ? shared.always[lane] : 0u, plus);
+    least = over_wave(has ? shared.least[lane] : kAlways, less), most = over_wave(has ? shared.most[lane] : 0u, more);
     if (able <= want) return Chosen{kNever, kNever, 0, able};
     if (want == 0) return Chosen{kAlways, kNever, 0, 0};
     if (always >= want) return Chosen{kAlways, kAlways, want, want};
@@ -71,12 +108,9 @@ __device__ __forceinline__ Chosen choose(Key key, uint32_t n, uint32_t want, Cho
         const uint32_t width = most - least;
         const uint32_t bits = width == 0 ? 0 : 32 - __builtin_clz(width);
         const uint32_t shift = bits > 11 ? bits - 11 : 0;
-        for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) shared.bins[b] = 0;
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-            const uint32_t k = key(i);
+        keys.each([&](uint32_t, uint32_t k, uint32_t) {
             if (k >= least && k <= most) atomicAdd(&shared.bins[(k - least) >> shift], 1u);
-        }
+        });
         __syncthreads();
         // bins in threads from the top: kBins / kThreads each
         constexpr uint32_t kEach = kBins / kThreads;
@@ -89,8 +123,7 @@ __device__ __forceinline__ Chosen choose(Key key, uint32_t n, uint32_t want, Cho
         const uint32_t upto = scan(sum);
         if (lane == 63) shared.able[wave] = upto;
         __syncthreads();
-        uint32_t before = upto - sum;
-        for (uint32_t w = 0; w < wave; ++w) before += shared.able[w];
+        uint32_t before = upto - sum + of_waves_before<kWaves>(shared.able);
 #pragma unroll
         for (uint32_t e = 0; e < kEach; ++e) {
             if (before < need && before + mine[e] >= need) {
@@ -99,6 +132,7 @@ __device__ __forceinline__ Chosen choose(Key key, uint32_t n, uint32_t want, Cho
                 shared.need = need - before;
             }
             before += mine[e];
+            shared.bins[kBins - 1 - (threadIdx.x * kEach + e)] = 0;   // for the next look
         }
         __syncthreads();
         const uint32_t bin = shared.bin, in_bin = shared.in_bin;
@@ -106,41 +140,37 @@ __device__ __forceinline__ Chosen choose(Key key, uint32_t n, uint32_t want, Cho
         least += bin << shift;
         if (need == in_bin) return Chosen{least - 1, kNever, 0, want};   // (least is no key of kNever: at least 1)
         if (shift == 0) return Chosen{least, least, need, want};
-        const uint32_t end = least + ((1u << shift) - 1);
-        most = end < most ? end : most;
-        __syncthreads();
+        most = less(most, least + ((1u << shift) - 1));
     }
 }
 
-// put(i, place, chosen) for each i, with the places of the chosen ones in the order of i.
-template <class Key, class Put>
-__device__ __forceinline__ void put_in_order(Key key, uint32_t n, const Chosen& c, ChooseShared& shared, Put put) {
+// put(i, place, step) for each chosen i, with the places in the order of i.
+template <uint32_t kThreads, class Keys, class Put>
+__device__ __forceinline__ void put_in_order(const Keys& keys, const Chosen& c, ChooseShared& shared, Put put) {
+    constexpr uint32_t kWaves = kThreads / 64;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t each = (n + kThreads - 1) / kThreads * 64;   // a wavefront's part of the row
-    const uint32_t from = wave * each < n ? wave * each : n, to = from + each < n ? from + each : n;
     uint32_t above = 0, equal = 0;
-    for (uint32_t i = from; i < to; i += 64) {
-        const uint32_t k = i + lane < to ? key(i + lane) : kNever;
+    keys.each([&](uint32_t, uint32_t k, uint32_t) {
         above += __builtin_popcountll(__ballot(k > c.above));
         equal += __builtin_popcountll(__ballot(k == c.equal && c.of_equal != 0));
-    }
+    });
+    const bool any = (above | equal) != 0;
     __syncthreads();
     if (lane == 0) shared.able[wave] = above, shared.always[wave] = equal;
     __syncthreads();
-    above = equal = 0;
-    for (uint32_t w = 0; w < wave; ++w) above += shared.able[w], equal += shared.always[w];
+    above = of_waves_before<kWaves>(shared.able), equal = of_waves_before<kWaves>(shared.always);
+    if (!any) return;
     const uint64_t before_me = (1ull << lane) - 1;
-    for (uint32_t i = from; i < to; i += 64) {
-        const bool there = i + lane < to;
-        const uint32_t k = there ? key(i + lane) : kNever;
+    keys.each([&](uint32_t i, uint32_t k, uint32_t s) {
         const uint64_t is_above = __ballot(k > c.above), is_equal = __ballot(k == c.equal && c.of_equal != 0);
+        if ((is_above | is_equal) == 0) return;
         const uint32_t rank = equal + __builtin_popcountll(is_equal & before_me);
         const bool chosen = k > c.above || ((is_equal >> lane & 1) && rank < c.of_equal);
         const uint32_t place = above + __builtin_popcountll(is_above & before_me) + (rank < c.of_equal ? rank : c.of_equal);
-        if (there) put(i + lane, place, chosen);
+        if (chosen) put(i, place, s);
         above += __builtin_popcountll(is_above);
         equal += __builtin_popcountll(is_equal);
-    }
+    });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -152,9 +182,9 @@ struct EvictArgs {
     uint32_t row_blocks, block_tokens, blocks, most, first, last;
 };
 
+template <uint32_t kThreads>
 __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     __shared__ ChooseShared shared;
-    __shared__ uint32_t keys[kLdsKeys];
     const uint32_t request = blockIdx.x;
     const int32_t len = a.lens[request], asked = a.evict[request];
     const float* weights = a.weights + (size_t)request * a.row_blocks;
@@ -162,20 +192,22 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     int32_t* row_out = a.tables_out == nullptr ? nullptr : a.tables_out + request * a.table_out_row;
     int32_t* victims = a.victims + (size_t)request * a.most;
     int32_t* victim_blocks = a.victim_blocks == nullptr ? nullptr : a.victim_blocks + (size_t)request * a.most;
-    uint32_t blocks = len <= 0 ? 0u : ((uint32_t)len - 1) / a.block_tokens + 1;
-    if (blocks > a.row_blocks) blocks = a.row_blocks;
+    const bool copied = row_out != nullptr && row_out != row;
     uint32_t want = asked <= 0 ? 0u : (uint32_t)asked;
     if (want > a.most) want = a.most;
-    const uint32_t n = blocks > a.last ? blocks - a.last : 0;   // the last ones stay
+    auto candidates = [&]() {   // below this place: the last ones stay
+        uint32_t blocks = len <= 0 ? 0u : ((uint32_t)len - 1) / a.block_tokens + 1;
+        if (blocks > a.row_blocks) blocks = a.row_blocks;
+        return blocks > a.last ? blocks - a.last : 0u;
+    };
     auto made = [&](uint32_t i, int32_t block, float w) {
         return i < a.first || (uint32_t)block >= a.blocks ? kNever : w == w ? ~ordered(w) : 1u;
     };
-    auto run = [&](auto key) {
-        const Chosen c = choose(key, n, want, shared);
-        put_in_order(key, n, c, shared, [&](uint32_t i, uint32_t place, bool chosen) {
-            if (!chosen) return;
+    auto run = [&](const auto& keys, auto block_of) {
+        const Chosen c = choose<kThreads>(keys, want, shared);   // (its barriers are between the row's copy and the holes)
+        put_in_order<kThreads>(keys, c, shared, [&](uint32_t i, uint32_t place, uint32_t s) {
             victims[place] = (int32_t)i;
-            if (victim_blocks != nullptr) victim_blocks[place] = row[i];
+            if (victim_blocks != nullptr) victim_blocks[place] = block_of(i, s);
             if (row_out != nullptr) row_out[i] = -1;   // (a table that is changed in place: the last look at it)
         });
         for (uint32_t i = c.count + threadIdx.x; i < a.most; i += kThreads) {
@@ -183,27 +215,36 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
             if (victim_blocks != nullptr) victim_blocks[i] = -1;
         }
     };
-    const bool copied = row_out != nullptr && row_out != row;
-    // eight of a thread's places at once: their loads are under way together
-    for (uint32_t i0 = threadIdx.x; i0 < a.row_blocks; i0 += 8 * kThreads) {
-        int32_t block[8];
-        float w[8];
+    if (HeldKeys<kThreads>::holds(a.row_blocks)) {
+        // (parts of the whole row, so that its copy takes no look of its own; all loads are under way together)
+        HeldKeys<kThreads> keys(a.row_blocks);
+        int32_t block[kHeld];
+        float w[kHeld];
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) {
-            const uint32_t i = i0 + e * kThreads;
-            block[e] = i < a.row_blocks ? row[i] : -1;
-            w[e] = i < n ? weights[i] : 0.f;
+        for (uint32_t s = 0; s < kHeld; ++s) {
+            const uint32_t i = keys.part.first + 64 * s;
+            block[s] = s < keys.part.steps && i < a.row_blocks ? row[i] : -1;
+        }
+        const uint32_t n = candidates();
+#pragma unroll
+        for (uint32_t s = 0; s < kHeld; ++s) {
+            const uint32_t i = keys.part.first + 64 * s;
+            w[s] = s < keys.part.steps && i < n ? weights[i] : 0.f;
         }
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) {
-            const uint32_t i = i0 + e * kThreads;
-            if (i < n && i < kLdsKeys) keys[i] = made(i, block[e], w[e]);
-            if (i < a.row_blocks && copied) row_out[i] = block[e];
+        for (uint32_t s = 0; s < kHeld; ++s) {
+            const uint32_t i = keys.part.first + 64 * s;
+            keys.key[s] = i < n ? made(i, block[s], w[s]) : kNever;
+            if (copied && s < keys.part.steps && i < a.row_blocks) row_out[i] = block[s];
         }
+        run(keys, [&](uint32_t, uint32_t s) { return block[s]; });
+    } else {
+        const uint32_t n = candidates();
+        if (copied)
+            for (uint32_t i = threadIdx.x; i < a.row_blocks; i += kThreads) row_out[i] = row[i];
+        auto read = [&](uint32_t i) { return made(i, row[i], weights[i]); };
+        run(ReadKeys<kThreads, decltype(read)>(n, read), [&](uint32_t i, uint32_t) { return row[i]; });
     }
-    __syncthreads();
-    if (n <= kLdsKeys) run([&](uint32_t i) { return keys[i]; });
-    else run([&](uint32_t i) { return made(i, row[i], weights[i]); });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -219,17 +260,23 @@ struct SelectArgs {
     uint32_t kv_heads, group, head_dim, block_tokens, row_blocks, entry_count, keep, first, last, part;
 };
 
+constexpr uint32_t kSelectThreads = kMostThreads, kSelectWaves = kSelectThreads / 64;
+// blocks that a wavefront scores at a step: so many that the registers hold their bounds
+constexpr uint32_t step_of(uint32_t chunks) { return chunks == 8 ? 16 : 32; }
+constexpr uint32_t kMostPart = 8192;         // blocks of a workgroup, whose keys are in LDS
+
 // Part blockIdx.x of the blocks of a request for one kv head: their keys, and by whichever workgroup is the last of the
 // row the choice.  The scores are products on the matrix cores, of 2 head_dim whole numbers: the bounds of sixteen blocks
 // with, for each of sixteen query heads, its negative channels (for the least values) and its positive ones.
 template <class H, uint32_t kChunks>   // kChunks pieces of 64 numbers
-__global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a) {
+    constexpr uint32_t kStep = step_of(kChunks);
     __shared__ ChooseShared shared;
-    __shared__ uint32_t keys[kLdsKeys];
+    __shared__ uint32_t part_keys[kMostPart];
     __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
     __shared__ float q_scale[16];
     __shared__ uint32_t last;
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = lane / 16, i = lane % 16;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, i = lane % 16;
     const uint32_t head = blockIdx.y, request = blockIdx.z, list = request * a.kv_heads + head;
     const int32_t len = a.lens[request];
     uint32_t blocks = len <= 0 ? 0u : ((uint32_t)len - 1) / a.block_tokens + 1;
@@ -240,19 +287,41 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
     const int32_t* row = a.tables + request * a.table_row;
     const uint32_t numbers = 2 * a.head_dim;
     const uint64_t entry_bytes = (uint64_t)a.kv_heads * numbers;
+    const int8_t* of_head = a.bounds + (uint64_t)head * numbers;
 
+    i32x4 x[kStep / 16][kChunks];   // of the step in hand
+    float scale;
+    uint64_t able;
+    auto load = [&](uint32_t j0) {
+        const uint32_t j = j0 + lane % kStep;
+        uint32_t entry = j < to ? (uint32_t)row[j] : ~0u;
+        able = __ballot(entry < a.entry_count);
+        if (entry >= a.entry_count) entry = 0;   // not chosen, whatever its score
+        scale = a.scales[(uint64_t)entry * a.kv_heads + head];
+#pragma unroll
+        for (uint32_t s = 0; s < kStep / 16; ++s) {
+            const int8_t* at = of_head + __shfl(entry, 16 * s + i) * entry_bytes;
+#pragma unroll
+            for (uint32_t c = 0; c < kChunks; ++c) {   // (beyond the numbers anything that is there: the query has zeros)
+                const uint32_t d = 64 * c + 16 * g;
+                x[s][c] = *(const i32x4*)(at + (d < numbers ? d : 0));
+            }
+        }
+    };
+    const uint32_t j_first = from + kStep * wave;
     for (uint32_t head0 = 0; head0 < a.group; head0 += 16) {
         const uint32_t heads = a.group - head0 < 16 ? a.group - head0 : 16;
+        if (j_first < to) load(j_first);     // under way while the queries are made whole numbers
         __syncthreads();
-        for (uint32_t h = wave; h < 16; h += kWaves) {
+        for (uint32_t h = wave; h < 16; h += kSelectWaves) {
             const uint8_t* from_q = a.q + request * a.q_request + (head * a.group + head0 + h) * a.q_head;
-            float x[kChunks / 2], most = 0.f;
+            float y[kChunks / 2], most = 0.f;
 #pragma unroll
             for (uint32_t c = 0; c < kChunks / 2; ++c) {
                 const uint32_t d = 64 * c + lane;
-                x[c] = h < heads && d < a.head_dim ? (float)*(const typename H::one*)(from_q + 2 * d) : 0.f;
-                if (!(fabsf(x[c]) < INFINITY)) x[c] = 0.f;
-                most = fmaxf(most, fabsf(x[c]));
+                y[c] = h < heads && d < a.head_dim ? (float)*(const typename H::one*)(from_q + 2 * d) : 0.f;
+                if (!(fabsf(y[c]) < INFINITY)) y[c] = 0.f;
+                most = fmaxf(most, fabsf(y[c]));
             }
             most = over_rows_max(row_max(most));
             const bool small = !(most >= 1e-30f);
@@ -260,10 +329,10 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
 #pragma unroll
             for (uint32_t c = 0; c < kChunks / 2; ++c) {
                 const uint32_t d = 64 * c + lane;
-                const int32_t y = small ? 0 : (int32_t)rintf(x[c] * by);
+                const int32_t whole = small ? 0 : (int32_t)rintf(y[c] * by);
                 if (d < a.head_dim) {
-                    q8[h][d] = (int8_t)(y < 0 ? y : 0);
-                    q8[h][a.head_dim + d] = (int8_t)(y > 0 ? y : 0);
+                    q8[h][d] = (int8_t)(whole < 0 ? whole : 0);
+                    q8[h][a.head_dim + d] = (int8_t)(whole > 0 ? whole : 0);
                 }
             }
             for (uint32_t d = numbers + lane; d < 64 * kChunks; d += 64) q8[h][d] = 0;
@@ -275,83 +344,65 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectArgs a) {
         for (uint32_t c = 0; c < kChunks; ++c) q[c] = *(const i32x4*)&q8[i][64 * c + 16 * g];
         const float qs = q_scale[i];
 
-        for (uint32_t j0 = from + 64 * wave; j0 < to; j0 += 64 * kWaves) {
-            const uint32_t j = j0 + lane;
-            uint32_t entry = j < to ? (uint32_t)row[j] : 0;
-            if (entry >= a.entry_count) entry = 0;   // not chosen, whatever its score
-            const float scale = a.scales[(uint64_t)entry * a.kv_heads + head];
-            const int8_t* of_head = a.bounds + (uint64_t)head * numbers;
-            i32x4 x[4][kChunks];
+        for (uint32_t j0 = j_first; j0 < to;) {
+            // of the blocks 16 s + 4 g + r of a row of lanes, lane 4 s + r keeps its own
+            float own = 0.f;
 #pragma unroll
-            for (uint32_t s = 0; s < 4; ++s) {
-                const int8_t* at = of_head + __shfl(entry, 16 * s + i) * entry_bytes;
-#pragma unroll
-                for (uint32_t c = 0; c < kChunks; ++c) {
-                    x[s][c] = i32x4{0, 0, 0, 0};
-                    if (64 * c + 16 * g < numbers) x[s][c] = *(const i32x4*)(at + 64 * c + 16 * g);
-                }
-            }
-#pragma unroll
-            for (uint32_t s = 0; s < 4; ++s) {
+            for (uint32_t s = 0; s < kStep / 16; ++s) {
                 i32x4 sum{0, 0, 0, 0};
 #pragma unroll
                 for (uint32_t c = 0; c < kChunks; ++c) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[s][c], q[c], sum, 0, 0, 0);
 #pragma unroll
-                for (uint32_t r = 0; r < 4; ++r) {   // head i, block 4 g + r
-                    const uint32_t b = 16 * s + 4 * g + r;
-                    float score = (float)sum[r] * __shfl(scale, b) * qs;
-                    if (i >= heads) score = -INFINITY;
-                    score = row_max(score);
-                    if (i == 0 && j0 + b < to) {
-                        uint32_t* key = &keys[j0 + b - from];
-                        const uint32_t now = ordered(score);
-                        *key = head0 == 0 || now > *key ? now : *key;
-                    }
+                for (uint32_t r = 0; r < 4; ++r) {
+                    const float score = (float)sum[r] * __shfl(scale, 16 * s + 4 * g + r) * qs;   // of head i
+                    const float most = row_max(i < heads ? score : -INFINITY);
+                    own = i == 4 * s + r ? most : own;
                 }
             }
+            const uint32_t b = 16 * (i / 4) + 4 * g + i % 4, j = j0 + b;
+            if (i < kStep / 4 && j < to) {
+                uint32_t key = ordered(own);
+                if (head0 != 0 && part_keys[j - from] > key) key = part_keys[j - from];
+                if (j < a.first || blocks - j <= a.last) key = kAlways;
+                part_keys[j - from] = able >> b & 1 ? key : kNever;
+            }
+            j0 += kStep * kSelectWaves;
+            if (j0 < to) load(j0);
         }
     }
     __syncthreads();
-    uint32_t* row_keys = a.keys + (size_t)list * a.row_blocks;
-    for (uint32_t j = from + threadIdx.x; j < to; j += kThreads) {
-        uint32_t key = keys[j - from];
-        if ((uint32_t)row[j] >= a.entry_count) key = kNever;
-        else if (j < a.first || blocks - j <= a.last) key = kAlways;
-        if (parts == 1) keys[j] = key;
-        else put_shared(row_keys + j, key);
-    }
     int32_t* selected = a.selected + (size_t)list * a.keep;
-    auto run = [&](auto key) {
-        const Chosen c = choose(key, blocks, a.keep, shared);
-        put_in_order(key, blocks, c, shared, [&](uint32_t j, uint32_t place, bool chosen) {
-            if (chosen) selected[place] = (int32_t)j;
-        });
-        for (uint32_t n = c.count + threadIdx.x; n < a.keep; n += kThreads) selected[n] = -1;
+    auto run = [&](const auto& keys) {
+        const Chosen c = choose<kSelectThreads>(keys, a.keep, shared);
+        put_in_order<kSelectThreads>(keys, c, shared, [&](uint32_t j, uint32_t place, uint32_t) { selected[place] = (int32_t)j; });
+        for (uint32_t n = c.count + threadIdx.x; n < a.keep; n += kSelectThreads) selected[n] = -1;
         if (threadIdx.x == 0 && a.counts != nullptr) a.counts[list] = (int32_t)c.count;
     };
-    if (parts > 1 && !last_to_arrive(a.arrived + list, parts, &last)) return;
-    if (blocks <= kLdsKeys) {
-        if (parts > 1)
-            for (uint32_t j0 = threadIdx.x; j0 < blocks; j0 += 8 * kThreads) {   // eight loads under way together
-                uint32_t k[8];
+    uint32_t* row_keys = a.keys + (size_t)list * a.row_blocks;
+    if (parts > 1) {
+        for (uint32_t j = from + threadIdx.x; j < to; j += kSelectThreads) put_shared(row_keys + j, part_keys[j - from]);
+        if (!last_to_arrive(a.arrived + list, parts, &last)) return;
+    }
+    if (HeldKeys<kSelectThreads>::holds(blocks)) {
+        HeldKeys<kSelectThreads> keys(blocks);
 #pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) k[e] = j0 + e * kThreads < blocks ? get_shared(row_keys + j0 + e * kThreads) : 0;
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e)
-                    if (j0 + e * kThreads < blocks) keys[j0 + e * kThreads] = k[e];
-            }
-        __syncthreads();
-        run([&](uint32_t j) { return keys[j]; });
+        for (uint32_t s = 0; s < kHeld; ++s) {
+            const uint32_t j = keys.part.first + 64 * s;
+            keys.key[s] = kNever;
+            if (s < keys.part.steps && j < blocks) keys.key[s] = parts == 1 ? part_keys[j] : get_shared(row_keys + j);
+        }
+        run(keys);
     } else {
-        run([&](uint32_t j) { return get_shared(row_keys + j); });
+        auto read = [&](uint32_t j) { return get_shared(row_keys + j); };
+        run(ReadKeys<kSelectThreads, decltype(read)>(blocks, read));
     }
 }
 
 template <class H>
 void launch(const SelectArgs& a, dim3 grid, hipStream_t stream) {
-    if (a.head_dim <= 64) select_kernel<H, 2><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.head_dim <= 128) select_kernel<H, 4><<<grid, kThreads, 0, stream>>>(a);
-    else select_kernel<H, 8><<<grid, kThreads, 0, stream>>>(a);
+    if (a.head_dim <= 64) select_kernel<H, 2><<<grid, kSelectThreads, 0, stream>>>(a);
+    else if (a.head_dim <= 128) select_kernel<H, 4><<<grid, kSelectThreads, 0, stream>>>(a);
+    else select_kernel<H, 8><<<grid, kSelectThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -387,15 +438,16 @@ int pgcm_kv_select(pgcm_kv_t* kv, const pgcm_kv_select_args* args, void* hip_str
     a.kv_heads = args->kv_heads, a.group = args->heads / args->kv_heads, a.head_dim = args->head_dim;
     a.block_tokens = args->block_tokens, a.row_blocks = args->row_blocks, a.entry_count = args->entry_count;
     a.keep = args->keep, a.first = args->first, a.last = args->last;
-    // a row in one workgroup, or in several where rows alone would not fill the chip; of whole steps of 512 blocks
+    // a row in one workgroup, or in several where rows alone would not fill the chip; of whole steps
+    const uint32_t step_blocks = step_of(args->head_dim > 128 ? 8 : 4) * kSelectWaves;
     const uint64_t lists = (uint64_t)args->requests * args->kv_heads;
-    const uint32_t steps = (args->row_blocks + 64 * kWaves - 1) / (64 * kWaves);
-    uint32_t ways = lists >= 512 ? 1 : (uint32_t)((512 + lists - 1) / lists);
+    const uint32_t steps = (args->row_blocks + step_blocks - 1) / step_blocks;
+    uint32_t ways = lists >= 256 ? 1 : (uint32_t)((256 + lists - 1) / lists);
     if (ways > steps) ways = steps;
     if (ways == 0) ways = 1;
-    uint32_t part = (steps + ways - 1) / ways * 64 * kWaves;
-    if (part > kLdsKeys) part = kLdsKeys;
-    if (part == 0) part = 64 * kWaves;
+    uint32_t part = (steps + ways - 1) / ways * step_blocks;
+    if (part > kMostPart) part = kMostPart;
+    if (part == 0) part = step_blocks;
     a.part = part;
     const uint32_t parts = args->row_blocks == 0 ? 1 : (args->row_blocks + part - 1) / part;
     const dim3 grid(parts, args->kv_heads, args->requests);
@@ -420,7 +472,8 @@ int pgcm_kv_evict(const pgcm_kv_evict_args* args, void* hip_stream) {
     a.table_row = args->table_row, a.table_out_row = args->table_out_row;
     a.row_blocks = args->row_blocks, a.block_tokens = args->block_tokens, a.blocks = args->blocks;
     a.most = args->most, a.first = args->first, a.last = args->last;
-    evict_kernel<<<args->requests, kThreads, 0, (hipStream_t)hip_stream>>>(a);
+    if (a.row_blocks <= 4 * 256) evict_kernel<256><<<args->requests, 256, 0, (hipStream_t)hip_stream>>>(a);
+    else evict_kernel<kMostThreads><<<args->requests, kMostThreads, 0, (hipStream_t)hip_stream>>>(a);
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 

@@ -141,13 +141,13 @@ struct Two {
 __device__ __forceinline__ Two of_row_pairs(float x) {
     const uint32_t u = __builtin_bit_cast(uint32_t, x);
     const auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const uint32_t a = y[0], b = y[1];   // (the builtin below does not take elements of a vector)
+    const uint32_t a = y[0], b = y[1];   // (of an element of a vector, the cast below takes the vector's first)
     return Two{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
 }
 __device__ __forceinline__ Two of_halves(float x) {
     const uint32_t u = __builtin_bit_cast(uint32_t, x);
     const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    const uint32_t a = y[0], b = y[1];   // (the builtin below does not take elements of a vector)
+    const uint32_t a = y[0], b = y[1];   // (of an element of a vector, the cast below takes the vector's first)
     return Two{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
 }
 __device__ __forceinline__ float over_rows_max(float x) {
@@ -157,6 +157,18 @@ __device__ __forceinline__ float over_rows_max(float x) {
 __device__ __forceinline__ float over_rows_sum(float x) {
     const Two p = of_row_pairs(x), h = of_halves(p.a + p.b);
     return h.a + h.b;
+}
+// the least or largest whole number of the wavefront
+template <class Of>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, Of of) {
+    x = of(x, (uint32_t)__builtin_amdgcn_update_dpp(0, x, kPairs, 0xF, 0xF, true));
+    x = of(x, (uint32_t)__builtin_amdgcn_update_dpp(0, x, kQuads, 0xF, 0xF, true));
+    x = of(x, (uint32_t)__builtin_amdgcn_update_dpp(0, x, kMirrorEight, 0xF, 0xF, true));
+    x = of(x, (uint32_t)__builtin_amdgcn_update_dpp(0, x, kMirrorRow, 0xF, 0xF, true));
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = of(p[0], p[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return of(h[0], h[1]);
 }
 // inclusive sums over the wavefront: in rows, then the rows before
 __device__ __forceinline__ uint32_t scan(uint32_t x) {
