@@ -73,9 +73,8 @@ int pgcm_kv_reserve(pgcm_kv_t* kv, uint32_t requests, uint32_t heads, uint32_t k
     if (kv == nullptr) return PGCM_ERR_ARG;
     if (const int rc = check_sizes(requests, heads, kv_heads, head_dim, block_tokens, row_blocks)) return rc;
     const Room a = attend_room(requests, heads, kv_heads, head_dim, (uint64_t)row_blocks * (block_tokens / kPiece));
-    const Room s = select_room(requests, kv_heads, row_blocks);
-    return kv_ensure(kv, a.counters > s.counters ? a.counters : s.counters,
-                     a.scratch > s.scratch ? a.scratch : s.scratch, (hipStream_t)hip_stream);
+    const size_t s = select_room(requests, kv_heads, row_blocks);
+    return kv_ensure(kv, a.counters, a.scratch > s ? a.scratch : s, (hipStream_t)hip_stream);
 }
 
 #pragma GCC visibility pop

@@ -254,74 +254,94 @@ struct SelectArgs {
     const int8_t* bounds;
     const float* scales;
     int32_t *selected, *counts;
-    uint32_t *arrived, *keys;
+    uint32_t* keys;
     int64_t q_request, q_head;  // bytes
     int64_t table_row;
-    uint32_t kv_heads, group, head_dim, block_tokens, row_blocks, entry_count, keep, first, last, part;
+    uint32_t requests, kv_heads, group, head_dim, block_tokens, row_blocks, entry_count, keep, first, last;
+    uint32_t parts;  // of a row: workgroups that score it
 };
 
-constexpr uint32_t kSelectThreads = kMostThreads, kSelectWaves = kSelectThreads / 64;
-// blocks that a wavefront scores at a step: so many that the registers hold their bounds
-constexpr uint32_t step_of(uint32_t chunks) { return chunks == 8 ? 16 : 32; }
-constexpr uint32_t kMostPart = 8192;         // blocks of a workgroup, whose keys are in LDS
-
-// Part blockIdx.x of the blocks of a request for one kv head: their keys, and by whichever workgroup is the last of the
-// row the choice.  The scores are products on the matrix cores, of 2 head_dim whole numbers: the bounds of sixteen blocks
-// with, for each of sixteen query heads, its negative channels (for the least values) and its positive ones.
-template <class H, uint32_t kChunks>   // kChunks pieces of 64 numbers
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a) {
-    constexpr uint32_t kStep = step_of(kChunks);
-    __shared__ ChooseShared shared;
-    __shared__ uint32_t part_keys[kMostPart];
-    __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
-    __shared__ float q_scale[16];
-    __shared__ uint32_t last;
-    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, i = lane % 16;
-    const uint32_t head = blockIdx.y, request = blockIdx.z, list = request * a.kv_heads + head;
+__device__ __forceinline__ uint32_t blocks_of(const SelectArgs& a, uint32_t request) {
     const int32_t len = a.lens[request];
-    uint32_t blocks = len <= 0 ? 0u : ((uint32_t)len - 1) / a.block_tokens + 1;
-    if (blocks > a.row_blocks) blocks = a.row_blocks;
-    const uint32_t parts = blocks == 0 ? 1 : (blocks + a.part - 1) / a.part;
-    if (blockIdx.x >= parts) return;
-    const uint32_t from = blockIdx.x * a.part, to = from + a.part < blocks ? from + a.part : blocks;
-    const int32_t* row = a.tables + request * a.table_row;
+    const uint32_t blocks = len <= 0 ? 0u : ((uint32_t)len - 1) / a.block_tokens + 1;
+    return blocks < a.row_blocks ? blocks : a.row_blocks;
+}
+
+template <uint32_t kThreads, class Keys>
+__device__ __forceinline__ void choose_list(const SelectArgs& a, uint32_t list, const Keys& keys, ChooseShared& shared) {
+    int32_t* selected = a.selected + (size_t)list * a.keep;
+    const Chosen c = choose<kThreads>(keys, a.keep, shared);
+    put_in_order<kThreads>(keys, c, shared, [&](uint32_t j, uint32_t place, uint32_t) { selected[place] = (int32_t)j; });
+    for (uint32_t n = c.count + threadIdx.x; n < a.keep; n += kThreads) selected[n] = -1;
+    if (threadIdx.x == 0 && a.counts != nullptr) a.counts[list] = (int32_t)c.count;
+}
+
+constexpr uint32_t kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
+constexpr uint32_t kWaveBlocks = 64;                          // that a wavefront scores at a time, in four steps
+constexpr uint32_t kPartBlocks = kScoreWaves * kWaveBlocks;   // ... and a workgroup
+constexpr uint32_t kWholeBlocks = 1024;                       // rows of up to so many are scored and chosen from in one launch
+
+// Keys of the blocks [from, to) of a request for one kv head, at key_of(j).  The scores are products on the matrix cores,
+// of 2 head_dim whole numbers: for each of sixteen query heads, its negative channels (for the least values) and its
+// positive ones, with the bounds of sixteen blocks.  All threads call it; q8 and q_scale are theirs.
+template <class H, uint32_t kChunks, class KeyOf>   // kChunks pieces of 64 numbers
+__device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uint32_t head, uint32_t from, uint32_t to,
+                                      uint32_t blocks, int8_t (&q8)[16][64 * kChunks + 16], float (&q_scale)[16], KeyOf key_of) {
+    // what the registers hold of bounds: steps, and pieces of each
+    constexpr uint32_t kTogether = kChunks == 2 ? 4 : kChunks == 4 ? 2 : 1, kAtOnce = kChunks < 4 ? kChunks : 4;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, i = lane % 16;
     const uint32_t numbers = 2 * a.head_dim;
     const uint64_t entry_bytes = (uint64_t)a.kv_heads * numbers;
     const int8_t* of_head = a.bounds + (uint64_t)head * numbers;
+    const int32_t* row = a.tables + request * a.table_row;
 
-    i32x4 x[kStep / 16][kChunks];   // of the step in hand
-    float scale;
-    uint64_t able;
-    auto load = [&](uint32_t j0) {
-        const uint32_t j = j0 + lane % kStep;
-        uint32_t entry = j < to ? (uint32_t)row[j] : ~0u;
-        able = __ballot(entry < a.entry_count);
-        if (entry >= a.entry_count) entry = 0;   // not chosen, whatever its score
-        scale = a.scales[(uint64_t)entry * a.kv_heads + head];
-#pragma unroll
-        for (uint32_t s = 0; s < kStep / 16; ++s) {
-            const int8_t* at = of_head + __shfl(entry, 16 * s + i) * entry_bytes;
-#pragma unroll
-            for (uint32_t c = 0; c < kChunks; ++c) {   // (beyond the numbers anything that is there: the query has zeros)
-                const uint32_t d = 64 * c + 16 * g;
-                x[s][c] = *(const i32x4*)(at + (d < numbers ? d : 0));
-            }
-        }
-    };
-    const uint32_t j_first = from + kStep * wave;
     for (uint32_t head0 = 0; head0 < a.group; head0 += 16) {
         const uint32_t heads = a.group - head0 < 16 ? a.group - head0 : 16;
-        if (j_first < to) load(j_first);     // under way while the queries are made whole numbers
-        __syncthreads();
-        for (uint32_t h = wave; h < 16; h += kSelectWaves) {
-            const uint8_t* from_q = a.q + request * a.q_request + (head * a.group + head0 + h) * a.q_head;
-            float y[kChunks / 2], most = 0.f;
+        // queries in 8 bits: four heads a wavefront
+        float y[4][kChunks / 2];
+#pragma unroll
+        for (uint32_t n = 0; n < 4; ++n) {
+            const uint32_t h = 4 * wave + n;
+            const uint8_t* at = a.q + request * a.q_request + (head * a.group + head0 + (h < heads ? h : 0)) * a.q_head;
 #pragma unroll
             for (uint32_t c = 0; c < kChunks / 2; ++c) {
                 const uint32_t d = 64 * c + lane;
-                y[c] = h < heads && d < a.head_dim ? (float)*(const typename H::one*)(from_q + 2 * d) : 0.f;
-                if (!(fabsf(y[c]) < INFINITY)) y[c] = 0.f;
-                most = fmaxf(most, fabsf(y[c]));
+                y[n][c] = h < heads && d < a.head_dim ? (float)*(const typename H::one*)(at + 2 * d) : 0.f;
+            }
+        }
+        i32x4 x[kTogether][kAtOnce];          // bounds of some steps, or of half of each
+        uint32_t known;                       // entries of the wavefront's blocks; 0 for those that cannot be chosen
+        uint64_t able;
+        float scale;
+        auto load = [&](uint32_t t0, uint32_t first) {
+#pragma unroll
+            for (uint32_t t = 0; t < kTogether; ++t) {
+                const int8_t* at = of_head + __shfl(known, 16 * (t0 + t) + i) * entry_bytes;
+#pragma unroll
+                for (uint32_t c = 0; c < kAtOnce; ++c) {   // (beyond the numbers anything that is there: the query has zeros)
+                    const uint32_t d = 64 * (first + c) + 16 * g;
+                    x[t][c] = *(const i32x4*)(at + (d < numbers ? d : 0));
+                }
+            }
+        };
+        auto begin = [&](uint32_t j0) {
+            const uint32_t entry = j0 + lane < to ? (uint32_t)row[j0 + lane] : ~0u;
+            able = __ballot(entry < a.entry_count);
+            known = entry < a.entry_count ? entry : 0;
+            scale = a.scales[(uint64_t)known * a.kv_heads + head];
+            load(0, 0);
+        };
+        uint32_t j0 = from + kWaveBlocks * wave;
+        if (j0 < to) begin(j0);               // under way while the queries are made whole numbers
+        __syncthreads();
+#pragma unroll
+        for (uint32_t n = 0; n < 4; ++n) {
+            const uint32_t h = 4 * wave + n;
+            float most = 0.f;
+#pragma unroll
+            for (uint32_t c = 0; c < kChunks / 2; ++c) {
+                if (!(fabsf(y[n][c]) < INFINITY)) y[n][c] = 0.f;
+                most = fmaxf(most, fabsf(y[n][c]));
             }
             most = over_rows_max(row_max(most));
             const bool small = !(most >= 1e-30f);
@@ -329,7 +349,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a) {
 #pragma unroll
             for (uint32_t c = 0; c < kChunks / 2; ++c) {
                 const uint32_t d = 64 * c + lane;
-                const int32_t whole = small ? 0 : (int32_t)rintf(y[c] * by);
+                const int32_t whole = small ? 0 : (int32_t)rintf(y[n][c] * by);
                 if (d < a.head_dim) {
                     q8[h][d] = (int8_t)(whole < 0 ? whole : 0);
                     q8[h][a.head_dim + d] = (int8_t)(whole > 0 ? whole : 0);
@@ -342,67 +362,119 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a) {
         i32x4 q[kChunks];
 #pragma unroll
         for (uint32_t c = 0; c < kChunks; ++c) q[c] = *(const i32x4*)&q8[i][64 * c + 16 * g];
-        const float qs = q_scale[i];
+        float qs[4];
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) qs[r] = q_scale[4 * g + r];
 
-        for (uint32_t j0 = j_first; j0 < to;) {
-            // of the blocks 16 s + 4 g + r of a row of lanes, lane 4 s + r keeps its own
-            float own = 0.f;
+        while (j0 < to) {
 #pragma unroll
-            for (uint32_t s = 0; s < kStep / 16; ++s) {
-                i32x4 sum{0, 0, 0, 0};
+            for (uint32_t t0 = 0; t0 < 4; t0 += kTogether) {
+                i32x4 sum[kTogether];
 #pragma unroll
-                for (uint32_t c = 0; c < kChunks; ++c) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[s][c], q[c], sum, 0, 0, 0);
+                for (uint32_t first = 0; first < kChunks; first += kAtOnce) {
 #pragma unroll
-                for (uint32_t r = 0; r < 4; ++r) {
-                    const float score = (float)sum[r] * __shfl(scale, 16 * s + 4 * g + r) * qs;   // of head i
-                    const float most = row_max(i < heads ? score : -INFINITY);
-                    own = i == 4 * s + r ? most : own;
+                    for (uint32_t t = 0; t < kTogether; ++t)
+#pragma unroll
+                        for (uint32_t c = 0; c < kAtOnce; ++c)
+                            sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[first + c], x[t][c],
+                                                                           first + c == 0 ? i32x4{0, 0, 0, 0} : sum[t], 0, 0, 0);
+                    if (first + kAtOnce < kChunks) load(t0, first + kAtOnce);
+                    else if (t0 + kTogether < 4) load(t0 + kTogether, 0);
+                }
+#pragma unroll
+                for (uint32_t t = 0; t < kTogether; ++t) {
+                    const float of_block = __shfl(scale, 16 * (t0 + t) + i);
+                    float most = -INFINITY;      // of block i: heads 4 g + r, then those of all rows of lanes
+#pragma unroll
+                    for (uint32_t r = 0; r < 4; ++r)
+                        if (4 * g + r < heads) most = fmaxf(most, (float)sum[t][r] * of_block * qs[r]);
+                    most = over_rows_max(most);
+                    const uint32_t j = j0 + 16 * (t0 + t) + i;
+                    if (g == 0 && j < to) {
+                        uint32_t key = ordered(most);
+                        if (head0 != 0 && *key_of(j) > key) key = *key_of(j);
+                        if (j < a.first || blocks - j <= a.last) key = kAlways;
+                        *key_of(j) = able >> (16 * (t0 + t) + i) & 1 ? key : kNever;
+                    }
                 }
             }
-            const uint32_t b = 16 * (i / 4) + 4 * g + i % 4, j = j0 + b;
-            if (i < kStep / 4 && j < to) {
-                uint32_t key = ordered(own);
-                if (head0 != 0 && part_keys[j - from] > key) key = part_keys[j - from];
-                if (j < a.first || blocks - j <= a.last) key = kAlways;
-                part_keys[j - from] = able >> b & 1 ? key : kNever;
-            }
-            j0 += kStep * kSelectWaves;
-            if (j0 < to) load(j0);
+            j0 += kPartBlocks;
+            if (j0 < to) begin(j0);
         }
-    }
-    __syncthreads();
-    int32_t* selected = a.selected + (size_t)list * a.keep;
-    auto run = [&](const auto& keys) {
-        const Chosen c = choose<kSelectThreads>(keys, a.keep, shared);
-        put_in_order<kSelectThreads>(keys, c, shared, [&](uint32_t j, uint32_t place, uint32_t) { selected[place] = (int32_t)j; });
-        for (uint32_t n = c.count + threadIdx.x; n < a.keep; n += kSelectThreads) selected[n] = -1;
-        if (threadIdx.x == 0 && a.counts != nullptr) a.counts[list] = (int32_t)c.count;
-    };
-    uint32_t* row_keys = a.keys + (size_t)list * a.row_blocks;
-    if (parts > 1) {
-        for (uint32_t j = from + threadIdx.x; j < to; j += kSelectThreads) put_shared(row_keys + j, part_keys[j - from]);
-        if (!last_to_arrive(a.arrived + list, parts, &last)) return;
-    }
-    if (HeldKeys<kSelectThreads>::holds(blocks)) {
-        HeldKeys<kSelectThreads> keys(blocks);
-#pragma unroll
-        for (uint32_t s = 0; s < kHeld; ++s) {
-            const uint32_t j = keys.part.first + 64 * s;
-            keys.key[s] = kNever;
-            if (s < keys.part.steps && j < blocks) keys.key[s] = parts == 1 ? part_keys[j] : get_shared(row_keys + j);
-        }
-        run(keys);
-    } else {
-        auto read = [&](uint32_t j) { return get_shared(row_keys + j); };
-        run(ReadKeys<kSelectThreads, decltype(read)>(blocks, read));
     }
 }
 
+// Rows of any length, part by part.  The heads of a part, whose entries and scales share lines, run on one XCD; parts go to
+// the XCDs in turn.
+template <class H, uint32_t kChunks>
+__global__ __launch_bounds__(kScoreThreads, 4) void score_kernel(SelectArgs a) {
+    __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
+    __shared__ float q_scale[16];
+    const uint32_t in_xcd = blockIdx.x / kXcds, head = in_xcd % a.kv_heads;
+    const uint32_t part = in_xcd / a.kv_heads * kXcds + blockIdx.x % kXcds;
+    // (each row begins with another of its parts: those that every row has would otherwise all go to one XCD)
+    const uint32_t request = part / a.parts, from = (part + request) % a.parts * kPartBlocks;
+    if (request >= a.requests) return;
+    const uint32_t blocks = blocks_of(a, request);
+    if (from >= blocks) return;
+    const uint32_t to = blocks - from < kPartBlocks ? blocks : from + kPartBlocks;
+    uint32_t* keys = a.keys + ((size_t)request * a.kv_heads + head) * a.row_blocks;
+    score<H, kChunks>(a, request, head, from, to, blocks, q8, q_scale, [&](uint32_t j) { return keys + j; });
+}
+
+__global__ __launch_bounds__(kMostThreads) void choose_kernel(SelectArgs a) {
+    __shared__ ChooseShared shared;
+    const uint32_t list = blockIdx.x, blocks = blocks_of(a, list / a.kv_heads);
+    const uint32_t* row_keys = a.keys + (size_t)list * a.row_blocks;
+    if (HeldKeys<kMostThreads>::holds(blocks)) {
+        HeldKeys<kMostThreads> keys(blocks);
+#pragma unroll
+        for (uint32_t s = 0; s < kHeld; ++s) {
+            const uint32_t j = keys.part.first + 64 * s;
+            keys.key[s] = s < keys.part.steps && j < blocks ? row_keys[j] : kNever;
+        }
+        choose_list<kMostThreads>(a, list, keys, shared);
+    } else {
+        auto read = [&](uint32_t j) { return row_keys[j]; };
+        choose_list<kMostThreads>(a, list, ReadKeys<kMostThreads, decltype(read)>(blocks, read), shared);
+    }
+}
+
+// Short rows, a workgroup each.
+template <class H, uint32_t kChunks>
+__global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void select_kernel(SelectArgs a) {
+    __shared__ ChooseShared shared;
+    __shared__ uint32_t row_keys[kWholeBlocks];
+    __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
+    __shared__ float q_scale[16];
+    const uint32_t list = blockIdx.x, request = list / a.kv_heads, blocks = blocks_of(a, request);
+    score<H, kChunks>(a, request, list % a.kv_heads, 0, blocks, blocks, q8, q_scale, [&](uint32_t j) { return row_keys + j; });
+    __syncthreads();
+    HeldKeys<kScoreThreads> keys(blocks);
+#pragma unroll
+    for (uint32_t s = 0; s < kHeld; ++s) {
+        const uint32_t j = keys.part.first + 64 * s;
+        keys.key[s] = s < keys.part.steps && j < blocks ? row_keys[j] : kNever;
+    }
+    choose_list<kScoreThreads>(a, list, keys, shared);
+}
+
+template <class H, uint32_t kChunks>
+void launch(const SelectArgs& a, hipStream_t stream) {
+    const uint32_t lists = a.requests * a.kv_heads;
+    if (a.row_blocks <= kWholeBlocks) {
+        select_kernel<H, kChunks><<<lists, kScoreThreads, 0, stream>>>(a);
+        return;
+    }
+    const uint32_t parts = (a.requests * a.parts + kXcds - 1) / kXcds * kXcds;
+    score_kernel<H, kChunks><<<parts * a.kv_heads, kScoreThreads, 0, stream>>>(a);
+    choose_kernel<<<lists, kMostThreads, 0, stream>>>(a);
+}
 template <class H>
-void launch(const SelectArgs& a, dim3 grid, hipStream_t stream) {
-    if (a.head_dim <= 64) select_kernel<H, 2><<<grid, kSelectThreads, 0, stream>>>(a);
-    else if (a.head_dim <= 128) select_kernel<H, 4><<<grid, kSelectThreads, 0, stream>>>(a);
-    else select_kernel<H, 8><<<grid, kSelectThreads, 0, stream>>>(a);
+void launch(const SelectArgs& a, hipStream_t stream) {
+    if (a.head_dim <= 64) launch<H, 2>(a, stream);
+    else if (a.head_dim <= 128) launch<H, 4>(a, stream);
+    else launch<H, 8>(a, stream);
 }
 
 }  // namespace
@@ -427,32 +499,20 @@ int pgcm_kv_select(pgcm_kv_t* kv, const pgcm_kv_select_args* args, void* hip_str
         return PGCM_ERR_ARG;
     if (!aligned(args->q, args->q_request, args->q_head) || !aligned(args->bounds)) return PGCM_ERR_ALIGN;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const Room room = select_room(args->requests, args->kv_heads, args->row_blocks);
-    if (const int rc = kv_ensure(kv, room.counters, room.scratch, stream)) return rc;
+    const size_t room = select_room(args->requests, args->kv_heads, args->row_blocks);
+    if (const int rc = kv_ensure(kv, 0, room, stream)) return rc;
     SelectArgs a{};
     a.q = (const uint8_t*)args->q;
     a.tables = args->tables, a.lens = args->lens, a.bounds = args->bounds, a.scales = args->scales;
     a.selected = args->selected, a.counts = args->counts;
-    a.arrived = (uint32_t*)kv->counters.at, a.keys = (uint32_t*)kv->scratch.at;
+    a.keys = (uint32_t*)kv->scratch.at;
     a.q_request = 2 * args->q_request, a.q_head = 2 * args->q_head, a.table_row = args->table_row;
-    a.kv_heads = args->kv_heads, a.group = args->heads / args->kv_heads, a.head_dim = args->head_dim;
-    a.block_tokens = args->block_tokens, a.row_blocks = args->row_blocks, a.entry_count = args->entry_count;
-    a.keep = args->keep, a.first = args->first, a.last = args->last;
-    // a row in one workgroup, or in several where rows alone would not fill the chip; of whole steps
-    const uint32_t step_blocks = step_of(args->head_dim > 128 ? 8 : 4) * kSelectWaves;
-    const uint64_t lists = (uint64_t)args->requests * args->kv_heads;
-    const uint32_t steps = (args->row_blocks + step_blocks - 1) / step_blocks;
-    uint32_t ways = lists >= 256 ? 1 : (uint32_t)((256 + lists - 1) / lists);
-    if (ways > steps) ways = steps;
-    if (ways == 0) ways = 1;
-    uint32_t part = (steps + ways - 1) / ways * step_blocks;
-    if (part > kMostPart) part = kMostPart;
-    if (part == 0) part = step_blocks;
-    a.part = part;
-    const uint32_t parts = args->row_blocks == 0 ? 1 : (args->row_blocks + part - 1) / part;
-    const dim3 grid(parts, args->kv_heads, args->requests);
-    if (args->half == PGCM_KV_F16) launch<F16>(a, grid, stream);
-    else launch<Bf16>(a, grid, stream);
+    a.requests = args->requests, a.kv_heads = args->kv_heads, a.group = args->heads / args->kv_heads;
+    a.head_dim = args->head_dim, a.block_tokens = args->block_tokens, a.row_blocks = args->row_blocks;
+    a.entry_count = args->entry_count, a.keep = args->keep, a.first = args->first, a.last = args->last;
+    a.parts = (args->row_blocks + kPartBlocks - 1) / kPartBlocks;
+    if (args->half == PGCM_KV_F16) launch<F16>(a, stream);
+    else launch<Bf16>(a, stream);
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 

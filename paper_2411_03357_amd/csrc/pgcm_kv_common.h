@@ -29,6 +29,7 @@ namespace pgcm_kv_impl {
 constexpr uint32_t kPiece = 16;  // tokens of a matrix-core tile: a block is a whole number of pieces
 constexpr uint32_t kMaxHeadDim = 256;
 constexpr uint32_t kMaxHeads = 65535;
+constexpr uint32_t kXcds = 8;
 constexpr uint32_t kTileTokens = 128;  // tokens that a workgroup of attention takes at a step
 
 // At least so many bytes of zeroed counters and of scratch.
@@ -87,9 +88,9 @@ inline Room attend_room(uint32_t requests, uint32_t heads, uint32_t kv_heads, ui
                                            4 * (size_t)requests * heads * row_pieces};
 }
 
-// Selection: a counter for each request and kv head; a key for each of its blocks.
-inline Room select_room(uint32_t requests, uint32_t kv_heads, uint32_t row_blocks) {
-    return Room{4 * (size_t)requests * kv_heads, 4 * (size_t)requests * kv_heads * row_blocks};
+// Selection: a key for each block of a request and kv head.
+inline size_t select_room(uint32_t requests, uint32_t kv_heads, uint32_t row_blocks) {
+    return 4 * (size_t)requests * kv_heads * row_blocks;
 }
 
 // ---- device side
