@@ -44,7 +44,7 @@ typedef struct {
     uint32_t kv_heads;
     uint32_t head_dim;
     uint32_t reserved;     /* 0 */
-    int64_t k_block, k_token, k_head; /* strides in elements */
+    int64_t k_block, k_token, k_head; /* strides in elements; those of tokens in [0, 2^25] for pgcm_kv_attend */
     int64_t v_block, v_token, v_head;
 } pgcm_kv_cache;
 

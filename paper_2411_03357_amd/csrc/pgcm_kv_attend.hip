@@ -2,7 +2,12 @@
 //
 // Per request, kv head and group of up to sixteen of its query heads (an "item"):
 //   s[t][h] = scale k_t . q_h,   m = max s,   out = sum 2^(s - m) v_t / sum 2^(s - m)     (s in units of log 2)
-// with running m and sums, one pass over K and V.
+// with running m and sums, one pass over K and V.  What bounds it is memory: at sixteen heads an item, 2 flops a byte.
+//
+// The tiles of all items, 128 tokens each, are cut into equal spans, one for each workgroup, so that neither lengths nor their
+// number matter; an item of several workgroups is joined by the last of them.  A workgroup's four wavefronts take 32 tokens of
+// a tile each and are joined through LDS at an item's end; the next tile's rows, the next item's among them, are on their way
+// to LDS then.
 #include "pgcm_kv_common.h"
 
 #include <cmath>
@@ -12,7 +17,15 @@ namespace {
 
 constexpr uint32_t kWaves = 4;
 constexpr uint32_t kThreads = kWaves * 64;
-constexpr uint32_t kMinTiles = 2;  // a workgroup's span, where the batch has as many: less is not worth joining
+constexpr int64_t kMostTokenStride = 1 << 25;
+constexpr uint32_t kCus = 256;
+// Which workgroups there are, by the tiles of an item on average:
+//   up to kShortItem: one for each tile, if that fills no more than the chip; above, for two: joining more parts costs more than
+//   a tile does (one request of 4096 tokens, 8 kv heads: 15 us with two tiles each, 18 with one)
+//   from kLongItem on: one for each compute unit, whose four wavefronts have 64 KiB under way; with two, memory serves no more
+//   and in a worse order (1 GiB in 16 items: 201 us with one, 212 with two; 1280 items of 1 to 16 tiles, where one would be
+//   alone with each item's end: 115 and 95)
+constexpr uint32_t kShortItem = 8, kLongItem = 16;
 static_assert(kTileTokens == kWaves * 2 * kPiece, "two pieces a wavefront");
 
 struct AttendArgs {
@@ -27,6 +40,10 @@ struct AttendArgs {
     float scale;  // times log2 e
 };
 
+// A request's length, which nothing writes to while the kernel runs: so it may come through the scalar cache.
+__device__ __forceinline__ int32_t len_of(const AttendArgs& a, uint32_t request) {
+    return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.lens)[request];
+}
 __device__ __forceinline__ uint32_t clamped_len(const AttendArgs& a, int32_t len) {
     const uint32_t room = a.row_blocks * a.block_tokens;
     return len <= 0 ? 0u : (uint32_t)len < room ? (uint32_t)len : room;
@@ -37,20 +54,12 @@ __device__ __forceinline__ uint32_t walked(const AttendArgs& a, int32_t len) {
     return a.selected == nullptr || n == 0 ? n : a.keep * a.block_tokens;
 }
 __device__ __forceinline__ uint32_t tiles_of(const AttendArgs& a, uint32_t request) {
-    return (walked(a, a.lens[request]) + kTileTokens - 1) / kTileTokens;
+    return (walked(a, len_of(a, request)) + kTileTokens - 1) / kTileTokens;
 }
 
 __device__ __forceinline__ float exp2_from(float x, float top) {  // 0 for x = -inf, whatever the top
     return __builtin_amdgcn_exp2f(x - (top == -INFINITY ? 0.f : top));
 }
-
-template <uint32_t kDim>
-struct AttendShared {
-    float sum[kWaves][16][kDim + 4];
-    float top[kWaves][16], total[kWaves][16];
-    float part_top[64][16], part_total[64][16];
-    uint32_t last;
-};
 
 // How channels and tokens lie in a wavefront of lanes (g = lane / 16, i = lane % 16), for a tile of 32 tokens:
 //   K as the left operand, piece by piece: lane has token i, channels 32 c + 8 g ... + 7 in step c
@@ -58,160 +67,241 @@ struct AttendShared {
 //     tokens 4 g + r of the first piece and of the second as its eight of lane (g, i)
 //   V: lane loads, of its eight tokens, the kRun channels from kRun i (+ 128); row i of the left operand of product
 //     t is channel kRun i + t, so that the lane has all of its operands' words and only swaps halves of registers
-template <class H, uint32_t kDim, bool kExact>
-struct Walk {
+template <uint32_t kDim>
+struct Layout {
     static constexpr uint32_t kSteps = kDim / 32;               // of the first product
     static constexpr uint32_t kRun = kDim == 64 ? 4 : 8;        // channels of V that a lane loads at once
     static constexpr uint32_t kParts = kDim == 256 ? 2 : 1;     // ... so many times
     static constexpr uint32_t kWords = kRun / 2;                // 32-bit words of that
+    };
 
-    f32x4 sum[kParts][kRun];
+constexpr uint32_t kMergedHeads = 4;   // at a time
+template <uint32_t kDim>
+struct AttendShared {
+    __align__(4096) uint8_t rows[kWaves][4 * 16 * 2 * kDim];
+    union {
+        float sum[kWaves][kMergedHeads][kDim + 4];
+        struct {
+            float top[64][16], total[64][16];
+        } part;
+    };
+    float top[kWaves][16], total[kWaves][16];
+    uint32_t last;
+};
+
+// A wavefront's tile, 32 rows of K and of V, goes to LDS as it comes, without a register: lanes ask for whole rows, sixteen
+// for 256 bytes.  (Asked for in the layout of the first product, sixteen lanes would ask for sixteen rows of K, and the cache
+// serve each by itself: 64 accesses an instruction instead of 16, 42 million for 1 GiB of cache instead of 17.)  Sixteen
+// bytes p of row r of K are kept at place p ^ swap(r), so that those of sixteen rows lie in different banks.
+template <uint32_t kDim>
+struct Rows : Layout<kDim> {
+    typedef Layout<kDim> L;
+    static constexpr uint32_t kPlaces = kDim / 8;               // of a row
+    static constexpr uint32_t kRowsAtOnce = 64 / kPlaces;       // that an instruction asks for
+    static constexpr uint32_t kAsked = 16 / kRowsAtOnce;        // instructions a piece
+    static constexpr uint32_t kPieceBytes = 16 * 2 * kDim, kBytes = 4 * kPieceBytes;
+
+    uint32_t k_at[kAsked], v_at;   // where the lane's bytes lie from an instruction's first row on
+
+    static __device__ __forceinline__ uint32_t swap(uint32_t row) { return kDim == 64 ? row / 2 % 8 : row % 16; }
+
+    __device__ __forceinline__ Rows(const AttendArgs& a, uint32_t lane) {
+        const uint32_t row = lane / kPlaces, there = a.head_dim / 8;   // (beyond the channels: anything that is there)
+#pragma unroll
+        for (uint32_t n = 0; n < kAsked; ++n) {
+            const uint32_t p = (lane % kPlaces) ^ swap(n * kRowsAtOnce + row);
+            k_at[n] = row * (uint32_t)a.k_token + 16 * (p < there ? p : 0);
+        }
+        v_at = row * (uint32_t)a.v_token + 16 * (lane % kPlaces < there ? lane % kPlaces : 0);
+    }
+    // Sixteen rows from `row` on, to `to`.  An instruction's constant offset counts on both sides, so that the place in LDS
+    // is set for up to four of them at once.
+    template <class At>
+    static __device__ __forceinline__ void ask(uint64_t row, int64_t stride, uint8_t* to, At at) {
+        const int64_t step = (int64_t)kRowsAtOnce * stride - 1024;
+#pragma unroll
+        for (uint32_t n = 0; n < kAsked; ++n) {
+            asked<kAsked>(row + at(n), to + n / 4 * 4096, n % 4);
+            row += n % 4 == 3 ? step + 4096 : step;
+        }
+    }
+    template <uint32_t>
+    static __device__ __forceinline__ void asked(uint64_t from, uint8_t* to, uint32_t n) {
+        typedef const __attribute__((address_space(1))) void* Global;
+        typedef __attribute__((address_space(3))) void* Lds;
+        if (n == 0) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 0, 0);
+        if (n == 1) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 1024, 0);
+        if (n == 2) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 2048, 0);
+        if (n == 3) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 3072, 0);
+    }
+    // k, v: addresses of the rows of the piece's first token; lds: K of both pieces, then V of both
+    __device__ __forceinline__ void ask_piece(const AttendArgs& a, uint8_t* lds, uint32_t which, uint64_t k, uint64_t v) const {
+        ask(k, a.k_token, lds + which * kPieceBytes, [&](uint32_t n) { return k_at[n]; });
+        ask(v, a.v_token, lds + (2 + which) * kPieceBytes, [&](uint32_t) { return v_at; });
+    }
+};
+
+// What a wavefront holds of a tile: K as the operand of the first product, V as rows.
+template <uint32_t kDim, bool kExact>
+struct Held : Layout<kDim> {
+    typedef Layout<kDim> L;
+    uint4 k[2][L::kSteps];
+    uint32_t v[L::kParts][8][L::kWords];
+
+    __device__ __forceinline__ void take(const AttendArgs& a, const uint8_t* lds, uint32_t g, uint32_t i) {
+#pragma unroll
+        for (uint32_t c = 0; c < L::kSteps; ++c)
+#pragma unroll
+            for (uint32_t which = 0; which < 2; ++which) {
+                k[which][c] = *(const uint4*)(lds + which * Rows<kDim>::kPieceBytes + i * 2 * kDim +
+                                              ((4 * c + g) ^ Rows<kDim>::swap(i)) * 16);
+                if (!kExact && 32 * c + 8 * g >= a.head_dim) k[which][c] = make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+        for (uint32_t p = 0; p < L::kParts; ++p)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                const uint8_t* at = lds + (2 + j / 4) * Rows<kDim>::kPieceBytes + (4 * g + j % 4) * 2 * kDim + 256 * p + 2 * L::kRun * i;
+                if constexpr (L::kWords == 4) {
+                    const uint4 x = *(const uint4*)at;
+                    v[p][j][0] = x.x, v[p][j][1] = x.y, v[p][j][2] = x.z, v[p][j][3] = x.w;
+                } else {
+                    const uint2 x = *(const uint2*)at;
+                    v[p][j][0] = x.x, v[p][j][1] = x.y;
+                }
+            }
+    }
+    // rows of tokens that are not there count as zero, whatever they hold
+    __device__ __forceinline__ void drop_v(uint32_t which, uint32_t valid, uint32_t g) {
+#pragma unroll
+        for (uint32_t p = 0; p < L::kParts; ++p)
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r)
+#pragma unroll
+                for (uint32_t w = 0; w < L::kWords; ++w)
+                    v[p][4 * which + r][w] = 4 * g + r < valid ? v[p][4 * which + r][w] : 0u;
+    }
+};
+
+template <class H, uint32_t kDim, bool kExact>
+struct Walk : Layout<kDim> {
+    typedef Layout<kDim> L;
+    f32x4 sum[L::kParts][L::kRun];
     float top, total;
-    uint4 q[kSteps], k[2][kSteps];
-    uint32_t v[kParts][8][kWords];
+    uint4 q[L::kSteps];
 
-    __device__ __forceinline__ void begin(const AttendArgs& a, const uint8_t* row, bool there, uint32_t g) {
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (uint32_t p = 0; p < kParts; ++p)
+        for (uint32_t p = 0; p < L::kParts; ++p)
 #pragma unroll
-            for (uint32_t t = 0; t < kRun; ++t) sum[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (uint32_t t = 0; t < L::kRun; ++t) sum[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         top = -INFINITY;
         total = 0.f;
+    }
+    __device__ __forceinline__ void load_q(const AttendArgs& a, const uint8_t* row, bool there, uint32_t g) {
 #pragma unroll
-        for (uint32_t c = 0; c < kSteps; ++c) {
+        for (uint32_t c = 0; c < L::kSteps; ++c) {
             const uint32_t d = 32 * c + 8 * g;
             q[c] = make_uint4(0, 0, 0, 0);
             if (there && (kExact || d < a.head_dim)) q[c] = *(const uint4*)(row + 2 * d);
         }
     }
-    __device__ __forceinline__ void load_k(const AttendArgs& a, uint32_t which, const uint8_t* lane_row, uint32_t g) {
+    __device__ __forceinline__ void scores(float (&s)[8], const Held<kDim, kExact>& held, float scale, uint32_t valid0,
+                                           uint32_t valid1, uint32_t g) const {
+        f32x4 s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (uint32_t c = 0; c < kSteps; ++c) {
-            const uint32_t d = 32 * c + 8 * g;
-            if (kExact || d < a.head_dim)
-                k[which][c] = *(const uint4*)(lane_row + 2 * d);
-            else
-                k[which][c] = make_uint4(0, 0, 0, 0);
+        for (uint32_t c = 0; c < L::kSteps; ++c) {
+            s0 = H::product(as_eight<H>(held.k[0][c]), as_eight<H>(q[c]), s0);
+            s1 = H::product(as_eight<H>(held.k[1][c]), as_eight<H>(q[c]), s1);
         }
-    }
-    // first_row: of the lane's first token in the piece
-    __device__ __forceinline__ void load_v(const AttendArgs& a, uint32_t which, const uint8_t* first_row, uint32_t i) {
 #pragma unroll
-        for (uint32_t p = 0; p < kParts; ++p) {
-            const uint32_t d = 128 * p + kRun * i;
+        for (uint32_t r = 0; r < 4; ++r) s[r] = s0[r] * scale, s[4 + r] = s1[r] * scale;
+        if (valid0 < kPiece || valid1 < kPiece) {
 #pragma unroll
             for (uint32_t r = 0; r < 4; ++r) {
-                uint32_t(&to)[kWords] = v[p][4 * which + r];
-                if (kExact || d < a.head_dim) {
-                    const uint8_t* from = first_row + r * a.v_token + 2 * d;
-                    if constexpr (kWords == 4) {
-                        const uint4 x = *(const uint4*)from;
-                        to[0] = x.x, to[1] = x.y, to[2] = x.z, to[3] = x.w;
-                    } else {
-                        const uint2 x = *(const uint2*)from;
-                        to[0] = x.x, to[1] = x.y;
-                    }
-                } else {
-#pragma unroll
-                    for (uint32_t w = 0; w < kWords; ++w) to[w] = 0;
-                }
+                s[r] = 4 * g + r < valid0 ? s[r] : -INFINITY;
+                s[4 + r] = 4 * g + r < valid1 ? s[4 + r] : -INFINITY;
             }
         }
     }
-    // rows of tokens that are not there count as zero, whatever they hold
-    __device__ __forceinline__ void drop_v(uint32_t which, uint32_t valid, uint32_t g) {
-#pragma unroll
-        for (uint32_t p = 0; p < kParts; ++p)
-#pragma unroll
-            for (uint32_t r = 0; r < 4; ++r)
-#pragma unroll
-                for (uint32_t w = 0; w < kWords; ++w)
-                    v[p][4 * which + r][w] = 4 * g + r < valid ? v[p][4 * which + r][w] : 0u;
-    }
-    __device__ __forceinline__ void scores(float (&s)[8], float scale, uint32_t valid0, uint32_t valid1, uint32_t g) const {
-        f32x4 s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (uint32_t c = 0; c < kSteps; ++c) {
-            s0 = H::product(as_eight<H>(k[0][c]), as_eight<H>(q[c]), s0);
-            s1 = H::product(as_eight<H>(k[1][c]), as_eight<H>(q[c]), s1);
-        }
-#pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) {
-            s[r] = 4 * g + r < valid0 ? s0[r] * scale : -INFINITY;
-            s[4 + r] = 4 * g + r < valid1 ? s1[r] * scale : -INFINITY;
-        }
-    }
-    // running maximum and sum; the scores become weights
+    // Sums are kept relative to a score that is no further than kSlack below the largest one so far, in units of log 2: then
+    // weights are at most 2^kSlack, and the sums need not be brought up to each new maximum.  The scores become weights.
+    static constexpr float kSlack = 8.f;
     __device__ __forceinline__ void weigh(float (&s)[8]) {
         float most = s[0];
 #pragma unroll
         for (uint32_t j = 1; j < 8; ++j) most = fmaxf(most, s[j]);
         most = over_rows_max(most);
-        if (__any(most > top)) {
+        if (__any(most > top + kSlack || (top == -INFINITY && most > top))) {
             const float now = fmaxf(most, top), keep = exp2_from(top, now);
             top = now;
             total *= keep;
 #pragma unroll
-            for (uint32_t p = 0; p < kParts; ++p)
+            for (uint32_t p = 0; p < L::kParts; ++p)
 #pragma unroll
-                for (uint32_t t = 0; t < kRun; ++t) sum[p][t] *= keep;
+                for (uint32_t t = 0; t < L::kRun; ++t) sum[p][t] *= keep;
         }
+        const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j) {
-            s[j] = exp2_from(s[j], top);
+            s[j] = __builtin_amdgcn_exp2f(s[j] - from);
             total += s[j];
         }
     }
-    __device__ __forceinline__ void add_v(const float (&s)[8]) {
+    __device__ __forceinline__ void add_v(const float (&s)[8], const Held<kDim, kExact>& held) {
         // A weight goes to the matrix cores as two halves, the second what the first leaves: with one, its rounding
         // would be as large as that of the output.
         typename H::eight high, low;
+        H::split(s, high, low);
+        typename H::eight x[L::kParts][L::kRun];
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            high[j] = (typename H::one)s[j];
-            low[j] = (typename H::one)(s[j] - (float)high[j]);
-        }
+        for (uint32_t p = 0; p < L::kParts; ++p)
 #pragma unroll
-        for (uint32_t p = 0; p < kParts; ++p)
-#pragma unroll
-            for (uint32_t t = 0; t < kRun; ++t) {
+            for (uint32_t t = 0; t < L::kRun; ++t) {
                 const uint32_t pick = t % 2 ? 0x07060302u : 0x05040100u;
-                const uint4 x = make_uint4(__builtin_amdgcn_perm(v[p][1][t / 2], v[p][0][t / 2], pick),
-                                           __builtin_amdgcn_perm(v[p][3][t / 2], v[p][2][t / 2], pick),
-                                           __builtin_amdgcn_perm(v[p][5][t / 2], v[p][4][t / 2], pick),
-                                           __builtin_amdgcn_perm(v[p][7][t / 2], v[p][6][t / 2], pick));
-                sum[p][t] = H::product(as_eight<H>(x), high, sum[p][t]);
-                sum[p][t] = H::product(as_eight<H>(x), low, sum[p][t]);
+                x[p][t] = as_eight<H>(make_uint4(__builtin_amdgcn_perm(held.v[p][1][t / 2], held.v[p][0][t / 2], pick),
+                                                 __builtin_amdgcn_perm(held.v[p][3][t / 2], held.v[p][2][t / 2], pick),
+                                                 __builtin_amdgcn_perm(held.v[p][5][t / 2], held.v[p][4][t / 2], pick),
+                                                 __builtin_amdgcn_perm(held.v[p][7][t / 2], held.v[p][6][t / 2], pick)));
+                sum[p][t] = H::product(x[p][t], high, sum[p][t]);
             }
+#pragma unroll
+        for (uint32_t p = 0; p < L::kParts; ++p)
+#pragma unroll
+            for (uint32_t t = 0; t < L::kRun; ++t) sum[p][t] = H::product(x[p][t], low, sum[p][t]);
     }
 };
 
-// Where a wavefront's pieces lie: lane l holds its l-th from `first` on (two of each tile).
-struct Pieces {
-    uint32_t block;   // number, or ~0: masked
-    uint32_t inside;  // token of the block in the low half, how many of its sixteen are there in the high one
+// What a workgroup walks over at a time: up to 32 tiles of an item.
+struct Segment {
+    uint32_t request, before, tiles;  // the request's first tile of all, and the tiles of each of its items
+    uint32_t item, tile, tile_to;     // of the request; of the item
 };
-__device__ __forceinline__ Pieces find_pieces(const AttendArgs& a, const int32_t* row, const int32_t* picked, uint32_t len,
-                                              uint32_t tile, uint32_t last_tile, uint32_t wave, uint32_t lane) {
-    Pieces p{~0u, 0u};
-    const uint32_t t = tile + lane / 2;
-    if (t >= last_tile) return p;
+
+// Where a wavefront's pieces of a segment lie: lane l has its l-th, two of each tile.
+struct Pieces {
+    uint32_t block;          // number; anything out of the pool, e.g. ~0: masked
+    uint32_t inside, valid;  // token of the block; how many of its sixteen are there
+};
+__device__ __forceinline__ Pieces find_pieces(const AttendArgs& a, const Segment& s, uint32_t wave, uint32_t lane) {
+    Pieces p{~0u, 0u, 0u};
+    const uint32_t t = s.tile + lane / 2;
+    if (t >= s.tile_to) return p;
     const uint32_t piece = t * (kTileTokens / kPiece) + 2 * wave + (lane & 1);
     const uint32_t per_block = a.block_tokens / kPiece;
     uint32_t place = piece / per_block;
     const uint32_t inside = (piece - place * per_block) * kPiece;
-    if (picked != nullptr) {
+    if (a.selected != nullptr) {
         if (place >= a.keep) return p;
-        place = (uint32_t)picked[place];
+        place = (uint32_t)a.selected[((size_t)s.request * a.kv_heads + s.item / a.group_tiles) * a.keep + place];
     }
     if (place >= a.row_blocks) return p;
+    const uint32_t len = clamped_len(a, len_of(a, s.request));
     const uint64_t token = (uint64_t)place * a.block_tokens + inside;
     if (token >= len) return p;
-    const uint32_t block = (uint32_t)row[place];
-    if (block >= a.blocks) return p;
-    const uint64_t valid = len - token < kPiece ? len - token : kPiece;
-    p.block = block;
-    p.inside = inside | (uint32_t)valid << 16;
+    p.valid = len - token < kPiece ? (uint32_t)(len - token) : kPiece;
+    p.inside = inside;
+    p.block = (uint32_t)a.tables[s.request * a.table_row + place];   // (looked at when it is used)
     return p;
 }
 
@@ -223,13 +313,13 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     const uint32_t g = lane / 16, i = lane % 16;
     const uint32_t per_request = a.kv_heads * a.group_tiles;
 
-    // The tiles of all items, in the order of requests and heads, in equal spans: this workgroup's is [from, to).
-    uint32_t all = 0, tiles = 0, upto = 0;   // those of up to 64 requests, and of all before and with them
+    // The tiles of all items
+    uint32_t some = 0, all = 0, tiles = 0;   // requests with any; all tiles; those of request `lane`, or of the last 64
     for (uint32_t b0 = 0; b0 < a.requests; b0 += 64) {
         const uint32_t b = b0 + lane;
         tiles = b < a.requests ? tiles_of(a, b) : 0;
-        upto = all + scan(tiles);
-        all = __builtin_amdgcn_readlane(upto, 63);
+        all += __builtin_amdgcn_readlane(scan(tiles), 63);
+        some += __builtin_popcountll(__ballot(tiles != 0));
         // requests without tokens are answered here
         uint64_t empty = __ballot(b < a.requests && tiles == 0 && b % gridDim.x == blockIdx.x);
         for (; empty != 0; empty &= empty - 1) {
@@ -243,9 +333,12 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
         }
     }
     all *= per_request;
+    some *= per_request;
     if (all == 0) return;
-    const uint32_t least = (all + kMinTiles - 1) / kMinTiles;
-    const uint32_t groups = gridDim.x < least ? gridDim.x : least;
+    // ... in the order of requests and heads, are cut into equal spans: this workgroup's is [from, to).
+    const uint32_t by_tiles = all / some <= kShortItem ? all : (all + 1) / 2, useful = by_tiles > some ? by_tiles : some;
+    uint32_t groups = all / some >= kLongItem && gridDim.x > kCus ? kCus : gridDim.x;
+    if (groups > useful) groups = useful;
     if (blockIdx.x >= groups) return;
     auto start_of = [&](uint32_t w) { return (uint32_t)((uint64_t)w * all / groups); };
     auto owner_of = [&](uint32_t tile) { return (uint32_t)((((uint64_t)tile + 1) * groups - 1) / all); };
@@ -254,11 +347,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     // the request that the span begins in, and its first tile
     uint32_t request = 0, before = 0;
     for (uint32_t b0 = 0, sum = 0; b0 < a.requests; b0 += 64) {
-        if (a.requests > 64) {
-            const uint32_t b = b0 + lane;
-            tiles = b < a.requests ? tiles_of(a, b) : 0;
-            upto = sum + scan(tiles);
-        }
+        if (a.requests > 64) tiles = b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
+        const uint32_t upto = sum + scan(tiles);
         const uint64_t past = __ballot(upto * per_request > from);
         if (past != 0) {
             const uint32_t at = __builtin_ctzll(past);
@@ -271,119 +361,139 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     request = __builtin_amdgcn_readfirstlane(request);
     before = __builtin_amdgcn_readfirstlane(before);
 
+    // the segment that begins at a tile
+    auto segment_at = [&](uint32_t at, uint32_t request, uint32_t before) {
+        Segment s{request, before, tiles_of(a, request), 0, 0, 0};
+        while (at >= s.before + s.tiles * per_request) {
+            s.before += s.tiles * per_request;
+            s.tiles = tiles_of(a, ++s.request);
+        }
+        s.item = (at - s.before) / s.tiles;
+        const uint32_t item_from = s.before + s.item * s.tiles;
+        s.tile = at - item_from;
+        const uint32_t item_to = item_from + s.tiles, end = to < item_to ? to : item_to;
+        s.tile_to = end - at < 32 ? end - item_from : s.tile + 32;
+        return s;
+    };
+
     W walk;
-    for (uint32_t at = from; at < to;) {
-        uint32_t tiles = tiles_of(a, request);
-        while (at >= before + tiles * per_request) {
-            before += tiles * per_request;
-            tiles = tiles_of(a, ++request);
+    const Rows<kDim> rows(a, lane);
+    // of the segment's pieces, lane by lane: how many tokens are there (none: masked), and where their rows lie
+    uint32_t piece_valid;
+    uint64_t piece_k, piece_v;
+    uint64_t live;                  // those that are not masked, from the tile in hand on
+    uint32_t valid0, valid1, in_segment;   // the next tile
+    uint64_t k0, k1, v0, v1;
+    auto lane_of = [](uint64_t x, uint32_t j) {
+        const uint32_t low = __builtin_amdgcn_readlane((uint32_t)x, j), high = __builtin_amdgcn_readlane((uint32_t)(x >> 32), j);
+        return (uint64_t)high << 32 | low;   // (what comes from a lane is an int)
+    };
+    // the next tile that is not masked as a whole, if there is one
+    auto seek = [&]() {
+        if (live == 0) return false;
+        const uint32_t j = __builtin_ctzll(live) & ~1u;
+        in_segment = j / 2;
+        live &= ~(3ull << j);
+        valid0 = __builtin_amdgcn_readlane(piece_valid, j), valid1 = __builtin_amdgcn_readlane(piece_valid, j + 1);
+        k0 = lane_of(piece_k, j), k1 = lane_of(piece_k, j + 1), v0 = lane_of(piece_v, j), v1 = lane_of(piece_v, j + 1);
+        return true;
+    };
+    auto use_pieces = [&](const Pieces& p, const Segment& s) {
+        const uint32_t head = s.item / a.group_tiles;
+        const bool there = p.block < a.blocks;
+        piece_valid = there ? p.valid : 0;
+        live = __ballot(there);
+        piece_k = (uint64_t)(uintptr_t)a.k + head * a.k_head + p.block * a.k_block + p.inside * a.k_token;
+        piece_v = (uint64_t)(uintptr_t)a.v + head * a.v_head + p.block * a.v_block + p.inside * a.v_token;
+        // A masked piece of a tile that is not masked as a whole has the other one's rows, which are there.
+        const uint64_t other_k = __shfl_xor(piece_k, 1), other_v = __shfl_xor(piece_v, 1);
+        piece_k = there ? piece_k : other_k;
+        piece_v = there ? piece_v : other_v;
+    };
+    uint8_t* const lds = shared.rows[wave];
+    auto ask = [&]() {
+        rows.ask_piece(a, lds, 0, k0, v0);
+        rows.ask_piece(a, lds, 1, k1, v1);
+    };
+    auto load_query = [&](const Segment& s) {
+        const uint32_t head0 = s.item % a.group_tiles * 16, first = s.item / a.group_tiles * a.group + head0;
+        const bool there = i < a.group - head0;
+        walk.load_q(a, a.q + s.request * a.q_request + (first + (there ? i : 0)) * a.q_head, there, g);
+    };
+
+    uint32_t at = from;
+    Segment now = segment_at(at, request, before);
+    use_pieces(find_pieces(a, now, wave, lane), now);
+    bool some_left = seek();
+    walk.clear();
+    load_query(now);
+    if (some_left) ask();
+    while (true) {
+        at += now.tile_to - now.tile;
+        const bool more = at < to;
+        Segment next = now;
+        Pieces next_pieces{~0u, 0u, 0u};
+        if (more) {         // where the next segment's pieces lie is asked for while this one is walked over
+            next = segment_at(at, now.request, now.before);
+            next_pieces = find_pieces(a, next, wave, lane);
         }
-        const uint32_t len = clamped_len(a, a.lens[request]);
-        const uint32_t item = (at - before) / tiles;
-        const uint32_t item_from = before + item * tiles, item_to = item_from + tiles;
-        const uint32_t head = item / a.group_tiles, head0 = item % a.group_tiles * 16;  // kv head; first of its group
+        const uint32_t head0 = now.item % a.group_tiles * 16, first_head = now.item / a.group_tiles * a.group + head0;
         const uint32_t heads = a.group - head0 < 16 ? a.group - head0 : 16;
-        const uint32_t first_head = head * a.group + head0;
-        uint32_t tile = at - item_from;
-        const uint32_t tile_to = (to < item_to ? to : item_to) - item_from;
-        const int32_t* row = a.tables + request * a.table_row;
-        const int32_t* picked =
-            a.selected == nullptr ? nullptr : a.selected + ((size_t)request * a.kv_heads + head) * a.keep;
-        const uint8_t *k0 = a.k + head * a.k_head, *v0 = a.v + head * a.v_head;
-
-        walk.begin(a, a.q + request * a.q_request + (first_head + (i < heads ? i : 0)) * a.q_head, i < heads, g);
-
-        Pieces pieces;
-        uint32_t b0, b1, in0, in1;   // of the tile in hand
-        auto take = [&](uint32_t j) {
-            b0 = __builtin_amdgcn_readlane(pieces.block, 2 * j), b1 = __builtin_amdgcn_readlane(pieces.block, 2 * j + 1);
-            in0 = __builtin_amdgcn_readlane(pieces.inside, 2 * j), in1 = __builtin_amdgcn_readlane(pieces.inside, 2 * j + 1);
-        };
-        // A masked piece of a tile that is not masked as a whole reads the other one's rows, which are there.
-        auto load_keys = [&](uint32_t x0, uint32_t x1, uint32_t n0, uint32_t n1) {
-            const bool one0 = x0 != ~0u, one1 = x1 != ~0u;
-            const uint32_t y0 = one0 ? x0 : x1, y1 = one1 ? x1 : x0;
-            const uint32_t o0 = (one0 ? n0 : n1) & 0xFFFF, o1 = (one1 ? n1 : n0) & 0xFFFF;
-            walk.load_k(a, 0, k0 + y0 * a.k_block + (o0 + i) * a.k_token, g);
-            walk.load_k(a, 1, k0 + y1 * a.k_block + (o1 + i) * a.k_token, g);
-        };
-        auto load_values = [&](uint32_t x0, uint32_t x1, uint32_t n0, uint32_t n1) {
-            const bool one0 = x0 != ~0u, one1 = x1 != ~0u;
-            const uint32_t y0 = one0 ? x0 : x1, y1 = one1 ? x1 : x0;
-            const uint32_t o0 = (one0 ? n0 : n1) & 0xFFFF, o1 = (one1 ? n1 : n0) & 0xFFFF;
-            walk.load_v(a, 0, v0 + y0 * a.v_block + (o0 + 4 * g) * a.v_token, i);
-            walk.load_v(a, 1, v0 + y1 * a.v_block + (o1 + 4 * g) * a.v_token, i);
-        };
-        // the next tile, from `tile` on, that is not masked as a whole; tile_to if none is
-        uint32_t looked = tile;      // pieces holds those of [looked, looked + 32)
-        auto seek = [&]() {
-            while (tile < tile_to) {
-                if (tile == looked) pieces = find_pieces(a, row, picked, len, tile, tile_to, wave, lane);
-                const uint64_t live = __ballot(pieces.block != ~0u);
-                const uint32_t past = tile - looked;      // < 32
-                const uint64_t rest = live >> (2 * past);
-                if (rest != 0) {
-                    const uint32_t skip = __builtin_ctzll(rest) / 2;
-                    tile += skip;
-                    take(past + skip);
-                    return;
-                }
-                looked += 32;
-                tile = looked < tile_to ? looked : tile_to;
+        bool ahead = false, turned = false;    // the next segment's first tile is asked for; its pieces are in use
+        while (some_left) {
+            const uint32_t here0 = valid0, here1 = valid1;
+            const uint32_t piece0 = (now.tile + in_segment) * (kTileTokens / kPiece) + 2 * wave;
+            Held<kDim, kExact> held;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the tile's rows are in LDS
+            held.take(a, lds, g, i);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // ... and have left it
+            // all rows of the next tile are asked for at once, and are under way while this one is worked on
+            some_left = seek();
+            if (!some_left && more) {
+                turned = true;
+                use_pieces(next_pieces, next);
+                ahead = seek();
             }
-        };
-        seek();
-        if (tile < tile_to) {
-            load_keys(b0, b1, in0, in1);
-            load_values(b0, b1, in0, in1);
-        }
-        while (tile < tile_to) {
-            const uint32_t valid0 = b0 == ~0u ? 0 : in0 >> 16, valid1 = b1 == ~0u ? 0 : in1 >> 16;
-            const uint32_t this_tile = tile;
+            if (some_left || ahead) ask();
             float s[8];
-            walk.scores(s, a.scale, valid0, valid1, g);
-            if (++tile == looked + 32) looked += 32;
-            seek();
-            if (tile < tile_to) load_keys(b0, b1, in0, in1);   // under way while the weights are made
+            walk.scores(s, held, a.scale, here0, here1, g);
             walk.weigh(s);
             if (a.piece_lse != nullptr) {
                 const float w0 = over_rows_sum((s[0] + s[1]) + (s[2] + s[3]));
                 const float w1 = over_rows_sum((s[4] + s[5]) + (s[6] + s[7]));
                 if (g == 0 && i < heads) {
                     const uint32_t per_row = a.row_blocks * (a.block_tokens / kPiece);
-                    float* to_row = a.piece_lse + ((size_t)request * a.kv_heads * a.group + first_head + i) * per_row +
-                                    this_tile * (kTileTokens / kPiece) + 2 * wave;
+                    float* to_row = a.piece_lse + ((size_t)now.request * a.kv_heads * a.group + first_head + i) * per_row + piece0;
                     // (a row's last tile may be cut by its end)
-                    if (valid0 != 0) to_row[0] = walk.top + __builtin_amdgcn_logf(w0);
-                    if (valid1 != 0) to_row[1] = walk.top + __builtin_amdgcn_logf(w1);
+                    if (here0 != 0) to_row[0] = walk.top + __builtin_amdgcn_logf(w0);
+                    if (here1 != 0) to_row[1] = walk.top + __builtin_amdgcn_logf(w1);
                 }
             }
-            if (valid0 < kPiece || valid1 < kPiece) {
-                walk.drop_v(0, valid0, g);
-                walk.drop_v(1, valid1, g);
+            if (here0 < kPiece || here1 < kPiece) {
+                held.drop_v(0, here0, g);
+                held.drop_v(1, here1, g);
             }
-            walk.add_v(s);
-            if (tile < tile_to) load_values(b0, b1, in0, in1);
+            walk.add_v(s, held);
+        }
+        if (more && !turned) {
+            use_pieces(next_pieces, next);
+            ahead = seek();
+            if (ahead) ask();
+        }
+        some_left = ahead;
+        const bool same = more && next.request == now.request && next.item == now.item;
+        if (more && !same) load_query(next);   // under way while this item is finished
+        if (same) {
+            now = next;
+            continue;
         }
 
         // The wavefronts' results as one.  A lane holds, of head i, channels kRun (4 g + r) + t.
         walk.total = over_rows_sum(walk.total);
-        __syncthreads();
-        if (i < heads) {
-#pragma unroll
-            for (uint32_t p = 0; p < W::kParts; ++p)
-#pragma unroll
-                for (uint32_t r = 0; r < 4; ++r)
-#pragma unroll
-                    for (uint32_t t = 0; t < W::kRun; t += 4)
-                        *(float4*)&shared.sum[wave][i][128 * p + W::kRun * (4 * g + r) + t] =
-                            make_float4(walk.sum[p][t][r], walk.sum[p][t + 1][r], walk.sum[p][t + 2][r], walk.sum[p][t + 3][r]);
-            if (g == 0) {
-                shared.top[wave][i] = walk.top;
-                shared.total[wave][i] = walk.total;
-            }
+        if (g == 0 && i < heads) {
+            shared.top[wave][i] = walk.top;
+            shared.total[wave][i] = walk.total;
         }
-        __syncthreads();
 
         auto finish = [&](uint32_t h, uint32_t d, float4 x, float top, float total) {
             const float by = total == 0.f ? 0.f : 1.f / total;   // (a NaN stays one)
@@ -393,47 +503,65 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                                         (typename H::one)(x.z * by), (typename H::one)(x.w * by)};
                 uint2 words;
                 __builtin_memcpy(&words, y, 8);
-                *(uint2*)(a.out + request * a.out_request + out_head * a.out_head + 2 * d) = words;
+                *(uint2*)(a.out + now.request * a.out_request + out_head * a.out_head + 2 * d) = words;
             }
             if (d == 0) {
                 const float of_head = total == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(total);
-                const size_t n = (size_t)request * a.kv_heads * a.group + out_head;
+                const size_t n = (size_t)now.request * a.kv_heads * a.group + out_head;
                 if (a.lse != nullptr) a.lse[n] = of_head * 0.693147180559945f;
                 if (a.piece_lse != nullptr) a.head_lse[n] = of_head;
             }
         };
 
+        const uint32_t item_from = now.before + now.item * now.tiles, item_to = item_from + now.tiles;
         const uint32_t first_part = owner_of(item_from), parts = owner_of(item_to - 1) - first_part + 1;
         constexpr uint32_t kQuads = kDim / 4;
-        const size_t part_floats = 16 * kDim + 32;
-        auto slot_of = [&](uint32_t w) {   // a workgroup's first item, or its last
+        const uint32_t rows_kept = a.group < 16 ? a.group : 16;
+        const size_t part_floats = (size_t)rows_kept * (kDim + 2);   // sums, then tops and totals
+        auto slot_of = [&](uint32_t w) {   // for a workgroup's first item, or for its last
             return a.partials + (2 * (size_t)w + (item_from > start_of(w) ? 1 : 0)) * part_floats;
         };
-        for (uint32_t x = threadIdx.x; x < heads * kQuads; x += kThreads) {
-            const uint32_t h = x / kQuads, d = x % kQuads * 4;
-            float top = shared.top[0][h];
+        float* slot = slot_of(blockIdx.x);
+        for (uint32_t h0 = 0; h0 < heads; h0 += kMergedHeads) {
+            const uint32_t these = heads - h0 < kMergedHeads ? heads - h0 : kMergedHeads;
+            __syncthreads();
+            if (i - h0 < these) {
 #pragma unroll
-            for (uint32_t w = 1; w < kWaves; ++w) top = fmaxf(top, shared.top[w][h]);
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            float total = 0.f;
+                for (uint32_t p = 0; p < W::kParts; ++p)
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; ++w) {
-                const float by = exp2_from(shared.top[w][h], top);
-                const float4 y = *(const float4*)&shared.sum[w][h][d];
-                total += shared.total[w][h] * by;
-                sum.x += y.x * by, sum.y += y.y * by, sum.z += y.z * by, sum.w += y.w * by;
+                    for (uint32_t r = 0; r < 4; ++r)
+#pragma unroll
+                        for (uint32_t t = 0; t < W::kRun; t += 4)
+                            *(float4*)&shared.sum[wave][i - h0][128 * p + W::kRun * (4 * g + r) + t] = make_float4(
+                                walk.sum[p][t][r], walk.sum[p][t + 1][r], walk.sum[p][t + 2][r], walk.sum[p][t + 3][r]);
             }
-            if (parts == 1) {
-                finish(h, d, sum, top, total);
-            } else {
-                float* slot = slot_of(blockIdx.x);
-                uint64_t* to_sum = (uint64_t*)(slot + h * kDim + d);
-                put_shared(to_sum, __builtin_bit_cast(uint64_t, make_float2(sum.x, sum.y)));
-                put_shared(to_sum + 1, __builtin_bit_cast(uint64_t, make_float2(sum.z, sum.w)));
-                if (d == 0) put_shared((uint64_t*)(slot + 16 * kDim) + h, __builtin_bit_cast(uint64_t, make_float2(top, total)));
+            __syncthreads();
+            for (uint32_t x = threadIdx.x; x < these * kQuads; x += kThreads) {
+                const uint32_t h = x / kQuads, d = x % kQuads * 4;
+                float top = shared.top[0][h0 + h];
+#pragma unroll
+                for (uint32_t w = 1; w < kWaves; ++w) top = fmaxf(top, shared.top[w][h0 + h]);
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                float total = 0.f;
+#pragma unroll
+                for (uint32_t w = 0; w < kWaves; ++w) {
+                    const float by = exp2_from(shared.top[w][h0 + h], top);
+                    const float4 y = *(const float4*)&shared.sum[w][h][d];
+                    total += shared.total[w][h0 + h] * by;
+                    sum.x += y.x * by, sum.y += y.y * by, sum.z += y.z * by, sum.w += y.w * by;
+                }
+                if (parts == 1) {
+                    finish(h0 + h, d, sum, top, total);
+                } else {
+                    uint64_t* to_sum = (uint64_t*)(slot + (h0 + h) * kDim + d);
+                    put_shared(to_sum, __builtin_bit_cast(uint64_t, make_float2(sum.x, sum.y)));
+                    put_shared(to_sum + 1, __builtin_bit_cast(uint64_t, make_float2(sum.z, sum.w)));
+                    if (d == 0)
+                        put_shared((uint64_t*)(slot + rows_kept * kDim) + h0 + h, __builtin_bit_cast(uint64_t, make_float2(top, total)));
+                }
             }
         }
-        if (parts > 1 && last_to_arrive(a.counters + request * per_request + item, parts, &shared.last)) {
+        if (parts > 1 && last_to_arrive(a.counters + now.request * per_request + now.item, parts, &shared.last)) {
             // the parts' results as one, 64 parts at a step
             constexpr uint32_t kMine = (16 * kQuads + kThreads - 1) / kThreads;
             float4 sum[kMine];
@@ -446,9 +574,9 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                 for (uint32_t x = threadIdx.x; x < some * heads; x += kThreads) {
                     const uint32_t p = x / heads, h = x - p * heads;
                     const float2 y = __builtin_bit_cast(
-                        float2, get_shared((const uint64_t*)(slot_of(first_part + p0 + p) + 16 * kDim) + h));
-                    shared.part_top[p][h] = y.x;
-                    shared.part_total[p][h] = y.y;
+                        float2, get_shared((const uint64_t*)(slot_of(first_part + p0 + p) + rows_kept * kDim) + h));
+                    shared.part.top[p][h] = y.x;
+                    shared.part.total[p][h] = y.y;
                 }
                 __syncthreads();
 #pragma unroll
@@ -457,7 +585,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                     if (x >= heads * kQuads) break;
                     const uint32_t h = x / kQuads, d = x % kQuads * 4;
                     float now = top[n];
-                    for (uint32_t p = 0; p < some; ++p) now = fmaxf(now, shared.part_top[p][h]);
+                    for (uint32_t p = 0; p < some; ++p) now = fmaxf(now, shared.part.top[p][h]);
                     const float keep = exp2_from(top[n], now);
                     top[n] = now;
                     total[n] *= keep;
@@ -467,8 +595,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                         const uint64_t* at_sum = (const uint64_t*)(slot_of(first_part + p0 + p) + h * kDim + d);
                         const float2 y = __builtin_bit_cast(float2, get_shared(at_sum));
                         const float2 z = __builtin_bit_cast(float2, get_shared(at_sum + 1));
-                        const float by = exp2_from(shared.part_top[p][h], now);
-                        total[n] += shared.part_total[p][h] * by;
+                        const float by = exp2_from(shared.part.top[p][h], now);
+                        total[n] += shared.part.total[p][h] * by;
                         sum[n].x += y.x * by, sum[n].y += y.y * by, sum[n].z += z.x * by, sum[n].w += z.y * by;
                     }
                 }
@@ -479,7 +607,10 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                 if (x < heads * kQuads) finish(x / kQuads, x % kQuads * 4, sum[n], top[n], total[n]);
             }
         }
-        at = item_from + tile_to;
+        if (!more) return;
+        __syncthreads();   // (what is in LDS of this item has been read)
+        walk.clear();
+        now = next;
     }
 }
 
@@ -489,7 +620,7 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(AttendArgs a, const f
     __shared__ float quarter[kWaves][64];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, request = blockIdx.y;
     const uint32_t j = blockIdx.x * 64 + lane, heads = a.kv_heads * a.group, per_block = a.block_tokens / kPiece;
-    const uint32_t len = clamped_len(a, a.lens[request]);
+    const uint32_t len = clamped_len(a, len_of(a, request));
     float sum = 0.f;
     if (j < a.row_blocks && (uint64_t)j * a.block_tokens < len && (uint32_t)a.tables[request * a.table_row + j] < a.blocks) {
         const uint32_t tokens = len - j * a.block_tokens < a.block_tokens ? len - j * a.block_tokens : a.block_tokens;
@@ -549,6 +680,9 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     if (const int rc = check_sizes(args->requests, args->heads, cache->kv_heads, cache->head_dim, cache->block_tokens,
                                    args->selected != nullptr && args->keep > args->row_blocks ? args->keep : args->row_blocks))
         return rc;
+    // (lanes' places within sixteen rows are counted in 32 bits)
+    if (cache->k_token < 0 || cache->k_token > kMostTokenStride || cache->v_token < 0 || cache->v_token > kMostTokenStride)
+        return PGCM_ERR_ARG;
     if (!aligned(args->q, args->q_request, args->q_head) || !aligned(args->out, args->out_request, args->out_head))
         return PGCM_ERR_ALIGN;
     const hipStream_t stream = (hipStream_t)hip_stream;
@@ -564,7 +698,7 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     a.counters = (uint32_t*)kv->counters.at;
     uint8_t* at = kv->scratch.at;
     a.partials = (float*)at;
-    at += whole_lines(4 * partial_floats(cache->head_dim) * 2 * kAttendGroups);
+    at += whole_lines(4 * partial_floats(cache->head_dim, args->heads / cache->kv_heads) * 2 * kAttendGroups);
     a.head_lse = (float*)at;
     at += whole_lines(4 * (size_t)args->requests * args->heads);
     a.piece_lse = weigh ? (float*)at : nullptr;
@@ -582,8 +716,9 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     // no more workgroups than the longest lengths could use
     const uint64_t walk_blocks = args->selected != nullptr ? args->keep : args->row_blocks;
     const uint64_t tiles = (walk_blocks * cache->block_tokens + kTileTokens - 1) / kTileTokens;
-    const uint64_t most = (tiles * a.requests * a.kv_heads * a.group_tiles + kMinTiles - 1) / kMinTiles;
-    const uint32_t groups = most > kAttendGroups ? kAttendGroups : most > 1 ? (uint32_t)most : 1;
+    const uint64_t items = (uint64_t)a.requests * a.kv_heads * a.group_tiles, most = tiles * items;
+    const uint64_t useful = most > items ? most : items;
+    const uint32_t groups = useful > kAttendGroups ? kAttendGroups : (uint32_t)useful;
     if (cache->half == PGCM_KV_F16) launch<F16>(a, groups, stream);
     else launch<Bf16>(a, groups, stream);
     if (hip_noted(hipGetLastError())) return PGCM_ERR_HIP;

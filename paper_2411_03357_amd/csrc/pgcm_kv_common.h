@@ -77,15 +77,16 @@ struct Room {
 };
 inline size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Attention: a counter for each request and group of up to sixteen query heads of one kv head; two partial results
-// for each workgroup; and, for weights, log-sums of heads and of each piece of a row.
+// Attention: a counter for each request and group of up to sixteen query heads of one kv head; two partial results for
+// each workgroup; and, for weights, log-sums of heads and of each piece of a row.
 constexpr uint32_t kAttendGroups = 512;  // workgroups of a launch, at most
-inline size_t partial_floats(uint32_t head_dim) { return 16 * (size_t)(head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 32; }
+inline size_t partial_floats(uint32_t head_dim, uint32_t group) {
+    return (size_t)(group < 16 ? group : 16) * ((head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 2);
+}
 inline Room attend_room(uint32_t requests, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint64_t row_pieces) {
-    const size_t groups = kv_heads * (size_t)((heads / kv_heads + kPiece - 1) / kPiece);
-    return Room{4 * groups * requests, whole_lines(4 * partial_floats(head_dim) * 2 * kAttendGroups) +
-                                           whole_lines(4 * (size_t)requests * heads) +
-                                           4 * (size_t)requests * heads * row_pieces};
+    const size_t group = heads / kv_heads, items = kv_heads * ((group + kPiece - 1) / kPiece) * requests;
+    return Room{4 * items, whole_lines(4 * partial_floats(head_dim, group) * 2 * kAttendGroups) +
+                               whole_lines(4 * (size_t)requests * heads) + 4 * (size_t)requests * heads * row_pieces};
 }
 
 // Selection: a key for each block of a request and kv head.
@@ -105,12 +106,33 @@ struct F16 {
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
+    // x as the sum of two halves, the first towards zero
+    static __device__ __forceinline__ void split(const float (&x)[8], eight& high, eight& low) {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; e += 2) {
+            const auto h = __builtin_amdgcn_cvt_pkrtz(x[e], x[e + 1]);
+            high[e] = (one)h[0], high[e + 1] = (one)h[1];
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) low[e] = (one)(x[e] - (float)high[e]);
+    }
 };
 struct Bf16 {
     typedef __bf16 one;
     typedef bf16x8 eight;
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ void split(const float (&x)[8], eight& high, eight& low) {
+        uint32_t words[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 8; e += 2) {   // (the upper half of a float is its bfloat16 towards zero)
+            const uint32_t a = __builtin_bit_cast(uint32_t, x[e]), b = __builtin_bit_cast(uint32_t, x[e + 1]);
+            words[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            low[e] = (one)(x[e] - __builtin_bit_cast(float, a & 0xFFFF0000u));
+            low[e + 1] = (one)(x[e + 1] - __builtin_bit_cast(float, b & 0xFFFF0000u));
+        }
+        high = __builtin_bit_cast(eight, words);
     }
 };
 

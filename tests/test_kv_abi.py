@@ -96,6 +96,9 @@ def test_attend_refuses():
                 dict(row_blocks=1 << 28), dict(selected=AT, keep=2, weights=AT), dict(kept=AT),
                 dict(requests=60000, row_blocks=1 << 26)):
         assert lib.pgcm_kv_attend(some, at, C.byref(_attend(**bad)), None) == ARG, bad
+    for bad in (dict(k_token=-128), dict(k_token=1 << 26), dict(v_token=-128), dict(v_token=1 << 26)):
+        cache = _cache(**bad)
+        assert lib.pgcm_kv_attend(some, C.byref(cache), C.byref(_attend()), None) == ARG, bad
     for bad in (dict(q=AT + 4), dict(q_request=4), dict(q_head=1), dict(out=AT + 8), dict(out_request=2), dict(out_head=12)):
         assert lib.pgcm_kv_attend(some, at, C.byref(_attend(**bad)), None) == ALIGN, bad
     assert lib.pgcm_kv_attend(some, at, C.byref(_attend(requests=0, q=None)), None) == 0
