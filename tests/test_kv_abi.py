@@ -97,8 +97,8 @@ def test_attend_refuses():
                 dict(requests=60000, row_blocks=1 << 26)):
         assert lib.pgcm_kv_attend(some, at, C.byref(_attend(**bad)), None) == ARG, bad
     for bad in (dict(k_token=-128), dict(k_token=1 << 26), dict(v_token=-128), dict(v_token=1 << 26)):
-        cache = _cache(**bad)
-        assert lib.pgcm_kv_attend(some, C.byref(cache), C.byref(_attend()), None) == ARG, bad
+        other = _cache(**bad)
+        assert lib.pgcm_kv_attend(some, C.byref(other), C.byref(_attend()), None) == ARG, bad
     for bad in (dict(q=AT + 4), dict(q_request=4), dict(q_head=1), dict(out=AT + 8), dict(out_request=2), dict(out_head=12)):
         assert lib.pgcm_kv_attend(some, at, C.byref(_attend(**bad)), None) == ALIGN, bad
     assert lib.pgcm_kv_attend(some, at, C.byref(_attend(requests=0, q=None)), None) == 0
