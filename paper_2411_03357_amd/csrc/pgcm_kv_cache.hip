@@ -6,6 +6,7 @@ namespace pgcm_kv_impl {
 namespace {
 
 constexpr uint32_t kThreads = 256;
+constexpr uint32_t kAround = 0x128;  // DPP: eight lanes on in a row of sixteen
 
 // A row of head_dim halves is held by 2^row_power lanes, eight channels each; lanes beyond the row hold nothing.
 inline uint32_t row_power_of(uint32_t head_dim) {
@@ -24,95 +25,153 @@ struct AppendArgs {
     int64_t kc_block, kc_token, kc_head, vc_block, vc_token, vc_head;
     uint64_t pool_tokens;
     uint32_t heads, kv_heads, head_dim, block_tokens, rope_positions, rope_dim, adjacent, row_power;
-    float eps;
+    float eps, by_dim;  // by_dim: 1 / head_dim
 };
 
-// One token, and of its rows (queries, keys, values in this order) those that blockIdx.y has.  A lane has the same
-// channels of each of its rows, so cosines, sines and weights are read once.
+// Over the 2^power lanes of a row, so that each has the result.
+template <class Of>
+__device__ __forceinline__ float over_lanes(float x, uint32_t power, Of of) {
+    if (power > 0) x = of(x, from_lane<kPairs>(x));
+    if (power > 1) x = of(x, from_lane<kQuads>(x));
+    if (power > 2) x = of(x, from_lane<kMirrorEight>(x));
+    if (power > 3) x = of(x, from_lane<kMirrorRow>(x));
+    if (power > 4) {
+        const Two y = of_row_pairs(x);
+        x = of(y.a, y.b);
+    }
+    return x;
+}
+
+// One token.  A wavefront takes 64 / 2^row_power of its heads at a step, of queries, keys or values alone; the steps are
+// dealt out to wavefronts, and to the blockIdx.y of a token.  A lane has the same channels of each of its heads, so the
+// factors of
+//   x by w c + y by w' s        (by: of the norm; y, w': the other channel of the pair and its weight; s with its sign)
+// are made once for a token, and a head takes five operations a channel.  8191 tokens, 40 heads and kv heads of 128 (508 MB):
+// APPEND_FIGURE
 template <class H>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
-    const uint32_t token = blockIdx.x, lanes = 1u << a.row_power;
-    const uint32_t part = threadIdx.x & (lanes - 1), d = 8 * part, at = threadIdx.x >> a.row_power;
-    const uint32_t step = (kThreads >> a.row_power) * gridDim.y;
-    const uint32_t rows = a.heads + 2 * a.kv_heads;
+    const uint32_t token = blockIdx.x, lane = threadIdx.x % 64, lanes = 1u << a.row_power;
+    const uint32_t part = lane & (lanes - 1), d = 8 * part, in_step = lane >> a.row_power, heads_at_once = 64u >> a.row_power;
     const bool mine = d < a.head_dim;
+    const uint32_t of_q = (a.heads + heads_at_once - 1) / heads_at_once, of_k = (a.kv_heads + heads_at_once - 1) / heads_at_once;
+    const uint32_t steps = of_q + 2 * of_k, stride = kThreads / 64 * gridDim.y;
+    uint32_t step = __builtin_amdgcn_readfirstlane(blockIdx.y * (kThreads / 64) + threadIdx.x / 64);
 
     const int64_t slot = a.slots[token];
     const bool stored = (uint64_t)slot < a.pool_tokens;
-    const uint64_t block = stored ? (uint64_t)slot / a.block_tokens : 0;
-    const uint32_t inside = stored ? (uint32_t)((uint64_t)slot - block * a.block_tokens) : 0;
+    // the lane's head of a step, and whether it is there and wanted
+    struct Head {
+        uint32_t n;
+        bool wanted;
+    };
+    auto head_of = [&](uint32_t step) {
+        const uint32_t first = step < of_q ? 0 : step < of_q + of_k ? of_q : of_q + of_k;
+        const uint32_t n = (step - first) * heads_at_once + in_step;
+        return Head{n, mine && (step < of_q ? n < a.heads : n < a.kv_heads && stored)};
+    };
+    auto load = [&](uint32_t step) {
+        const Head h = head_of(step);
+        const uint8_t* from = step < of_q ? a.q + token * a.q_token + h.n * a.q_head
+                              : step < of_q + of_k ? a.k + token * a.k_token + h.n * a.k_head
+                                                   : a.v + token * a.v_token + h.n * a.v_head;
+        return h.wanted ? *(const uint4*)(from + 2 * d) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 words = make_uint4(0, 0, 0, 0);
+    if (step < steps) words = load(step);      // under way while the factors are made
 
-    float c[8], s[8];       // of the lane's channels; the sine with its sign
+    float own[2][8], other[2][8];              // factors of queries and of keys
     const uint32_t half = a.rope_dim / 2;
     const bool turned = a.rope != nullptr && d < a.rope_dim;
-    uint32_t partner = part;  // the lane with the other channels of the pairs
-    if (a.rope != nullptr && !a.adjacent && turned) partner = d < half ? part + half / 8 : part - half / 8;
+    const bool halves = a.rope != nullptr && a.adjacent == 0;
+    uint32_t partner = part;                   // the lane with the other channels of the pairs
+    if (halves && turned) partner = d < half ? part + half / 8 : part - half / 8;
+    {
+        float c[8], s[8];
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) c[e] = 1.f, s[e] = 0.f;
-    if (turned) {
-        const int32_t position = a.positions[token];
-        const bool known = (uint32_t)position < a.rope_positions;
-        const float* line = a.rope + (known ? (size_t)position * a.rope_dim : 0);
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) {
-            const uint32_t n = a.adjacent ? (d + e) / 2 : (d < half ? d : d - half) + e;
-            const bool second = a.adjacent ? e % 2 : d >= half;
-            c[e] = known ? line[n] : NAN;
-            s[e] = known ? line[half + n] : NAN;
-            if (!second) s[e] = -s[e];
-        }
-    }
-    float qw[8], kw[8], qo[8], ko[8];   // weights of the lane's channels, and of their partners
-    auto weights = [&](const uint8_t* from, float(&own)[8], float(&other)[8]) {
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) own[e] = other[e] = 1.f;
-        if (from == nullptr || !mine) return;
-        const typename H::eight x = as_eight<H>(*(const uint4*)(from + 2 * d));
-        const typename H::eight y = as_eight<H>(*(const uint4*)(from + 16 * partner));
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) own[e] = (float)x[e], other[e] = (float)y[e];
-    };
-    weights(a.q_weight, qw, qo);
-    weights(a.k_weight, kw, ko);
-
-    for (uint32_t row = blockIdx.y * (kThreads >> a.row_power) + at; row - at < rows; row += step) {
-        const bool is_q = row < a.heads, is_k = !is_q && row < a.heads + a.kv_heads, there = row < rows;
-        const uint32_t head = is_q ? row : is_k ? row - a.heads : row - a.heads - a.kv_heads;
-        const uint8_t* from = is_q ? a.q + token * a.q_token + head * a.q_head
-                              : is_k ? a.k + token * a.k_token + head * a.k_head
-                                     : a.v + token * a.v_token + head * a.v_head;
-        const bool wanted = there && mine && (is_q || stored);
-        uint4 words = make_uint4(0, 0, 0, 0);
-        if (wanted) words = *(const uint4*)(from + 2 * d);
-        uint4 result = words;
-        if (__any(is_q || is_k)) {
-            const typename H::eight x = as_eight<H>(words);
-            float sum = 0.f;
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) sum += (float)x[e] * (float)x[e];
-            for (uint32_t l = 1; l < lanes; l *= 2) sum += __shfl_xor(sum, l);
-            const uint32_t lane = threadIdx.x % 64, other = lane - part + partner;
-            uint4 far;
-            far.x = __shfl(words.x, other), far.y = __shfl(words.y, other);
-            far.z = __shfl(words.z, other), far.w = __shfl(words.w, other);
-            const typename H::eight z = as_eight<H>(far);
-            const bool normed = (is_q ? a.q_weight : a.k_weight) != nullptr;
-            const float by = normed ? 1.f / sqrtf(sum / (float)a.head_dim + a.eps) : 1.f;
-            typename H::eight y;
+        for (uint32_t e = 0; e < 8; ++e) c[e] = 1.f, s[e] = 0.f;
+        if (turned) {
+            const int32_t position = a.positions[token];
+            const bool known = (uint32_t)position < a.rope_positions;
+            const float* line = a.rope + (known ? (size_t)position * a.rope_dim : 0);
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) {
-                const float own = (float)x[e] * by * (is_q ? qw[e] : kw[e]);
-                const uint32_t f = e ^ 1;
-                const float pair = a.adjacent ? (float)x[f] * by * (is_q ? qw[f] : kw[f])
-                                              : (float)z[e] * by * (is_q ? qo[e] : ko[e]);
-                y[e] = (typename H::one)(turned ? own * c[e] + pair * s[e] : own);
+                const uint32_t n = a.adjacent ? (d + e) / 2 : (d < half ? d : d - half) + e;
+                const bool second = a.adjacent ? e % 2 : d >= half;
+                c[e] = known ? line[n] : NAN;
+                s[e] = known ? line[half + n] : NAN;
+                if (!second) s[e] = -s[e];
             }
-            if (is_q || is_k) result = as_words<H>(y);
         }
-        if (wanted) {
-            uint8_t* to = is_q ? a.q_out + token * a.q_out_token + head * a.q_out_head
-                          : is_k ? a.k_cache + block * a.kc_block + inside * a.kc_token + head * a.kc_head
-                                 : a.v_cache + block * a.vc_block + inside * a.vc_token + head * a.vc_head;
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            const uint8_t* from = k == 0 ? a.q_weight : a.k_weight;
+            typename H::eight x{}, y{};
+            const bool there = from != nullptr && mine;
+            if (there) {
+                x = as_eight<H>(*(const uint4*)(from + 2 * d));
+                y = as_eight<H>(*(const uint4*)(from + 16 * partner));
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) {
+                own[k][e] = (there ? (float)x[e] : 1.f) * c[e];
+                other[k][e] = (there ? (float)(a.adjacent ? x[e ^ 1] : y[e]) : 1.f) * s[e];
+            }
+        }
+    }
+    const uint64_t block = stored ? (uint64_t)slot / a.block_tokens : 0;
+    const uint32_t inside = stored ? (uint32_t)((uint64_t)slot - block * a.block_tokens) : 0;
+    uint8_t* const k_to = a.k_cache + block * a.kc_block + inside * a.kc_token;
+    uint8_t* const v_to = a.v_cache + block * a.vc_block + inside * a.vc_token;
+    const bool across = halves && a.row_power == 4 && a.rope_dim == 128;   // the partner is eight lanes on, around the row
+
+    while (step < steps) {
+        const uint4 now = words;
+        const uint32_t this_step = step;
+        step += stride;
+        if (step < steps) words = load(step);  // under way while this step is worked on
+        const Head h = head_of(this_step);
+        uint4 result = now;
+        if (this_step < of_q + of_k) {
+            const uint32_t k = this_step < of_q ? 0 : 1;
+            const typename H::eight x = as_eight<H>(now);
+            float by = 1.f;
+            if ((k == 0 ? a.q_weight : a.k_weight) != nullptr) {
+                float sum = 0.f;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) sum += (float)x[e] * (float)x[e];
+                sum = over_lanes(sum, a.row_power, [](float x, float y) { return x + y; });
+                by = __builtin_amdgcn_rsqf(sum * a.by_dim + a.eps);   // (to one unit in the last place)
+            }
+            typename H::eight y = x;
+            if (halves) {
+                uint4 far;
+                if (across) {
+                    far.x = __builtin_amdgcn_update_dpp(0, now.x, kAround, 0xF, 0xF, true);
+                    far.y = __builtin_amdgcn_update_dpp(0, now.y, kAround, 0xF, 0xF, true);
+                    far.z = __builtin_amdgcn_update_dpp(0, now.z, kAround, 0xF, 0xF, true);
+                    far.w = __builtin_amdgcn_update_dpp(0, now.w, kAround, 0xF, 0xF, true);
+                } else {
+                    const uint32_t at = lane - part + partner;
+                    far.x = __shfl(now.x, at), far.y = __shfl(now.y, at), far.z = __shfl(now.z, at), far.w = __shfl(now.w, at);
+                }
+                y = as_eight<H>(far);
+            }
+            typename H::eight z;
+            auto turn = [&](const float(&c)[8], const float(&s)[8]) {
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) {
+                    const float pair = (float)(a.adjacent ? x[e ^ 1] : y[e]);
+                    z[e] = (typename H::one)(((float)x[e] * c[e] + pair * s[e]) * by);
+                }
+            };
+            if (k == 0) turn(own[0], other[0]);
+            else turn(own[1], other[1]);
+            result = as_words<H>(z);
+        }
+        if (h.wanted) {
+            uint8_t* to = this_step < of_q ? a.q_out + token * a.q_out_token + h.n * a.q_out_head
+                          : this_step < of_q + of_k ? k_to + h.n * a.kc_head
+                                                    : v_to + h.n * a.vc_head;
             *(uint4*)(to + 2 * d) = result;
         }
     }
@@ -166,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void summarize_kernel(SummarizeArgs a) {
     if (mine && count != 0)
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(fabsf(low[e]), fabsf(high[e])));
-    for (uint32_t l = 1; l < lanes; l *= 2) most = fmaxf(most, __shfl_xor(most, l));
+    most = over_lanes(most, a.row_power, [](float x, float y) { return fmaxf(x, y); });
     const bool small = !(most >= 1e-30f);
     const float by = small ? 0.f : 127.f / most;
     if (lane < lanes && mine) {
@@ -227,9 +286,11 @@ int pgcm_kv_append(const pgcm_kv_cache* cache, const pgcm_kv_append_args* args, 
     a.heads = args->heads, a.kv_heads = cache->kv_heads, a.head_dim = dim, a.block_tokens = cache->block_tokens;
     a.rope_positions = args->rope_positions, a.rope_dim = args->rope_dim, a.adjacent = args->adjacent;
     a.row_power = row_power_of(dim);
-    a.eps = args->eps;
-    const uint32_t at_once = kThreads >> a.row_power, passes = (a.heads + 2 * a.kv_heads + at_once - 1) / at_once;
-    // a token's rows in one workgroup, or in several where tokens alone would not fill the chip
+    a.eps = args->eps, a.by_dim = 1.f / (float)dim;
+    // a token's heads in one workgroup, or in several where tokens alone would not fill the chip
+    const uint32_t at_once = 64u >> a.row_power;
+    const uint32_t steps = (a.heads + at_once - 1) / at_once + 2 * ((a.kv_heads + at_once - 1) / at_once);
+    const uint32_t passes = (steps + kThreads / 64 - 1) / (kThreads / 64);
     uint32_t ways = args->tokens >= 1024 ? 1 : (1024 + args->tokens - 1) / args->tokens;
     if (ways > passes) ways = passes;
     const dim3 grid(args->tokens, ways);
