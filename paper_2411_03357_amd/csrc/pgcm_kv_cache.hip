@@ -2,6 +2,8 @@
 // element once: what bounds them is memory.
 #include "pgcm_kv_common.h"
 
+#include <type_traits>
+
 namespace pgcm_kv_impl {
 namespace {
 
@@ -186,63 +188,108 @@ struct SummarizeArgs {
     uint32_t n, kv_heads, head_dim, block_tokens, pool, entry_count, row_power;
 };
 
-// A wavefront for each block and head: 64 / 2^row_power tokens at a time.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+// Two halves as whole numbers in their order, and back: an involution.
+__device__ __forceinline__ s16x2 in_order(s16x2 x) { return x ^ ((x >> 15) & (s16x2)(short)0x7FFF); }
+__device__ __forceinline__ s16x2 as_two(uint32_t x) { return __builtin_bit_cast(s16x2, x); }
+__device__ __forceinline__ uint32_t as_word(s16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+// x of the lanes whose number differs in 2^n, n < 6
+__device__ __forceinline__ uint32_t opposite(uint32_t x, uint32_t n) {
+    if (n == 4) {
+        const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return y[0] ^ y[1] ^ x;
+    }
+    if (n == 5) {
+        const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return y[0] ^ y[1] ^ x;
+    }
+    return __shfl_xor(x, 1u << n);
+}
+
+// A wavefront for each block and head: 64 / 2^row_power tokens at a time.  Least and largest values are those of the halves as
+// whole numbers in order, two an instruction; whatever is not finite lies at the ends of that order, and if any is found there
+// the block is gone through again with zeros in such places.  SUMMARIZE_FIGURE
 template <class H>
 __global__ __launch_bounds__(kThreads) void summarize_kernel(SummarizeArgs a) {
-    const uint32_t lane = threadIdx.x % 64;
-    const uint64_t task = (uint64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint64_t task = (uint64_t)blockIdx.x * (kThreads / 64) + wave;
     const uint32_t n = (uint32_t)(task / a.kv_heads), head = (uint32_t)(task - (uint64_t)n * a.kv_heads);
     if (n >= a.n) return;
     const uint32_t block = (uint32_t)a.blocks[n], entry = a.entries == nullptr ? block : (uint32_t)a.entries[n];
     if (block >= a.pool || entry >= a.entry_count) return;
     const int32_t asked = a.counts[n];
     const uint32_t count = asked <= 0 ? 0u : (uint32_t)asked < a.block_tokens ? (uint32_t)asked : a.block_tokens;
-    const uint32_t lanes = 1u << a.row_power, part = lane & (lanes - 1), d = 8 * part;
+    const uint32_t lanes = 1u << a.row_power, part = lane & (lanes - 1), d = 8 * part, at_once = 64u >> a.row_power;
+    const uint32_t in_turn = lane >> a.row_power;
     const bool mine = d < a.head_dim;
-
-    float low[8], high[8];
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) low[e] = INFINITY, high[e] = -INFINITY;
     const uint8_t* from = a.k + block * a.k_block + head * a.k_head + 2 * d;
-    if (mine) {
-#pragma unroll 4
-        for (uint32_t t = lane >> a.row_power; t < count; t += 64 >> a.row_power) {
-            const typename H::eight x = as_eight<H>(*(const uint4*)(from + t * a.k_token));
+
+    s16x2 low[4], high[4];
+    auto walk = [&](auto careful) {
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) {
-                const float y = (float)x[e], z = fabsf(y) < INFINITY ? y : 0.f;
-                low[e] = fminf(low[e], z), high[e] = fmaxf(high[e], z);
+        for (uint32_t w = 0; w < 4; ++w) low[w] = (s16x2)(short)0x7FFF, high[w] = (s16x2)(short)0x8000;
+        if (!mine) return;
+#pragma unroll 4
+        for (uint32_t t = in_turn; t < count; t += at_once) {
+            const uint4 x = *(const uint4*)(from + t * a.k_token);
+            uint32_t words[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (uint32_t w = 0; w < 4; ++w) {
+                if constexpr (decltype(careful)::value) {
+                    constexpr uint32_t kInf = H::kInfinity;
+                    if ((words[w] & kInf) == kInf) words[w] &= 0xFFFF0000u;
+                    if ((words[w] & kInf << 16) == kInf << 16) words[w] &= 0xFFFFu;
+                }
+                const s16x2 k = in_order(as_two(words[w]));
+                low[w] = __builtin_elementwise_min(low[w], k), high[w] = __builtin_elementwise_max(high[w], k);
             }
         }
-    }
-    for (uint32_t l = lanes; l < 64; l *= 2)
+    };
+    walk(std::false_type());
+    if (count != 0) {
+        s16x2 least = low[0], most = high[0];
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) {
-            low[e] = fminf(low[e], __shfl_xor(low[e], l));
-            high[e] = fmaxf(high[e], __shfl_xor(high[e], l));
+        for (uint32_t w = 1; w < 4; ++w)
+            least = __builtin_elementwise_min(least, low[w]), most = __builtin_elementwise_max(most, high[w]);
+        const short end = (short)H::kInfinity;
+        const bool beyond = mine && in_turn < count && ((most.x >= end) | (most.y >= end) | (least.x <= ~end) | (least.y <= ~end));
+        if (__any(beyond)) walk(std::true_type());
+    }
+    for (uint32_t l = a.row_power; l < 6; ++l)
+#pragma unroll
+        for (uint32_t w = 0; w < 4; ++w) {
+            low[w] = __builtin_elementwise_min(low[w], as_two(opposite(as_word(low[w]), l)));
+            high[w] = __builtin_elementwise_max(high[w], as_two(opposite(as_word(high[w]), l)));
         }
-    float most = 0.f;
+    auto value = [](uint32_t word, uint32_t e) {   // of a half
+        const uint16_t bits = (uint16_t)(word >> (16 * e));
+        return (float)__builtin_bit_cast(typename H::one, bits);
+    };
+    uint32_t ends[8];   // the halves themselves
+#pragma unroll
+    for (uint32_t w = 0; w < 4; ++w) ends[w] = as_word(in_order(low[w])), ends[4 + w] = as_word(in_order(high[w]));
+    // |x| is largest at an end; as whole numbers, without the sign, halves are in the order of |x|
+    s16x2 size = (s16x2)(short)0;
     if (mine && count != 0)
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(fabsf(low[e]), fabsf(high[e])));
+        for (uint32_t w = 0; w < 8; ++w) size = __builtin_elementwise_max(size, as_two(ends[w] & 0x7FFF7FFFu));
+    const short larger = size.x > size.y ? size.x : size.y;
+    float most = value((uint32_t)(uint16_t)larger, 0);
     most = over_lanes(most, a.row_power, [](float x, float y) { return fmaxf(x, y); });
     const bool small = !(most >= 1e-30f);
     const float by = small ? 0.f : 127.f / most;
-    if (lane < lanes && mine) {
-        uint32_t words[4];
+    // four numbers a lane at a time: words 0 and 1 of a lane's eight channels are the least values, 2 and 3 the largest
+    for (uint32_t w = in_turn; w < 4; w += at_once) {
+        uint32_t bytes = 0;
+        const uint32_t pair0 = w == 0 ? ends[0] : w == 1 ? ends[2] : w == 2 ? ends[4] : ends[6];
+        const uint32_t pair1 = w == 0 ? ends[1] : w == 1 ? ends[3] : w == 2 ? ends[5] : ends[7];
 #pragma unroll
-        for (uint32_t w = 0; w < 4; ++w) {
-            words[w] = 0;
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-                const float x = w < 2 ? low[4 * w + e] : high[4 * w - 8 + e];
-                const int32_t whole = small ? 0 : (int32_t)rintf(x * by);
-                words[w] |= ((uint32_t)whole & 0xFF) << (8 * e);
-            }
+        for (uint32_t e = 0; e < 4; ++e) {
+            const int32_t whole = small ? 0 : (int32_t)rintf(value(e < 2 ? pair0 : pair1, e % 2) * by);
+            bytes |= ((uint32_t)whole & 0xFF) << (8 * e);
         }
-        int8_t* to = a.bounds + ((uint64_t)entry * a.kv_heads + head) * 2 * a.head_dim + d;
-        *(uint2*)to = make_uint2(words[0], words[1]);
-        *(uint2*)(to + a.head_dim) = make_uint2(words[2], words[3]);
+        if (mine)
+            *(uint32_t*)(a.bounds + ((uint64_t)entry * a.kv_heads + head) * 2 * a.head_dim + (w / 2) * a.head_dim + d + 4 * (w % 2)) = bytes;
     }
     if (lane == 0) a.scales[(uint64_t)entry * a.kv_heads + head] = small ? 0.f : most / 127.f;
 }

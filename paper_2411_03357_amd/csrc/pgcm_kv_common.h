@@ -103,6 +103,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 struct F16 {
     typedef _Float16 one;
     typedef f16x8 eight;
+    static constexpr uint32_t kInfinity = 0x7C00;
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
@@ -120,6 +121,7 @@ struct F16 {
 struct Bf16 {
     typedef __bf16 one;
     typedef bf16x8 eight;
+    static constexpr uint32_t kInfinity = 0x7F80;
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
