@@ -7,7 +7,7 @@ namespace {
 
 constexpr uint32_t kMostThreads = 1024;
 constexpr uint32_t kHeld = 16;        // keys that a lane holds in registers; longer rows are read from memory at each look
-constexpr uint32_t kBins = 2048;
+constexpr uint32_t kBinBits = 10, kBins = 1u << kBinBits;
 constexpr uint32_t kNever = 0, kAlways = 0xFFFFFFFFu;  // keys of what cannot be chosen, and of what is chosen before all others
 
 // Whole numbers in the order of numbers; those of -inf and inf are not kNever and kAlways.
@@ -55,9 +55,9 @@ struct ReadKeys {
 };
 
 struct ChooseShared {
-    uint32_t bins[kBins];
+    __align__(16) uint32_t bins[3][kBins];   // of a look and of the next one; those of the one before may still be read
     uint32_t able[kMostThreads / 64], always[kMostThreads / 64], least[kMostThreads / 64], most[kMostThreads / 64];
-    uint32_t bin, in_bin, need;
+    uint32_t above[kMostThreads / 64], equal[kMostThreads / 64];
 };
 
 // What is chosen: the keys above `above`, and of those equal to `equal` the first `of_equal`; `count` in all.
@@ -66,7 +66,6 @@ struct Chosen {
 };
 
 // The sum of the figures of the wavefronts before this one.
-template <uint32_t kWaves>
 __device__ __forceinline__ uint32_t of_waves_before(const uint32_t* figures) {
     const uint32_t lane = threadIdx.x % 64;
     return over_wave(lane < threadIdx.x / 64 ? figures[lane] : 0u, [](uint32_t a, uint32_t b) { return a + b; });
@@ -89,7 +88,7 @@ __device__ __forceinline__ Chosen choose(const Keys& keys, uint32_t want, Choose
     });
     least = over_wave(least, less);
     most = over_wave(most, more);
-    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) shared.bins[b] = 0;
+    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) shared.bins[0][b] = 0;
     if (lane == 0) shared.able[wave] = able, shared.always[wave] = always, shared.least[wave] = least, shared.most[wave] = most;
     __syncthreads();
     // (a wavefront's figures in a lane each: sixteen wavefronts that read all of them one by one keep LDS busy for 0.5 us)
@@ -102,42 +101,38 @@ __device__ __forceinline__ Chosen choose(const Keys& keys, uint32_t want, Choose
     if (always >= want) return Chosen{kAlways, kAlways, want, want};
 
     // The place of the last one chosen, within [least, most]: counts of equal pieces of that range, from the top, then
-    // the piece that it is in; as a rule one or two looks, at most three.
+    // the piece that it is in; as a rule one or two looks, at most four.  Each wavefront adds up all counts by itself, which
+    // takes less than a barrier.
     uint32_t need = want - always;
-    while (true) {
+    for (uint32_t look = 0;; ++look) {
         const uint32_t width = most - least;
         const uint32_t bits = width == 0 ? 0 : 32 - __builtin_clz(width);
-        const uint32_t shift = bits > 11 ? bits - 11 : 0;
+        const uint32_t shift = bits > kBinBits ? bits - kBinBits : 0;
+        uint32_t* bins = shared.bins[look % 3];
         keys.each([&](uint32_t, uint32_t k, uint32_t) {
-            if (k >= least && k <= most) atomicAdd(&shared.bins[(k - least) >> shift], 1u);
+            if (k >= least && k <= most) atomicAdd(&bins[(k - least) >> shift], 1u);
         });
+        for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) shared.bins[(look + 1) % 3][b] = 0;
         __syncthreads();
-        // bins in threads from the top: kBins / kThreads each
-        constexpr uint32_t kEach = kBins / kThreads;
-        uint32_t mine[kEach], sum = 0;
+        // lane l adds up the l-th of 64 runs of bins from the top
+        constexpr uint32_t kRun = kBins / 64;
+        uint32_t sum = 0;
 #pragma unroll
-        for (uint32_t e = 0; e < kEach; ++e) {
-            mine[e] = shared.bins[kBins - 1 - (threadIdx.x * kEach + e)];
-            sum += mine[e];
+        for (uint32_t e = 0; e < kRun; e += 4) {
+            const uint4 x = *(const uint4*)&bins[(63 - lane) * kRun + (e + 4 * lane) % kRun];   // (in turn, for LDS's banks)
+            sum += (x.x + x.y) + (x.z + x.w);
         }
-        const uint32_t upto = scan(sum);
-        if (lane == 63) shared.able[wave] = upto;
-        __syncthreads();
-        uint32_t before = upto - sum + of_waves_before<kWaves>(shared.able);
-#pragma unroll
-        for (uint32_t e = 0; e < kEach; ++e) {
-            if (before < need && before + mine[e] >= need) {
-                shared.bin = kBins - 1 - (threadIdx.x * kEach + e);
-                shared.in_bin = mine[e];
-                shared.need = need - before;
-            }
-            before += mine[e];
-            shared.bins[kBins - 1 - (threadIdx.x * kEach + e)] = 0;   // for the next look
-        }
-        __syncthreads();
-        const uint32_t bin = shared.bin, in_bin = shared.in_bin;
-        need = shared.need;
-        least += bin << shift;
+        uint32_t upto = scan(sum);
+        const uint32_t run = __builtin_ctzll(__ballot(upto >= need));
+        const uint32_t before_run = __builtin_amdgcn_readlane(upto - sum, run);
+        // ... and the run's bins, one a lane
+        const uint32_t top = (64 - run) * kRun - 1;
+        sum = lane < kRun ? bins[top - lane] : 0;
+        upto = before_run + scan(sum);
+        const uint32_t at = __builtin_ctzll(__ballot(upto >= need));
+        const uint32_t in_bin = __builtin_amdgcn_readlane(sum, at);
+        need -= (uint32_t)__builtin_amdgcn_readlane(upto - sum, at);
+        least += (top - at) << shift;
         if (need == in_bin) return Chosen{least - 1, kNever, 0, want};   // (least is no key of kNever: at least 1)
         if (shift == 0) return Chosen{least, least, need, want};
         most = less(most, least + ((1u << shift) - 1));
@@ -147,7 +142,6 @@ __device__ __forceinline__ Chosen choose(const Keys& keys, uint32_t want, Choose
 // put(i, place, step) for each chosen i, with the places in the order of i.
 template <uint32_t kThreads, class Keys, class Put>
 __device__ __forceinline__ void put_in_order(const Keys& keys, const Chosen& c, ChooseShared& shared, Put put) {
-    constexpr uint32_t kWaves = kThreads / 64;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     uint32_t above = 0, equal = 0;
     keys.each([&](uint32_t, uint32_t k, uint32_t) {
@@ -155,11 +149,10 @@ __device__ __forceinline__ void put_in_order(const Keys& keys, const Chosen& c, 
         equal += __builtin_popcountll(__ballot(k == c.equal && c.of_equal != 0));
     });
     const bool any = (above | equal) != 0;
+    if (lane == 0) shared.above[wave] = above, shared.equal[wave] = equal;
     __syncthreads();
-    if (lane == 0) shared.able[wave] = above, shared.always[wave] = equal;
-    __syncthreads();
-    above = of_waves_before<kWaves>(shared.able), equal = of_waves_before<kWaves>(shared.always);
     if (!any) return;
+    above = of_waves_before(shared.above), equal = of_waves_before(shared.equal);
     const uint64_t before_me = (1ull << lane) - 1;
     keys.each([&](uint32_t i, uint32_t k, uint32_t s) {
         const uint64_t is_above = __ballot(k > c.above), is_equal = __ballot(k == c.equal && c.of_equal != 0);
@@ -279,7 +272,10 @@ __device__ __forceinline__ void choose_list(const SelectArgs& a, uint32_t list, 
 constexpr uint32_t kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
 constexpr uint32_t kWaveBlocks = 64;                          // that a wavefront scores at a time, in four steps
 constexpr uint32_t kPartBlocks = kScoreWaves * kWaveBlocks;   // ... and a workgroup
-constexpr uint32_t kWholeBlocks = 1024;                       // rows of up to so many are scored and chosen from in one launch
+// Rows scored and chosen from in one launch, a workgroup each: of up to kShortBlocks (one request with 8 lists: of 100 blocks
+// 8.4 us, of 500 11.7, in two launches 11.2 and 12.6), and of up to kWholeBlocks where there are lists for all compute units
+// (of 1000 blocks: 32 requests 21.4 us and 22.9, one 16.1 and 13.1).
+constexpr uint32_t kShortBlocks = 512, kWholeBlocks = 1024, kListsToFill = 256;
 
 // Keys of the blocks [from, to) of a request for one kv head, at key_of(j).  The scores are products on the matrix cores,
 // of 2 head_dim whole numbers: for each of sixteen query heads, its negative channels (for the least values) and its
@@ -462,7 +458,7 @@ __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void select_ke
 template <class H, uint32_t kChunks>
 void launch(const SelectArgs& a, hipStream_t stream) {
     const uint32_t lists = a.requests * a.kv_heads;
-    if (a.row_blocks <= kWholeBlocks) {
+    if (a.row_blocks <= kShortBlocks || (a.row_blocks <= kWholeBlocks && lists >= kListsToFill)) {
         select_kernel<H, kChunks><<<lists, kScoreThreads, 0, stream>>>(a);
         return;
     }
@@ -532,7 +528,8 @@ int pgcm_kv_evict(const pgcm_kv_evict_args* args, void* hip_stream) {
     a.table_row = args->table_row, a.table_out_row = args->table_out_row;
     a.row_blocks = args->row_blocks, a.block_tokens = args->block_tokens, a.blocks = args->blocks;
     a.most = args->most, a.first = args->first, a.last = args->last;
-    if (a.row_blocks <= 4 * 256) evict_kernel<256><<<args->requests, 256, 0, (hipStream_t)hip_stream>>>(a);
+    // four wavefronts a row, or sixteen for longer ones (8 rows of 2000 blocks: 7.7 us and 8.2; of 4000 9.3 and 9.1)
+    if (a.row_blocks <= 2048) evict_kernel<256><<<args->requests, 256, 0, (hipStream_t)hip_stream>>>(a);
     else evict_kernel<kMostThreads><<<args->requests, kMostThreads, 0, (hipStream_t)hip_stream>>>(a);
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
