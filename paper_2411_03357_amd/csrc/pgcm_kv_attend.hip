@@ -224,16 +224,15 @@ struct Walk : Layout<kDim> {
             }
         }
     }
-    // Sums are kept relative to a score that is no further than kSlack below the largest one so far, in units of log 2: then
-    // weights are at most 2^kSlack, and the sums need not be brought up to each new maximum.  The scores become weights.
-    static constexpr float kSlack = 8.f;
+    // Sums are kept relative to 2^top, which makes the largest weight so far 2^H::kLargest when they were last brought up to
+    // it, and at most 2^H::kOverflows before the next time: a new maximum rarely takes that.  The scores become weights.
     __device__ __forceinline__ void weigh(float (&s)[8]) {
         float most = s[0];
 #pragma unroll
         for (uint32_t j = 1; j < 8; ++j) most = fmaxf(most, s[j]);
         most = over_rows_max(most);
-        if (__any(most > top + kSlack || (top == -INFINITY && most > top))) {
-            const float now = fmaxf(most, top), keep = exp2_from(top, now);
+        if (__any(most > top + H::kOverflows || (top == -INFINITY && most > top))) {
+            const float now = fmaxf(most - H::kLargest, top), keep = exp2_from(top, now);
             top = now;
             total *= keep;
 #pragma unroll

@@ -104,6 +104,9 @@ struct F16 {
     typedef _Float16 one;
     typedef f16x8 eight;
     static constexpr uint32_t kInfinity = 0x7C00;
+    // Weights of attention, as powers of 2: the largest ones near the end of the range, since the least that a half can tell
+    // apart, 2^-24, is then 2^-37 of them; beside a weight of 1, 2^-21 would keep three bits.
+    static constexpr float kLargest = 13.f, kOverflows = 15.f;
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
@@ -122,6 +125,7 @@ struct Bf16 {
     typedef __bf16 one;
     typedef bf16x8 eight;
     static constexpr uint32_t kInfinity = 0x7F80;
+    static constexpr float kLargest = 0.f, kOverflows = 8.f;   // (the range is that of a float)
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }

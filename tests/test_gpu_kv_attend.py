@@ -140,6 +140,24 @@ def test_large_scores_and_scales():
         _check(r, q, scale=scale)
 
 
+@pytest.mark.parametrize("half", [F16, BF16])
+def test_small_weights_beside_a_large_one(half):
+    """a first token that has nearly all of the weight and no value, and many whose weights are 2^-20.6 of its: what is left
+    of these in halves must be as exact as the output.  Three hundred requests that share their blocks, so that a wavefront
+    takes many tokens of one."""
+    r = ref.Requests(15, [2048], 1, 64, half)
+    r.v = r.v.abs()
+    r.k[:, :, :, 0] = -14.296875
+    r.k[int(r.tables[0, 0]), 0], r.v[int(r.tables[0, 0]), 0] = 0, 0
+    q = torch.zeros(1, 2, 64, dtype=half)
+    q[:, :, 0] = 1
+    want = ref.attend(r, q, 1.0)
+    r.tables, r.lens = np.repeat(r.tables, 300, 0), r.lens * 300
+    out, lse, _ = _run(r, q.expand(300, 2, 64).contiguous(), scale=1.0)
+    ref.within(out, [x.expand(300, 2, 64) for x in want[0]], "out")
+    ref.within(lse, [x.expand(300, 2) for x in want[1]], "lse")
+
+
 def test_nan_of_a_request_stays_its_own():
     r = ref.Requests(14, [40, 40], 1, 64, BF16)
     q = ref.numbers(14, 2, 2, 64).to(BF16)
