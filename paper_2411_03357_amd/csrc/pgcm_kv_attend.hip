@@ -5,9 +5,9 @@
 // with running m and sums, one pass over K and V.  What bounds it is memory: at sixteen heads an item, 2 flops a byte.
 //
 // The tiles of all items, 128 tokens each, are cut into equal spans, one for each workgroup, so that neither lengths nor their
-// number matter; an item of several workgroups is joined by the last of them.  A workgroup's four wavefronts take 32 tokens of
-// a tile each and are joined through LDS at an item's end; the next tile's rows, the next item's among them, are on their way
-// to LDS then.
+// number matter; an item of several workgroups is joined by the last of them, in two levels if they are many.  A workgroup's
+// four wavefronts take 32 tokens of a tile each and are joined through LDS at an item's end; the next tile's rows, the next
+// item's among them, are on their way to LDS then.
 #include "pgcm_kv_common.h"
 
 #include <cmath>
@@ -21,11 +21,16 @@ constexpr int64_t kMostTokenStride = 1 << 25;
 constexpr uint32_t kCus = 256;
 // Which workgroups there are, by the tiles of an item on average:
 //   up to kShortItem: one for each tile, if that fills no more than the chip; above, for two: joining more parts costs more than
-//   a tile does (one request of 4096 tokens, 8 kv heads: 15 us with two tiles each, 18 with one)
-//   from kLongItem on: one for each compute unit, whose four wavefronts have 64 KiB under way; with two, memory serves no more
-//   and in a worse order (1 GiB in 16 items: 201 us with one, 212 with two; 1280 items of 1 to 16 tiles, where one would be
-//   alone with each item's end: 115 and 95)
-constexpr uint32_t kShortItem = 8, kLongItem = 16;
+//   a tile does (one request of 4096 tokens, 8 kv heads: 14.1 us with two tiles each, 17.4 with one)
+//   from kLongItem on, if there are kManyTiles for each compute unit: one for each, whose four wavefronts have 64 KiB under way;
+//   with two, memory serves no more and in a worse order (1 GiB in 16 items, 64 tiles each: 201 us with one, 208 with two; 8
+//   items, 4 tiles each: 21.8 and 22.5).  With fewer tiles or shorter items one would be alone with each item's end (24 items,
+//   3.6 tiles each: 24.7 and 21.7; 1280 items of 1 to 16 tiles: 115 and 95).
+constexpr uint32_t kShortItem = 8, kLongItem = 16, kManyTiles = 4;
+// Parts of an item that are joined in one go, by what a thread reads of each; more are joined in groups, and the groups then: of
+// 128 channels and 4 heads, 16 parts 14.1 us in one go and 15.2 in two, 32 parts 19.5 and 17.7; 128 parts of 16 heads 79 and 35.
+constexpr uint32_t kJoinedAtOnce = 24;
+static_assert(kJoinedAtOnce * kJoinedAtOnce >= kAttendGroups, "two levels are enough");
 static_assert(kTileTokens == kWaves * 2 * kPiece, "two pieces a wavefront");
 
 struct AttendArgs {
@@ -82,7 +87,7 @@ struct AttendShared {
     union {
         float sum[kWaves][kMergedHeads][kDim + 4];
         struct {
-            float top[64][16], total[64][16];
+            float top[kJoinedAtOnce][16], total[kJoinedAtOnce][16];
         } part;
     };
     float top[kWaves][16], total[kWaves][16];
@@ -336,7 +341,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     if (all == 0) return;
     // ... in the order of requests and heads, are cut into equal spans: this workgroup's is [from, to).
     const uint32_t by_tiles = all / some <= kShortItem ? all : (all + 1) / 2, useful = by_tiles > some ? by_tiles : some;
-    uint32_t groups = all / some >= kLongItem && gridDim.x > kCus ? kCus : gridDim.x;
+    const bool alone = kDim == 256 || (all / some >= kLongItem && all >= kManyTiles * kCus);   // (of 256 channels, two have no room)
+    uint32_t groups = alone && gridDim.x > kCus ? kCus : gridDim.x;
     if (groups > useful) groups = useful;
     if (blockIdx.x >= groups) return;
     auto start_of = [&](uint32_t w) { return (uint32_t)((uint64_t)w * all / groups); };
@@ -517,10 +523,17 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
         constexpr uint32_t kQuads = kDim / 4;
         const uint32_t rows_kept = a.group < 16 ? a.group : 16;
         const size_t part_floats = (size_t)rows_kept * (kDim + 2);   // sums, then tops and totals
-        auto slot_of = [&](uint32_t w) {   // for a workgroup's first item, or for its last
-            return a.partials + (2 * (size_t)w + (item_from > start_of(w) ? 1 : 0)) * part_floats;
+        // (a workgroup's first item and its last one are the two of several parts)
+        auto slot_of = [&](uint32_t w) { return 2 * w + (item_from > start_of(w) ? 1 : 0); };
+        auto part_at = [&](uint32_t w) { return a.partials + slot_of(w) * part_floats; };
+        float* slot = part_at(blockIdx.x);
+        auto put_part = [&](float* part, uint32_t h, uint32_t d, float4 sum, float top, float total) {
+            uint64_t* to_sum = (uint64_t*)(part + h * kDim + d);
+            put_shared(to_sum, __builtin_bit_cast(uint64_t, make_float2(sum.x, sum.y)));
+            put_shared(to_sum + 1, __builtin_bit_cast(uint64_t, make_float2(sum.z, sum.w)));
+            if (d == 0)
+                put_shared((uint64_t*)(part + rows_kept * kDim) + h, __builtin_bit_cast(uint64_t, make_float2(top, total)));
         };
-        float* slot = slot_of(blockIdx.x);
         for (uint32_t h0 = 0; h0 < heads; h0 += kMergedHeads) {
             const uint32_t these = heads - h0 < kMergedHeads ? heads - h0 : kMergedHeads;
             __syncthreads();
@@ -552,58 +565,80 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                 if (parts == 1) {
                     finish(h0 + h, d, sum, top, total);
                 } else {
-                    uint64_t* to_sum = (uint64_t*)(slot + (h0 + h) * kDim + d);
-                    put_shared(to_sum, __builtin_bit_cast(uint64_t, make_float2(sum.x, sum.y)));
-                    put_shared(to_sum + 1, __builtin_bit_cast(uint64_t, make_float2(sum.z, sum.w)));
-                    if (d == 0)
-                        put_shared((uint64_t*)(slot + rows_kept * kDim) + h0 + h, __builtin_bit_cast(uint64_t, make_float2(top, total)));
+                    put_part(slot, h0 + h, d, sum, top, total);
                 }
             }
         }
-        if (parts > 1 && last_to_arrive(a.counters + now.request * per_request + now.item, parts, &shared.last)) {
-            // the parts' results as one, 64 parts at a step
-            constexpr uint32_t kMine = (16 * kQuads + kThreads - 1) / kThreads;
+        // The parts' results as one: those of workgroups first, first + apart, ..., to the outputs or to the first's place.
+        // (Loads of eight words under way together: sixteen take registers from the walk, 22.2 us and 19.7 for 480 items of 64
+        // channels; four 36.6 and 34.9 for two items of 16 heads.)
+        constexpr uint32_t kMine = (16 * kQuads + kThreads - 1) / kThreads, kTogether = 8 / kMine;
+        auto join = [&](uint32_t first, uint32_t apart, uint32_t count, bool last) {
+            for (uint32_t x = threadIdx.x; x < count * heads; x += kThreads) {
+                const uint32_t p = x / heads, h = x - p * heads;
+                const float2 y = __builtin_bit_cast(
+                    float2, get_shared((const uint64_t*)(part_at(first + p * apart) + rows_kept * kDim) + h));
+                shared.part.top[p][h] = y.x;
+                shared.part.total[p][h] = y.y;
+            }
+            __syncthreads();
             float4 sum[kMine];
             float top[kMine], total[kMine];
 #pragma unroll
-            for (uint32_t n = 0; n < kMine; ++n) sum[n] = make_float4(0.f, 0.f, 0.f, 0.f), top[n] = -INFINITY, total[n] = 0.f;
-            for (uint32_t p0 = 0; p0 < parts; p0 += 64) {
-                const uint32_t some = parts - p0 < 64 ? parts - p0 : 64;
-                __syncthreads();
-                for (uint32_t x = threadIdx.x; x < some * heads; x += kThreads) {
-                    const uint32_t p = x / heads, h = x - p * heads;
-                    const float2 y = __builtin_bit_cast(
-                        float2, get_shared((const uint64_t*)(slot_of(first_part + p0 + p) + rows_kept * kDim) + h));
-                    shared.part.top[p][h] = y.x;
-                    shared.part.total[p][h] = y.y;
+            for (uint32_t n = 0; n < kMine; ++n) {
+                const uint32_t x = threadIdx.x + n * kThreads, h = x / kQuads;
+                sum[n] = make_float4(0.f, 0.f, 0.f, 0.f), top[n] = -INFINITY, total[n] = 0.f;
+                if (x < heads * kQuads)
+                    for (uint32_t p = 0; p < count; ++p) top[n] = fmaxf(top[n], shared.part.top[p][h]);
+            }
+            for (uint32_t p0 = 0; p0 < count; p0 += kTogether) {
+                uint64_t y[kTogether][kMine][2];   // under way together
+#pragma unroll
+                for (uint32_t e = 0; e < kTogether; ++e) {
+                    const uint32_t p = p0 + e < count ? p0 + e : p0;
+                    const float* from = part_at(first + p * apart);
+#pragma unroll
+                    for (uint32_t n = 0; n < kMine; ++n) {
+                        const uint32_t x = threadIdx.x + n * kThreads;
+                        const uint64_t* at_sum = (const uint64_t*)(from + 4 * (x < heads * kQuads ? x : 0));
+                        y[e][n][0] = get_shared(at_sum), y[e][n][1] = get_shared(at_sum + 1);
+                    }
                 }
-                __syncthreads();
 #pragma unroll
                 for (uint32_t n = 0; n < kMine; ++n) {
-                    const uint32_t x = threadIdx.x + n * kThreads;
-                    if (x >= heads * kQuads) break;
-                    const uint32_t h = x / kQuads, d = x % kQuads * 4;
-                    float now = top[n];
-                    for (uint32_t p = 0; p < some; ++p) now = fmaxf(now, shared.part.top[p][h]);
-                    const float keep = exp2_from(top[n], now);
-                    top[n] = now;
-                    total[n] *= keep;
-                    sum[n].x *= keep, sum[n].y *= keep, sum[n].z *= keep, sum[n].w *= keep;
-#pragma unroll 8
-                    for (uint32_t p = 0; p < some; ++p) {
-                        const uint64_t* at_sum = (const uint64_t*)(slot_of(first_part + p0 + p) + h * kDim + d);
-                        const float2 y = __builtin_bit_cast(float2, get_shared(at_sum));
-                        const float2 z = __builtin_bit_cast(float2, get_shared(at_sum + 1));
-                        const float by = exp2_from(shared.part.top[p][h], now);
-                        total[n] += shared.part.total[p][h] * by;
-                        sum[n].x += y.x * by, sum[n].y += y.y * by, sum[n].z += z.x * by, sum[n].w += z.y * by;
+                    const uint32_t x = threadIdx.x + n * kThreads, h = x / kQuads;
+                    if (x >= heads * kQuads) continue;
+#pragma unroll
+                    for (uint32_t e = 0; e < kTogether; ++e) {
+                        if (p0 + e >= count) break;
+                        const float2 u = __builtin_bit_cast(float2, y[e][n][0]), v = __builtin_bit_cast(float2, y[e][n][1]);
+                        const float by = exp2_from(shared.part.top[p0 + e][h], top[n]);
+                        total[n] += shared.part.total[p0 + e][h] * by;
+                        sum[n].x += u.x * by, sum[n].y += u.y * by, sum[n].z += v.x * by, sum[n].w += v.y * by;
                     }
                 }
             }
+            float* to_part = part_at(first);
 #pragma unroll
             for (uint32_t n = 0; n < kMine; ++n) {
-                const uint32_t x = threadIdx.x + n * kThreads;
-                if (x < heads * kQuads) finish(x / kQuads, x % kQuads * 4, sum[n], top[n], total[n]);
+                const uint32_t x = threadIdx.x + n * kThreads, h = x / kQuads, d = x % kQuads * 4;
+                if (x >= heads * kQuads) continue;
+                if (last) finish(h, d, sum[n], top[n], total[n]);
+                else put_part(to_part, h, d, sum[n], top[n], total[n]);
+            }
+        };
+        if (parts > 1) {
+            // in one go, or in groups of as many as there are groups
+            uint32_t fan = parts;
+            if (parts * ((heads * kQuads + kThreads - 1) / kThreads) > kJoinedAtOnce)
+                for (fan = 4; fan * fan < parts;) ++fan;
+            const uint32_t mine = (blockIdx.x - first_part) / fan * fan, count = parts - mine < fan ? parts - mine : fan;
+            bool last = last_to_arrive(a.counters + slot_of(first_part + mine), count, &shared.last);
+            if (last) {
+                join(first_part + mine, 1, count, fan == parts);
+                const uint32_t groups_of = (parts + fan - 1) / fan;
+                if (fan < parts && last_to_arrive(a.counters + 2 * kAttendGroups + slot_of(first_part), groups_of, &shared.last))
+                    join(first_part, fan, groups_of, true);
             }
         }
         if (!more) return;

@@ -77,15 +77,14 @@ struct Room {
 };
 inline size_t whole_lines(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Attention: a counter for each request and group of up to sixteen query heads of one kv head; two partial results for
-// each workgroup; and, for weights, log-sums of heads and of each piece of a row.
+// Attention: two partial results for each workgroup, and for each of these two counters; and, for weights, log-sums of heads
+// and of each piece of a row.
 constexpr uint32_t kAttendGroups = 512;  // workgroups of a launch, at most
 inline size_t partial_floats(uint32_t head_dim, uint32_t group) {
     return (size_t)(group < 16 ? group : 16) * ((head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 2);
 }
 inline Room attend_room(uint32_t requests, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, uint64_t row_pieces) {
-    const size_t group = heads / kv_heads, items = kv_heads * ((group + kPiece - 1) / kPiece) * requests;
-    return Room{4 * items, whole_lines(4 * partial_floats(head_dim, group) * 2 * kAttendGroups) +
+    return Room{4 * 2 * 2 * kAttendGroups, whole_lines(4 * partial_floats(head_dim, heads / kv_heads) * 2 * kAttendGroups) +
                                whole_lines(4 * (size_t)requests * heads) + 4 * (size_t)requests * heads * row_pieces};
 }
 

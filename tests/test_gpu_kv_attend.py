@@ -123,6 +123,12 @@ def test_one_request_in_many_workgroups(dim, kv, group):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("dim,group,tokens", [(64, 1, 9000), (128, 16, 7001), (128, 3, 13000), (256, 20, 5000)])
+def test_parts_joined_in_groups(dim, group, tokens):
+    r = ref.Requests(21, [tokens, 40], 1, dim, BF16, holes=0.2)
+    _check(r, ref.numbers(21, 2, group, dim).to(BF16), weigh=True)
+
+
 def test_many_requests():
     """more than the lanes of a wavefront, most of them short or empty, as one batch"""
     rng = np.random.default_rng(5)
