@@ -48,18 +48,21 @@ __device__ __forceinline__ float over_lanes(float x, uint32_t power, Of of) {
 // dealt out to wavefronts, and to the blockIdx.y of a token.  A lane has the same channels of each of its heads, so the
 // factors of
 //   x by w c + y by w' s        (by: of the norm; y, w': the other channel of the pair and its weight; s with its sign)
-// are made once for a token, and a head takes five operations a channel.  8191 tokens, 40 heads and kv heads of 128 (508 MB):
-// 107 us, 4.7 TB/s, the rate of a large copy; 64 tokens of 32 and 8: 4.7 us, the launch and three loads one after the other.
+// are made once for a token, and a head takes five operations a channel.  What they take is asked for before anything is
+// waited for, the table's line in pieces of sixteen bytes (word by word, a batch of 300 tokens took twice as long).  8191
+// tokens, 40 heads and kv heads of 128 (508 MB): 104 us, 4.9 TB/s, the rate of a large copy; 64 tokens of 32 and 8: 4.7 us, the
+// launch and two loads one after the other.
 template <class H>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     const uint32_t token = blockIdx.x, lane = threadIdx.x % 64, lanes = 1u << a.row_power;
     const uint32_t part = lane & (lanes - 1), d = 8 * part, in_step = lane >> a.row_power, heads_at_once = 64u >> a.row_power;
     const bool mine = d < a.head_dim;
     const uint32_t of_q = (a.heads + heads_at_once - 1) / heads_at_once, of_k = (a.kv_heads + heads_at_once - 1) / heads_at_once;
-    const uint32_t steps = of_q + 2 * of_k, stride = kThreads / 64 * gridDim.y;
-    uint32_t step = __builtin_amdgcn_readfirstlane(blockIdx.y * (kThreads / 64) + threadIdx.x / 64);
+    const uint32_t steps = of_q + 2 * of_k, waves = blockDim.x / 64, stride = waves * gridDim.y;
+    uint32_t step = __builtin_amdgcn_readfirstlane(blockIdx.y * waves + threadIdx.x / 64);
 
     const int64_t slot = a.slots[token];
+    const int32_t position = a.rope == nullptr ? 0 : a.positions[token];
     const bool stored = (uint64_t)slot < a.pool_tokens;
     // the lane's head of a step, and whether it is there and wanted
     struct Head {
@@ -81,38 +84,49 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     uint4 words = make_uint4(0, 0, 0, 0);
     if (step < steps) words = load(step);      // under way while the factors are made
 
-    float own[2][8], other[2][8];              // factors of queries and of keys
     const uint32_t half = a.rope_dim / 2;
     const bool turned = a.rope != nullptr && d < a.rope_dim;
     const bool halves = a.rope != nullptr && a.adjacent == 0;
     uint32_t partner = part;                   // the lane with the other channels of the pairs
     if (halves && turned) partner = d < half ? part + half / 8 : part - half / 8;
+    // weights of queries' channels and of keys', and those of the partner's
+    uint4 weight[2], far_weight[2];
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        const uint8_t* from = k == 0 ? a.q_weight : a.k_weight;
+        weight[k] = far_weight[k] = make_uint4(0, 0, 0, 0);
+        if (from != nullptr && mine) weight[k] = *(const uint4*)(from + 2 * d), far_weight[k] = *(const uint4*)(from + 16 * partner);
+    }
+    float own[2][8], other[2][8];              // factors of queries and of keys
     {
+        const bool known = (uint32_t)position < a.rope_positions;
         float c[8], s[8];
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) c[e] = 1.f, s[e] = 0.f;
         if (turned) {
-            const int32_t position = a.positions[token];
-            const bool known = (uint32_t)position < a.rope_positions;
-            const float* line = a.rope + (known ? (size_t)position * a.rope_dim : 0);
+            // eight pairs in a row, or four (an adjacent pair's channels have the same)
+            const float* line = a.rope + (known ? (size_t)position * a.rope_dim : 0) + (a.adjacent ? d / 2 : d < half ? d : d - half);
+            const float4 c0 = *(const float4*)line, s0 = *(const float4*)(line + half);
+            if (a.adjacent) {
+                c[0] = c[1] = c0.x, c[2] = c[3] = c0.y, c[4] = c[5] = c0.z, c[6] = c[7] = c0.w;
+                s[1] = s0.x, s[3] = s0.y, s[5] = s0.z, s[7] = s0.w;
+                s[0] = -s0.x, s[2] = -s0.y, s[4] = -s0.z, s[6] = -s0.w;
+            } else {
+                const float4 c1 = *(const float4*)(line + 4), s1 = *(const float4*)(line + half + 4);
+                c[0] = c0.x, c[1] = c0.y, c[2] = c0.z, c[3] = c0.w, c[4] = c1.x, c[5] = c1.y, c[6] = c1.z, c[7] = c1.w;
+                s[0] = s0.x, s[1] = s0.y, s[2] = s0.z, s[3] = s0.w, s[4] = s1.x, s[5] = s1.y, s[6] = s1.z, s[7] = s1.w;
+                if (d < half)
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) {
-                const uint32_t n = a.adjacent ? (d + e) / 2 : (d < half ? d : d - half) + e;
-                const bool second = a.adjacent ? e % 2 : d >= half;
-                c[e] = known ? line[n] : NAN;
-                s[e] = known ? line[half + n] : NAN;
-                if (!second) s[e] = -s[e];
+                    for (uint32_t e = 0; e < 8; ++e) s[e] = -s[e];
             }
+            if (!known)
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) c[e] = s[e] = NAN;
         }
 #pragma unroll
         for (uint32_t k = 0; k < 2; ++k) {
-            const uint8_t* from = k == 0 ? a.q_weight : a.k_weight;
-            typename H::eight x{}, y{};
-            const bool there = from != nullptr && mine;
-            if (there) {
-                x = as_eight<H>(*(const uint4*)(from + 2 * d));
-                y = as_eight<H>(*(const uint4*)(from + 16 * partner));
-            }
+            const bool there = (k == 0 ? a.q_weight : a.k_weight) != nullptr;
+            const typename H::eight x = as_eight<H>(weight[k]), y = as_eight<H>(far_weight[k]);
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) {
                 own[k][e] = (there ? (float)x[e] : 1.f) * c[e];
@@ -342,15 +356,22 @@ int pgcm_kv_append(const pgcm_kv_cache* cache, const pgcm_kv_append_args* args, 
     a.rope_positions = args->rope_positions, a.rope_dim = args->rope_dim, a.adjacent = args->adjacent;
     a.row_power = row_power_of(dim);
     a.eps = args->eps, a.by_dim = 1.f / (float)dim;
-    // a token's heads in one workgroup, or in several where tokens alone would not fill the chip
+    // A token's workgroup: a wavefront for every eight steps, so that the factors are worth making (8000 tokens of six steps: one
+    // 19.4 us, two 21.3, four 27.4; 2000 of 24 steps: two 23.8, three 21.3, four 24.1; 8191 of 30: two 108.6, four 103.2), but
+    // not under 4096 in all; and several workgroups where tokens alone would not fill the chip.
     const uint32_t at_once = 64u >> a.row_power;
     const uint32_t steps = (a.heads + at_once - 1) / at_once + 2 * ((a.kv_heads + at_once - 1) / at_once);
-    const uint32_t passes = (steps + kThreads / 64 - 1) / (kThreads / 64);
+    constexpr uint32_t kWaves = kThreads / 64;
+    uint32_t waves = (steps + 7) / 8;
+    if (waves < (4096 + args->tokens - 1) / args->tokens) waves = (4096 + args->tokens - 1) / args->tokens;
+    if (waves > kWaves) waves = kWaves;
+    const uint32_t passes = (steps + waves - 1) / waves;
     uint32_t ways = args->tokens >= 1024 ? 1 : (1024 + args->tokens - 1) / args->tokens;
     if (ways > passes) ways = passes;
+    const uint32_t threads = 64 * waves;
     const dim3 grid(args->tokens, ways);
-    if (cache->half == PGCM_KV_F16) append_kernel<F16><<<grid, kThreads, 0, (hipStream_t)hip_stream>>>(a);
-    else append_kernel<Bf16><<<grid, kThreads, 0, (hipStream_t)hip_stream>>>(a);
+    if (cache->half == PGCM_KV_F16) append_kernel<F16><<<grid, threads, 0, (hipStream_t)hip_stream>>>(a);
+    else append_kernel<Bf16><<<grid, threads, 0, (hipStream_t)hip_stream>>>(a);
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 

@@ -64,6 +64,26 @@ def test_append(half, dim, rope_dim, adjacent):
         assert bool((pool == 7.0).all())        # nothing else was written
 
 
+@pytest.mark.parametrize("tokens,heads,kv,dim", [(4097, 3, 1, 64), (2100, 8, 2, 128), (4100, 20, 10, 80), (1400, 16, 8, 256)])
+def test_append_many_tokens(tokens, heads, kv, dim):
+    """workgroups of one wavefront to four"""
+    half, block = BF16, 32
+    blocks = -(-tokens // block)
+    x = ref.numbers(6, tokens, heads + 2 * kv, dim).to(half)
+    weight, table = (1 + ref.numbers(7, dim, std=0.3)).to(half), _table(tokens, dim)
+    slots = np.random.default_rng(8).permutation(block * blocks)[:tokens]
+    packed, pool = x.cuda(), torch.empty(blocks, 2, block, kv, dim, dtype=half, device="cuda")
+    out = torch.empty(tokens, heads, dim, dtype=half, device="cuda")
+    pgcm.kv_append(pgcm.KVCache(pool[:, 0], pool[:, 1]), packed[:, :heads], packed[:, heads:heads + kv], packed[:, heads + kv:],
+                   torch.arange(tokens, dtype=torch.int32).cuda(), torch.from_numpy(slots).cuda(), out,
+                   q_weight=weight.cuda(), k_weight=weight.cuda(), eps=1e-5, rope=table.cuda())
+    want = ref.turned(x[:, :heads + kv], weight, 1e-5, table, range(tokens), False)
+    _near(out, want[:, :heads], None, half, dim, "q")
+    at, pool = (slots // block, slots % block), pool.cpu()
+    _near(pool[:, 0][at], want[:, heads:], None, half, dim, "k")
+    assert torch.equal(pool[:, 1][at], x[:, heads + kv:])
+
+
 def test_append_passes_over_slots_and_marks_positions():
     half, kv, dim = BF16, 2, 64
     x = ref.numbers(3, 6, 4 + 2 * kv, dim).to(half)
