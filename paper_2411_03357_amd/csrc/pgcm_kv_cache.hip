@@ -199,7 +199,7 @@ struct SummarizeArgs {
     int8_t* bounds;
     float* scales;
     int64_t k_block, k_token, k_head;  // bytes
-    uint32_t n, kv_heads, head_dim, block_tokens, pool, entry_count, row_power;
+    uint32_t n, kv_heads, head_dim, block_tokens, pool, entry_count, row_power, group_power;
 };
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
@@ -220,24 +220,29 @@ __device__ __forceinline__ uint32_t opposite(uint32_t x, uint32_t n) {
     return __shfl_xor(x, 1u << n);
 }
 
-// A wavefront for each block and head: 64 / 2^row_power tokens at a time.  Least and largest values are those of the halves as
-// whole numbers in order, two an instruction; whatever is not finite lies at the ends of that order, and if any is found there
-// the block is gone through again with zeros in such places.  8192
-// blocks of 8 heads of 128 (286 MB): 61 us, 4.7 TB/s, the rate of a large copy; with one token's load at a time 68.
-template <class H>
+// 2^group_power lanes for each block and head: 2^(group_power - row_power) tokens at a time.  Least and largest values are those
+// of the halves as whole numbers in order, two an instruction; whatever is not finite lies at the ends of that order, and if any
+// is found there the block is gone through again with zeros in such places.  8192 blocks of 8 heads of 128 (286 MB): 61 us, 4.7
+// TB/s, the rate of a large copy; with one token's load at a time 68.  kWhole: all lanes of the wavefront (known when compiled,
+// so that the block's numbers are the wavefront's: 61 us and 63).
+template <class H, bool kWhole>
 __global__ __launch_bounds__(kThreads) void summarize_kernel(SummarizeArgs a) {
-    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint64_t task = (uint64_t)blockIdx.x * (kThreads / 64) + wave;
-    const uint32_t n = (uint32_t)(task / a.kv_heads), head = (uint32_t)(task - (uint64_t)n * a.kv_heads);
-    if (n >= a.n) return;
-    const uint32_t block = (uint32_t)a.blocks[n], entry = a.entries == nullptr ? block : (uint32_t)a.entries[n];
-    if (block >= a.pool || entry >= a.entry_count) return;
-    const int32_t asked = a.counts[n];
-    const uint32_t count = asked <= 0 ? 0u : (uint32_t)asked < a.block_tokens ? (uint32_t)asked : a.block_tokens;
-    const uint32_t lanes = 1u << a.row_power, part = lane & (lanes - 1), d = 8 * part, at_once = 64u >> a.row_power;
-    const uint32_t in_turn = lane >> a.row_power;
+    const uint32_t lane = threadIdx.x % 64, group_power = kWhole ? 6 : a.group_power;
+    const uint32_t in_workgroup = threadIdx.x >> group_power;
+    const uint32_t task = blockIdx.x * (kThreads >> group_power) + (kWhole ? __builtin_amdgcn_readfirstlane(in_workgroup) : in_workgroup);
+    const uint32_t n = task / a.kv_heads, head = task - n * a.kv_heads;
+    uint32_t block = ~0u, entry = ~0u;
+    int32_t asked = 0;
+    if (n < a.n) {
+        block = (uint32_t)a.blocks[n], entry = a.entries == nullptr ? block : (uint32_t)a.entries[n];
+        asked = a.counts[n];
+    }
+    const bool wanted = block < a.pool && entry < a.entry_count;
+    const uint32_t count = !wanted || asked <= 0 ? 0u : (uint32_t)asked < a.block_tokens ? (uint32_t)asked : a.block_tokens;
+    const uint32_t lanes = 1u << a.row_power, part = lane & (lanes - 1), d = 8 * part, at_once = 1u << (group_power - a.row_power);
+    const uint32_t in_turn = lane >> a.row_power & (at_once - 1);
     const bool mine = d < a.head_dim;
-    const uint8_t* from = a.k + block * a.k_block + head * a.k_head + 2 * d;
+    const uint8_t* from = a.k + (wanted ? block * a.k_block + head * a.k_head : 0) + 2 * d;
 
     s16x2 low[4], high[4];
     auto walk = [&](auto careful) {
@@ -268,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void summarize_kernel(SummarizeArgs a) {
         }
     };
     walk(std::false_type());
-    if (count != 0) {
+    {
         s16x2 least = low[0], most = high[0];
 #pragma unroll
         for (uint32_t w = 0; w < 4; ++w)
@@ -281,7 +286,7 @@ __global__ __launch_bounds__(kThreads) void summarize_kernel(SummarizeArgs a) {
         const uint16_t bits = (uint16_t)(word >> (16 * e));
         return (float)__builtin_bit_cast(typename H::one, bits);
     };
-    for (uint32_t l = a.row_power; l < 6; ++l)
+    for (uint32_t l = a.row_power; l < group_power; ++l)
 #pragma unroll
         for (uint32_t w = 0; w < 4; ++w) {
             low[w] = __builtin_elementwise_min(low[w], as_two(opposite(as_word(low[w]), l)));
@@ -311,9 +316,9 @@ __global__ __launch_bounds__(kThreads) void summarize_kernel(SummarizeArgs a) {
             const int32_t whole = small ? 0 : (int32_t)rintf(value(e < 2 ? pair0 : pair1, e % 2) * by);
             bytes |= ((uint32_t)whole & 0xFF) << (8 * e);
         }
-        if (mine) *(uint32_t*)(a.bounds + to * 2 * a.head_dim + (w / 2) * a.head_dim + d + 4 * (w % 2)) = bytes;
+        if (mine && wanted) *(uint32_t*)(a.bounds + to * 2 * a.head_dim + (w / 2) * a.head_dim + d + 4 * (w % 2)) = bytes;
     }
-    if (lane == 0) a.scales[to] = small ? 0.f : most / 127.f;
+    if (part == 0 && in_turn == 0 && wanted) a.scales[to] = small ? 0.f : most / 127.f;
 }
 
 }  // namespace
@@ -389,9 +394,20 @@ int pgcm_kv_summarize(const pgcm_kv_cache* cache, uint32_t n, const int32_t* blo
     a.k_block = 2 * cache->k_block, a.k_token = 2 * cache->k_token, a.k_head = 2 * cache->k_head;
     a.n = n, a.kv_heads = cache->kv_heads, a.head_dim = cache->head_dim, a.block_tokens = cache->block_tokens;
     a.pool = cache->blocks, a.entry_count = entry_count, a.row_power = row_power_of(cache->head_dim);
-    const uint32_t groups = (uint32_t)(((uint64_t)n * a.kv_heads + kThreads / 64 - 1) / (kThreads / 64));
-    if (cache->half == PGCM_KV_F16) summarize_kernel<F16><<<groups, kThreads, 0, (hipStream_t)hip_stream>>>(a);
-    else summarize_kernel<Bf16><<<groups, kThreads, 0, (hipStream_t)hip_stream>>>(a);
+    // four tokens a lane, if a wavefront's lanes are too many for that (8000 blocks of 16 tokens, 4 heads of 64: 26.4 us with a
+    // wavefront each, 13 with half of one)
+    a.group_power = a.row_power;
+    while (a.group_power < 6 && (4u << (a.group_power - a.row_power)) < a.block_tokens) ++a.group_power;
+    const uint64_t threads = (uint64_t)n * a.kv_heads << a.group_power;
+    const uint32_t groups = (uint32_t)((threads + kThreads - 1) / kThreads);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (cache->half == PGCM_KV_F16) {
+        if (a.group_power == 6) summarize_kernel<F16, true><<<groups, kThreads, 0, stream>>>(a);
+        else summarize_kernel<F16, false><<<groups, kThreads, 0, stream>>>(a);
+    } else {
+        if (a.group_power == 6) summarize_kernel<Bf16, true><<<groups, kThreads, 0, stream>>>(a);
+        else summarize_kernel<Bf16, false><<<groups, kThreads, 0, stream>>>(a);
+    }
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 
