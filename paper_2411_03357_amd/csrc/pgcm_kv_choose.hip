@@ -270,8 +270,11 @@ __device__ __forceinline__ void choose_list(const SelectArgs& a, uint32_t list, 
 }
 
 constexpr uint32_t kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
-constexpr uint32_t kWaveBlocks = 64;                          // that a wavefront scores at a time, in four steps
-constexpr uint32_t kPartBlocks = kScoreWaves * kWaveBlocks;   // ... and a workgroup
+// A wavefront scores 16 kSteps blocks at a time, a part of a row so many times its wavefronts: four steps, or one where four
+// would leave half of the compute units without a part (8 lists of 1250 blocks, 256 channels: 14 us with one, 20 with four; 256
+// lists of up to 2048 blocks, 128 channels: 28 and 22).
+constexpr uint32_t kMostSteps = 4, kFewParts = 128;
+__host__ __device__ constexpr uint32_t part_blocks(uint32_t steps) { return kScoreWaves * 16 * steps; }
 // Rows scored and chosen from in one launch, a workgroup each: of up to kShortBlocks (one request with 8 lists: of 100 blocks
 // 8.4 us, of 500 11.7, in two launches 11.2 and 12.6), and of up to kWholeBlocks where there are lists for all compute units
 // (of 1000 blocks: 32 requests 21.4 us and 22.9, one 16.1 and 13.1).
@@ -280,11 +283,12 @@ constexpr uint32_t kShortBlocks = 512, kWholeBlocks = 1024, kListsToFill = 256;
 // Keys of the blocks [from, to) of a request for one kv head, at key_of(j).  The scores are products on the matrix cores,
 // of 2 head_dim whole numbers: for each of sixteen query heads, its negative channels (for the least values) and its
 // positive ones, with the bounds of sixteen blocks.  All threads call it; q8 and q_scale are theirs.
-template <class H, uint32_t kChunks, class KeyOf>   // kChunks pieces of 64 numbers
+template <class H, uint32_t kChunks, uint32_t kSteps, class KeyOf>   // kChunks pieces of 64 numbers
 __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uint32_t head, uint32_t from, uint32_t to,
                                       uint32_t blocks, int8_t (&q8)[16][64 * kChunks + 16], float (&q_scale)[16], KeyOf key_of) {
     // what the registers hold of bounds: steps, and pieces of each
-    constexpr uint32_t kTogether = kChunks == 2 ? 4 : kChunks == 4 ? 2 : 1, kAtOnce = kChunks < 4 ? kChunks : 4;
+    constexpr uint32_t kTogether = kSteps == 1 ? 1 : kChunks == 4 ? 2 : 4, kAtOnce = kChunks < 4 || kSteps == 1 ? kChunks : 4;
+    constexpr uint32_t kWaveBlocks = 16 * kSteps;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, i = lane % 16;
     const uint32_t numbers = 2 * a.head_dim;
     const uint64_t entry_bytes = (uint64_t)a.kv_heads * numbers;
@@ -321,7 +325,7 @@ __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uin
             }
         };
         auto begin = [&](uint32_t j0) {
-            const uint32_t entry = j0 + lane < to ? (uint32_t)row[j0 + lane] : ~0u;
+            const uint32_t entry = lane < kWaveBlocks && j0 + lane < to ? (uint32_t)row[j0 + lane] : ~0u;
             able = __ballot(entry < a.entry_count);
             known = entry < a.entry_count ? entry : 0;
             scale = a.scales[(uint64_t)known * a.kv_heads + head];
@@ -364,7 +368,7 @@ __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uin
 
         while (j0 < to) {
 #pragma unroll
-            for (uint32_t t0 = 0; t0 < 4; t0 += kTogether) {
+            for (uint32_t t0 = 0; t0 < kSteps; t0 += kTogether) {
                 i32x4 sum[kTogether];
 #pragma unroll
                 for (uint32_t first = 0; first < kChunks; first += kAtOnce) {
@@ -375,7 +379,7 @@ __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uin
                             sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[first + c], x[t][c],
                                                                            first + c == 0 ? i32x4{0, 0, 0, 0} : sum[t], 0, 0, 0);
                     if (first + kAtOnce < kChunks) load(t0, first + kAtOnce);
-                    else if (t0 + kTogether < 4) load(t0 + kTogether, 0);
+                    else if (t0 + kTogether < kSteps) load(t0 + kTogether, 0);
                 }
 #pragma unroll
                 for (uint32_t t = 0; t < kTogether; ++t) {
@@ -394,7 +398,7 @@ __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uin
                     }
                 }
             }
-            j0 += kPartBlocks;
+            j0 += part_blocks(kSteps);
             if (j0 < to) begin(j0);
         }
     }
@@ -402,20 +406,20 @@ __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uin
 
 // Rows of any length, part by part.  The heads of a part, whose entries and scales share lines, run on one XCD; parts go to
 // the XCDs in turn.
-template <class H, uint32_t kChunks>
-__global__ __launch_bounds__(kScoreThreads, 4) void score_kernel(SelectArgs a) {
+template <class H, uint32_t kChunks, uint32_t kSteps>
+__global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void score_kernel(SelectArgs a) {
     __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
     __shared__ float q_scale[16];
     const uint32_t in_xcd = blockIdx.x / kXcds, head = in_xcd % a.kv_heads;
     const uint32_t part = in_xcd / a.kv_heads * kXcds + blockIdx.x % kXcds;
     // (each row begins with another of its parts: those that every row has would otherwise all go to one XCD)
-    const uint32_t request = part / a.parts, from = (part + request) % a.parts * kPartBlocks;
+    const uint32_t request = part / a.parts, from = (part + request) % a.parts * part_blocks(kSteps);
     if (request >= a.requests) return;
     const uint32_t blocks = blocks_of(a, request);
     if (from >= blocks) return;
-    const uint32_t to = blocks - from < kPartBlocks ? blocks : from + kPartBlocks;
+    const uint32_t to = blocks - from < part_blocks(kSteps) ? blocks : from + part_blocks(kSteps);
     uint32_t* keys = a.keys + ((size_t)request * a.kv_heads + head) * a.row_blocks;
-    score<H, kChunks>(a, request, head, from, to, blocks, q8, q_scale, [&](uint32_t j) { return keys + j; });
+    score<H, kChunks, kSteps>(a, request, head, from, to, blocks, q8, q_scale, [&](uint32_t j) { return keys + j; });
 }
 
 __global__ __launch_bounds__(kMostThreads) void choose_kernel(SelectArgs a) {
@@ -444,7 +448,7 @@ __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void select_ke
     __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
     __shared__ float q_scale[16];
     const uint32_t list = blockIdx.x, request = list / a.kv_heads, blocks = blocks_of(a, request);
-    score<H, kChunks>(a, request, list % a.kv_heads, 0, blocks, blocks, q8, q_scale, [&](uint32_t j) { return row_keys + j; });
+    score<H, kChunks, kMostSteps>(a, request, list % a.kv_heads, 0, blocks, blocks, q8, q_scale, [&](uint32_t j) { return row_keys + j; });
     __syncthreads();
     HeldKeys<kScoreThreads> keys(blocks);
 #pragma unroll
@@ -455,19 +459,26 @@ __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void select_ke
     choose_list<kScoreThreads>(a, list, keys, shared);
 }
 
+template <class H, uint32_t kChunks, uint32_t kSteps>
+void launch_score(SelectArgs& a, hipStream_t stream) {
+    a.parts = (a.row_blocks + part_blocks(kSteps) - 1) / part_blocks(kSteps);
+    const uint32_t parts = (a.requests * a.parts + kXcds - 1) / kXcds * kXcds;
+    score_kernel<H, kChunks, kSteps><<<parts * a.kv_heads, kScoreThreads, 0, stream>>>(a);
+}
 template <class H, uint32_t kChunks>
-void launch(const SelectArgs& a, hipStream_t stream) {
+void launch(SelectArgs& a, hipStream_t stream) {
     const uint32_t lists = a.requests * a.kv_heads;
     if (a.row_blocks <= kShortBlocks || (a.row_blocks <= kWholeBlocks && lists >= kListsToFill)) {
         select_kernel<H, kChunks><<<lists, kScoreThreads, 0, stream>>>(a);
         return;
     }
-    const uint32_t parts = (a.requests * a.parts + kXcds - 1) / kXcds * kXcds;
-    score_kernel<H, kChunks><<<parts * a.kv_heads, kScoreThreads, 0, stream>>>(a);
+    const uint64_t parts = (uint64_t)lists * ((a.row_blocks + part_blocks(kMostSteps) - 1) / part_blocks(kMostSteps));
+    if (parts > kFewParts) launch_score<H, kChunks, kMostSteps>(a, stream);
+    else launch_score<H, kChunks, 1>(a, stream);
     choose_kernel<<<lists, kMostThreads, 0, stream>>>(a);
 }
 template <class H>
-void launch(const SelectArgs& a, hipStream_t stream) {
+void launch(SelectArgs& a, hipStream_t stream) {
     if (a.head_dim <= 64) launch<H, 2>(a, stream);
     else if (a.head_dim <= 128) launch<H, 4>(a, stream);
     else launch<H, 8>(a, stream);
@@ -506,7 +517,6 @@ int pgcm_kv_select(pgcm_kv_t* kv, const pgcm_kv_select_args* args, void* hip_str
     a.requests = args->requests, a.kv_heads = args->kv_heads, a.group = args->heads / args->kv_heads;
     a.head_dim = args->head_dim, a.block_tokens = args->block_tokens, a.row_blocks = args->row_blocks;
     a.entry_count = args->entry_count, a.keep = args->keep, a.first = args->first, a.last = args->last;
-    a.parts = (args->row_blocks + kPartBlocks - 1) / kPartBlocks;
     if (args->half == PGCM_KV_F16) launch<F16>(a, stream);
     else launch<Bf16>(a, stream);
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
