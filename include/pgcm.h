@@ -60,14 +60,14 @@ typedef enum {
     PGCM_OK = 0,
     PGCM_ERR_ARG = -1,   /* a required pointer is NULL, n is too large, a key or IV length is
                             not allowed, or the key lives on another GPU */
-    PGCM_ERR_ALIGN = -2, /* a src or dst pointer is not 16-byte aligned */
+    PGCM_ERR_ALIGN = -2, /* a src or dst pointer is not 16-byte aligned (pgcm_kv.h: a pointer or a stride) */
     PGCM_ERR_LEN = -3,   /* a chunk is longer than 2^36 - 32 bytes (the GCM limit), or than a
                             forced unit size allows (pgcm_set_unit_bytes) */
     PGCM_ERR_NOMEM = -4, /* host or device allocation failed */
     PGCM_ERR_HIP = -5,   /* a HIP call failed; see pgcm_last_hip_error */
     PGCM_ERR_BUSY = -6,  /* pgcm_bounce.h: every buffer of a pool is held */
     PGCM_ERR_CAPACITY = -7 /* pgcm_encrypt_batch_static: the batch needs more than the fixed
-                              buffers of that call hold */
+                              buffers of that call hold; pgcm_kv.h: a captured call would have to allocate */
 } pgcm_status;
 
 #define PGCM_MAX_CHUNK_BYTES ((((uint64_t)1) << 36) - 32)
