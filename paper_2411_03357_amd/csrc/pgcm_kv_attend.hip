@@ -342,14 +342,18 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     all *= per_request;
     some *= per_request;
     if (all == 0) return;
-    // ... in the order of requests and heads, are cut into equal spans: this workgroup's is [from, to).
+    // ... in the order of requests and heads, are cut into equal spans (of one tile more or less): this workgroup's is [from, to).
     const uint32_t by_tiles = all / some <= kShortItem ? all : (all + 1) / 2, useful = by_tiles > some ? by_tiles : some;
     const bool alone = kDim == 256 || (all / some >= kLongItem && all >= kManyTiles * kCus);   // (of 256 channels, two have no room)
     uint32_t groups = alone && gridDim.x > kCus ? kCus : gridDim.x;
     if (groups > useful) groups = useful;
     if (blockIdx.x >= groups) return;
-    auto start_of = [&](uint32_t w) { return (uint32_t)((uint64_t)w * all / groups); };
-    auto owner_of = [&](uint32_t tile) { return (uint32_t)((((uint64_t)tile + 1) * groups - 1) / all); };
+    const uint32_t share = all / groups, longer = all - share * groups;   // the first `longer` spans have one tile more
+    auto start_of = [&](uint32_t w) { return w * share + (w < longer ? w : longer); };
+    auto owner_of = [&](uint32_t tile) {
+        const uint32_t in_longer = longer * (share + 1), x = tile - longer;   // (of the others: less what the longer ones have more)
+        return tile < in_longer ? tile / (share + 1) : x / share;
+    };
     const uint32_t from = start_of(blockIdx.x), to = start_of(blockIdx.x + 1);
 
     // the request that the span begins in, and its first tile
