@@ -4,13 +4,13 @@
 //   s[t][h] = scale k_t . q_h,   m = max s,   out = sum 2^(s - m) v_t / sum 2^(s - m)     (s in units of log 2)
 // with running m and sums, one pass over K and V.  What bounds it is memory: at sixteen heads an item, 16 flops a byte.
 // Two requests of 131 059 tokens, 8 kv heads of 128 (1.07 GB): 201 us, 5.3 TB/s, each byte read once; a kernel that only reads
-// the same rows takes 192 to 206.  32 of up to 2048 tokens, 40 heads of 128 (396 MB): 91 us, 4.4 TB/s.  One of 33 tokens, 40
+// the same rows takes 192 to 206.  32 of up to 2048 tokens, 40 heads of 128 (396 MB): 86 us, 4.6 TB/s.  One of 33 tokens, 40
 // heads: 6.5 us, the launch and trips to memory one after the other (lengths, tables, rows).
 //
 // The tiles of all items, 128 tokens each, are cut into equal spans, one for each workgroup, so that neither lengths nor their
-// number matter; an item of several workgroups is joined by the last of them, in two levels if they are many.  A workgroup's
-// four wavefronts take 32 tokens of a tile each and are joined through LDS at an item's end; the next tile's rows, the next
-// item's among them, are on their way to LDS then.
+// number matter (short items are left whole); an item of several workgroups is joined by the last of them, in two levels if they
+// are many.  A workgroup's four wavefronts take 32 tokens of a tile each and are joined through LDS at an item's end; the next
+// tile's rows, the next item's among them, are on their way to LDS then.
 #include "pgcm_kv_common.h"
 
 #include <cmath>
@@ -22,13 +22,16 @@ constexpr uint32_t kWaves = 4;
 constexpr uint32_t kThreads = kWaves * 64;
 constexpr int64_t kMostTokenStride = 1 << 25;
 constexpr uint32_t kCus = 256;
-// Which workgroups there are, by the tiles of an item on average:
+// Which workgroups there are.  One for each item, if none is longer than kWholeTiles, or than kWholeTilesOfMany where there are
+// kManyItems: joining parts costs more than a few tiles do (80 items of 4 tiles: 10.3 us, in parts 12.0; 504 of up to 4, 14.7 and
+// 19.6; 248 of up to 5, 17.0 and 17.6; but 8 items of 8 tiles 12.8 and 9.6).  Else, by the tiles of an item on average:
 //   up to kShortItem: one for each tile, if that fills no more than the chip; above, for two: joining more parts costs more than
 //   a tile does (one request of 4096 tokens, 8 kv heads: 14.1 us with two tiles each, 17.4 with one)
 //   from kLongItem on, if there are kManyTiles for each compute unit: one for each, whose four wavefronts have 64 KiB under way;
 //   with two, memory serves no more and in a worse order (1 GiB in 16 items, 64 tiles each: 201 us with one, 208 with two; 8
 //   items, 4 tiles each: 21.8 and 22.5).  With fewer tiles or shorter items one would be alone with each item's end (24 items,
 //   3.6 tiles each: 24.7 and 21.7; 1280 items of 1 to 16 tiles: 115 and 95).
+constexpr uint32_t kWholeTiles = 4, kWholeTilesOfMany = 8, kManyItems = 64;
 constexpr uint32_t kShortItem = 8, kLongItem = 16, kManyTiles = 4;
 // Parts of an item that are joined in one go, by what a thread reads of each; more are joined in groups, and the groups then: of
 // 128 channels and 4 heads, 16 parts 14.1 us in one go and 15.2 in two, 32 parts 19.5 and 17.7; 128 parts of 16 heads 79 and 35.
@@ -321,12 +324,13 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     const uint32_t per_request = a.kv_heads * a.group_tiles;
 
     // The tiles of all items
-    uint32_t some = 0, all = 0, tiles = 0;   // requests with any; all tiles; those of request `lane`, or of the last 64
+    uint32_t some = 0, all = 0, longest = 0, tiles = 0;   // requests with any; all tiles; of a request; of request `lane`, or of the last 64
     for (uint32_t b0 = 0; b0 < a.requests; b0 += 64) {
         const uint32_t b = b0 + lane;
         tiles = b < a.requests ? tiles_of(a, b) : 0;
         all += __builtin_amdgcn_readlane(scan(tiles), 63);
         some += __builtin_popcountll(__ballot(tiles != 0));
+        longest = tiles > longest ? tiles : longest;
         // requests without tokens are answered here
         uint64_t empty = __ballot(b < a.requests && tiles == 0 && b % gridDim.x == blockIdx.x);
         for (; empty != 0; empty &= empty - 1) {
@@ -342,11 +346,15 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     all *= per_request;
     some *= per_request;
     if (all == 0) return;
-    // ... in the order of requests and heads, are cut into equal spans (of one tile more or less): this workgroup's is [from, to).
+    longest = over_wave(longest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    const bool whole = longest <= (some >= kManyItems ? kWholeTilesOfMany : kWholeTiles) && some <= gridDim.x;
+    // ... in the order of requests and heads, are cut into equal spans (of one tile more or less), or at the items' ends: this
+    // workgroup's is [from, to).
     const uint32_t by_tiles = all / some <= kShortItem ? all : (all + 1) / 2, useful = by_tiles > some ? by_tiles : some;
     const bool alone = kDim == 256 || (all / some >= kLongItem && all >= kManyTiles * kCus);   // (of 256 channels, two have no room)
     uint32_t groups = alone && gridDim.x > kCus ? kCus : gridDim.x;
     if (groups > useful) groups = useful;
+    if (whole) groups = some;
     if (blockIdx.x >= groups) return;
     const uint32_t share = all / groups, longer = all - share * groups;   // the first `longer` spans have one tile more
     auto start_of = [&](uint32_t w) { return w * share + (w < longer ? w : longer); };
@@ -354,24 +362,34 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
         const uint32_t in_longer = longer * (share + 1), x = tile - longer;   // (of the others: less what the longer ones have more)
         return tile < in_longer ? tile / (share + 1) : x / share;
     };
-    const uint32_t from = start_of(blockIdx.x), to = start_of(blockIdx.x + 1);
+    uint32_t from = start_of(blockIdx.x), to = start_of(blockIdx.x + 1);
 
     // the request that the span begins in, and its first tile
     uint32_t request = 0, before = 0;
-    for (uint32_t b0 = 0, sum = 0; b0 < a.requests; b0 += 64) {
+    for (uint32_t b0 = 0, sum = 0, there = 0; b0 < a.requests; b0 += 64) {
         if (a.requests > 64) tiles = b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
         const uint32_t upto = sum + scan(tiles);
-        const uint64_t past = __ballot(upto * per_request > from);
+        const uint64_t any = __ballot(tiles != 0);
+        const uint32_t nth = there + __builtin_popcountll(any & (2ull << lane) - 1);   // of those with any
+        const uint64_t past = __ballot(whole ? nth * per_request > blockIdx.x : upto * per_request > from);
         if (past != 0) {
             const uint32_t at = __builtin_ctzll(past);
             request = b0 + at;
             before = __builtin_amdgcn_readlane(upto - tiles, at) * per_request;
+            if (whole) {
+                const uint32_t its = __builtin_amdgcn_readlane(tiles, at), n = __builtin_amdgcn_readlane(nth, at) - 1;
+                from = before + (blockIdx.x - n * per_request) * its;
+                to = from + its;
+            }
             break;
         }
         sum = __builtin_amdgcn_readlane(upto, 63);
+        there += __builtin_popcountll(any);
     }
     request = __builtin_amdgcn_readfirstlane(request);
     before = __builtin_amdgcn_readfirstlane(before);
+    from = __builtin_amdgcn_readfirstlane(from);
+    to = __builtin_amdgcn_readfirstlane(to);
 
     // the segment that begins at a tile
     auto segment_at = [&](uint32_t at, uint32_t request, uint32_t before) {
@@ -526,7 +544,11 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
         };
 
         const uint32_t item_from = now.before + now.item * now.tiles, item_to = item_from + now.tiles;
-        const uint32_t first_part = owner_of(item_from), parts = owner_of(item_to - 1) - first_part + 1;
+        uint32_t first_part = blockIdx.x, parts = 1;
+        if (item_from < from || item_to > to) {
+            first_part = owner_of(item_from);
+            parts = owner_of(item_to - 1) - first_part + 1;
+        }
         constexpr uint32_t kQuads = kDim / 4;
         const uint32_t rows_kept = a.group < 16 ? a.group : 16;
         const size_t part_floats = (size_t)rows_kept * (kDim + 2);   // sums, then tops and totals
