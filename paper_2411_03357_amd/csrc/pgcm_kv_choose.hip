@@ -6,7 +6,10 @@ namespace pgcm_kv_impl {
 namespace {
 
 constexpr uint32_t kMostThreads = 1024;
-constexpr uint32_t kHeld = 16;        // keys that a lane holds in registers; longer rows are read from memory at each look
+// Keys that a lane holds in registers, kHeld; rows that are too long for kMostHeld are read from memory at each look.  All loops
+// over them are laid out in full, so that of a kernel with room for more keys than the row has much code is fetched and passed
+// over: 256 rows of up to 8192 keys take 11.5 us with room for 8 keys a lane, 13.0 with room for 16.
+constexpr uint32_t kFewHeld = 2, kSomeHeld = 8, kMostHeld = 16;
 constexpr uint32_t kBinBits = 10, kBins = 1u << kBinBits;
 constexpr uint32_t kNever = 0, kAlways = 0xFFFFFFFFu;  // keys of what cannot be chosen, and of what is chosen before all others
 
@@ -26,7 +29,7 @@ struct Part {
         first = threadIdx.x / 64 * 64 * steps + threadIdx.x % 64;
     }
 };
-template <uint32_t kThreads>
+template <uint32_t kThreads, uint32_t kHeld>
 struct HeldKeys {
     Part<kThreads> part;
     uint32_t key[kHeld];
@@ -179,7 +182,7 @@ struct EvictArgs {
 
 // A row a workgroup: the least weights are the largest of what ~ makes of them.  One row of 128 blocks 5.2 us, the launch and
 // its steps one after the other; 256 rows of up to 8192 blocks, 64 leaving (9 MB): 12.9 us, a compute unit each.
-template <uint32_t kThreads>
+template <uint32_t kThreads, uint32_t kHeld>
 __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     __shared__ ChooseShared shared;
     const uint32_t request = blockIdx.x;
@@ -212,9 +215,9 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
             if (victim_blocks != nullptr) victim_blocks[i] = -1;
         }
     };
-    if (HeldKeys<kThreads>::holds(a.row_blocks)) {
+    if (HeldKeys<kThreads, kHeld>::holds(a.row_blocks)) {
         // (parts of the whole row, so that its copy takes no look of its own; all loads are under way together)
-        HeldKeys<kThreads> keys(a.row_blocks);
+        HeldKeys<kThreads, kHeld> keys(a.row_blocks);
         int32_t block[kHeld];
         float w[kHeld];
 #pragma unroll
@@ -428,12 +431,13 @@ __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void score_ker
 }
 
 // ... and chosen from: 256 rows of up to 2048 keys 7.2 us, 8 of 8192 9.0.
+template <uint32_t kHeld>
 __global__ __launch_bounds__(kMostThreads) void choose_kernel(SelectArgs a) {
     __shared__ ChooseShared shared;
     const uint32_t list = blockIdx.x, blocks = blocks_of(a, list / a.kv_heads);
     const uint32_t* row_keys = a.keys + (size_t)list * a.row_blocks;
-    if (HeldKeys<kMostThreads>::holds(blocks)) {
-        HeldKeys<kMostThreads> keys(blocks);
+    if (HeldKeys<kMostThreads, kHeld>::holds(blocks)) {
+        HeldKeys<kMostThreads, kHeld> keys(blocks);
 #pragma unroll
         for (uint32_t s = 0; s < kHeld; ++s) {
             const uint32_t j = keys.part.first + 64 * s;
@@ -447,16 +451,16 @@ __global__ __launch_bounds__(kMostThreads) void choose_kernel(SelectArgs a) {
 }
 
 // Short rows, a workgroup each, whose keys stay in LDS: 8 lists of 100 blocks 8.4 us.
-template <class H, uint32_t kChunks>
+template <class H, uint32_t kChunks, uint32_t kHeld>
 __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void select_kernel(SelectArgs a) {
     __shared__ ChooseShared shared;
-    __shared__ uint32_t row_keys[kWholeBlocks];
+    __shared__ uint32_t row_keys[kScoreThreads * kHeld];
     __shared__ __align__(16) int8_t q8[16][64 * kChunks + 16];
     __shared__ float q_scale[16];
     const uint32_t list = blockIdx.x, request = list / a.kv_heads, blocks = blocks_of(a, request);
     score<H, kChunks, kMostSteps>(a, request, list % a.kv_heads, 0, blocks, blocks, q8, q_scale, [&](uint32_t j) { return row_keys + j; });
     __syncthreads();
-    HeldKeys<kScoreThreads> keys(blocks);
+    HeldKeys<kScoreThreads, kHeld> keys(blocks);
 #pragma unroll
     for (uint32_t s = 0; s < kHeld; ++s) {
         const uint32_t j = keys.part.first + 64 * s;
@@ -474,14 +478,21 @@ void launch_score(SelectArgs& a, hipStream_t stream) {
 template <class H, uint32_t kChunks>
 void launch(SelectArgs& a, hipStream_t stream) {
     const uint32_t lists = a.requests * a.kv_heads;
-    if (a.row_blocks <= kShortBlocks || (a.row_blocks <= kWholeBlocks && lists >= kListsToFill)) {
-        select_kernel<H, kChunks><<<lists, kScoreThreads, 0, stream>>>(a);
+    static_assert(kShortBlocks <= kScoreThreads * kFewHeld && kWholeBlocks <= kScoreThreads * kSomeHeld, "rows fit");
+    if (a.row_blocks <= kShortBlocks) {
+        select_kernel<H, kChunks, kFewHeld><<<lists, kScoreThreads, 0, stream>>>(a);
+        return;
+    }
+    if (a.row_blocks <= kWholeBlocks && lists >= kListsToFill) {
+        select_kernel<H, kChunks, kSomeHeld><<<lists, kScoreThreads, 0, stream>>>(a);
         return;
     }
     const uint64_t parts = (uint64_t)lists * ((a.row_blocks + part_blocks(kMostSteps) - 1) / part_blocks(kMostSteps));
     if (parts > kFewParts) launch_score<H, kChunks, kMostSteps>(a, stream);
     else launch_score<H, kChunks, 1>(a, stream);
-    choose_kernel<<<lists, kMostThreads, 0, stream>>>(a);
+    if (a.row_blocks <= kMostThreads * kFewHeld) choose_kernel<kFewHeld><<<lists, kMostThreads, 0, stream>>>(a);
+    else if (a.row_blocks <= kMostThreads * kSomeHeld) choose_kernel<kSomeHeld><<<lists, kMostThreads, 0, stream>>>(a);
+    else choose_kernel<kMostHeld><<<lists, kMostThreads, 0, stream>>>(a);
 }
 template <class H>
 void launch(SelectArgs& a, hipStream_t stream) {
@@ -545,8 +556,12 @@ int pgcm_kv_evict(const pgcm_kv_evict_args* args, void* hip_stream) {
     a.row_blocks = args->row_blocks, a.block_tokens = args->block_tokens, a.blocks = args->blocks;
     a.most = args->most, a.first = args->first, a.last = args->last;
     // four wavefronts a row, or sixteen for longer ones (8 rows of 2000 blocks: 7.7 us and 8.2; of 4000 9.3 and 9.1)
-    if (a.row_blocks <= 2048) evict_kernel<256><<<args->requests, 256, 0, (hipStream_t)hip_stream>>>(a);
-    else evict_kernel<kMostThreads><<<args->requests, kMostThreads, 0, (hipStream_t)hip_stream>>>(a);
+    constexpr uint32_t kFew = 256;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (a.row_blocks <= kFew * kFewHeld) evict_kernel<kFew, kFewHeld><<<args->requests, kFew, 0, stream>>>(a);
+    else if (a.row_blocks <= kFew * kSomeHeld) evict_kernel<kFew, kSomeHeld><<<args->requests, kFew, 0, stream>>>(a);
+    else if (a.row_blocks <= kMostThreads * kSomeHeld) evict_kernel<kMostThreads, kSomeHeld><<<args->requests, kMostThreads, 0, stream>>>(a);
+    else evict_kernel<kMostThreads, kMostHeld><<<args->requests, kMostThreads, 0, stream>>>(a);
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 
