@@ -9,6 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpgcm.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
+KV_MARSHAL = os.path.join(HERE, "_kv_marshal.so")    # a torch extension; the rest does without torch
 SOURCES = ["pgcm_kernels.hip", "pgcm_bitsliced.hip", "pgcm_host.hip", "pgcm_bounce.hip", "pgcm_pipe.hip",
            "pgcm_seq.cpp", "pgcm_kv.hip", "pgcm_kv_attend.hip", "pgcm_kv_cache.hip", "pgcm_kv_choose.hip"]
 HEADERS = ["pgcm_kernels.h", "pgcm_types.h", "pgcm_arrive.h", "pgcm_contexts.h", "pgcm_one_launch.h",
@@ -40,26 +41,36 @@ def hipcc() -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(MARSHAL):
+    built = (LIB, MARSHAL, KV_MARSHAL)
+    if not all(os.path.exists(b) for b in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(MARSHAL))
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["marshal.cpp"]] + \
+    t = min(os.path.getmtime(b) for b in built)
+    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["marshal.cpp", "kv_marshal.cpp"]] + \
         [os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
-def build_marshal() -> None:
+def _host_build(source, target, *more) -> None:
     cxx = shutil.which("g++") or shutil.which("c++")
     if cxx is None:
         raise RuntimeError("no host C++ compiler")
-    tmp = MARSHAL + ".tmp%d" % os.getpid()
+    tmp = target + ".tmp%d" % os.getpid()
     proc = subprocess.run([cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                            "-Wall", "-I" + sysconfig.get_paths()["include"],
-                           os.path.join(CSRC, "marshal.cpp"), "-o", tmp],
+                           os.path.join(CSRC, source), "-o", tmp, *more],
                           stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if proc.returncode != 0:
-        raise RuntimeError("compiling marshal.cpp failed:\n" + proc.stdout)
-    os.replace(tmp, MARSHAL)
+        raise RuntimeError("compiling %s failed:\n%s" % (source, proc.stdout))
+    os.replace(tmp, target)
+
+
+def build_marshal() -> None:
+    _host_build("marshal.cpp", MARSHAL)
+    import torch
+    at = os.path.dirname(torch.__file__)
+    _host_build("kv_marshal.cpp", KV_MARSHAL, "-isystem", os.path.join(at, "include"),
+                "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(), "-L" + os.path.join(at, "lib"),
+                "-ltorch_python", "-ltorch_cpu", "-lc10")
 
 
 def build(force: bool = True, verbose: bool = False) -> str:

@@ -48,7 +48,7 @@ class _Evict(C.Structure):
 
 
 _bound = None
-_marshal = None     # native marshalling (csrc/marshal.cpp), bound to _bound
+_marshal = None     # native marshalling (csrc/kv_marshal.cpp), bound to _bound
 
 
 def _lib():
@@ -67,10 +67,9 @@ def _lib():
         for name in KV_EXPORTS:
             if name != "pgcm_kv_destroy":
                 getattr(lib, name).restype = C.c_int
-        from . import _marshal as m
-        m.kv_bind(*[C.cast(getattr(lib, "pgcm_kv_" + n), _vp).value
-                    for n in ("append", "attend", "summarize", "select", "evict")],
-                  torch.float16, torch.bfloat16, torch.int8, torch.int32, torch.int64, torch.float32)
+        from . import _kv_marshal as m
+        m.bind(*[C.cast(getattr(lib, "pgcm_kv_" + n), _vp).value
+                 for n in ("append", "attend", "summarize", "select", "evict")])
         global _marshal
         _marshal = m
         _bound = lib
