@@ -1,6 +1,6 @@
 // Native marshalling of the operators on KV blocks (kv.py): a torch extension, as what a tensor is takes five calls of the
-// interpreter to ask it and some nanoseconds to read (an append of nine tensors: 6.1 us of the host and 4.0).  Each call gives the status,
-// or None for anything unusual, which the Python code then names.
+// interpreter to ask it and some nanoseconds to read (an append of nine tensors: 6.1 us of the host and 4.0).  Each call gives
+// the status, or None for anything unusual, which the Python code then names.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>

@@ -50,7 +50,7 @@ __device__ __forceinline__ float over_lanes(float x, uint32_t power, Of of) {
 //   x by w c + y by w' s        (by: of the norm; y, w': the other channel of the pair and its weight; s with its sign)
 // are made once for a token, and a head takes five operations a channel.  What they take is asked for before anything is
 // waited for, the table's line in pieces of sixteen bytes (word by word, a batch of 300 tokens took twice as long).  8191
-// tokens, 40 heads and kv heads of 128 (508 MB): 104 us, 4.9 TB/s, the rate of a large copy; 64 tokens of 32 and 8: 4.7 us, the
+// tokens, 40 heads and kv heads of 128 (508 MB): 104 us, 4.9 TB/s, the rate of a large copy; 64 tokens of 32 and 8: 3.8 us, the
 // launch and two loads one after the other.
 template <class H>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {

@@ -76,7 +76,7 @@ __device__ __forceinline__ uint32_t of_waves_before(const uint32_t* figures) {
 
 // The `want` largest keys.  All threads call it.  Keys are whole numbers, so that counts say exactly where the last one chosen
 // lies, and no order of threads shows.  What bounds it are looks at the keys, each with its counts in LDS and a barrier: 256 rows
-// of up to 8192, 64 chosen, 13.1 us with keys in registers, 18.5 with keys read from memory at each look.
+// of up to 8192, 64 chosen, 11.3 us with keys in registers, 18 with keys read from memory at each look.
 template <uint32_t kThreads, class Keys>
 __device__ __forceinline__ Chosen choose(const Keys& keys, uint32_t want, ChooseShared& shared) {
     constexpr uint32_t kWaves = kThreads / 64;
@@ -180,8 +180,8 @@ struct EvictArgs {
     uint32_t row_blocks, block_tokens, blocks, most, first, last;
 };
 
-// A row a workgroup: the least weights are the largest of what ~ makes of them.  One row of 128 blocks 5.2 us, the launch and
-// its steps one after the other; 256 rows of up to 8192 blocks, 64 leaving (9 MB): 12.9 us, a compute unit each.
+// A row a workgroup: the least weights are the largest of what ~ makes of them.  One row of 128 blocks 3.2 us, the launch and
+// its steps one after the other; 256 rows of up to 8192 blocks, 64 leaving (9 MB): 11.3 us, a compute unit each.
 template <uint32_t kThreads, uint32_t kHeld>
 __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     __shared__ ChooseShared shared;
@@ -283,9 +283,9 @@ constexpr uint32_t kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
 constexpr uint32_t kMostSteps = 4, kFewParts = 128;
 __host__ __device__ constexpr uint32_t part_blocks(uint32_t steps) { return kScoreWaves * 16 * steps; }
 // Rows scored and chosen from in one launch, a workgroup each: of up to kShortBlocks (one request with 8 lists: of 100 blocks
-// 8.4 us, of 500 11.7, in two launches 11.2 and 12.6), and of up to kWholeBlocks where there are lists for all compute units
-// (of 1000 blocks: 32 requests 21.4 us and 22.9, one 16.1 and 13.1).
-constexpr uint32_t kShortBlocks = 512, kWholeBlocks = 1024, kListsToFill = 256;
+// 7.3 us, of 250 8.3, of 500 10.7, in two launches 9.9, 10.2 and 10.2), and of up to kWholeBlocks where there are lists for all
+// compute units (of 1000 blocks: 32 requests 21.0 us and 22.1, one 15.2 and 10.4).
+constexpr uint32_t kShortBlocks = 384, kWholeBlocks = 1024, kListsToFill = 256;
 
 // Keys of the blocks [from, to) of a request for one kv head, at key_of(j).  The scores are products on the matrix cores,
 // of 2 head_dim whole numbers: for each of sixteen query heads, its negative channels (for the least values) and its
@@ -412,7 +412,7 @@ __device__ __forceinline__ void score(const SelectArgs& a, uint32_t request, uin
 }
 
 // Rows of any length, part by part.  What bounds it is memory: 32 requests of up to 2048 blocks, 8 kv heads of 128 (45 MB) take
-// 14.5 us, 3.1 TB/s, some 4 of them the launch's; 1 of 8192 (17 MB) 9.0.  The heads of a part, whose entries and scales share
+// 14.9 us, 3.0 TB/s, some 4 of them the launch's; 1 of 8192 (17 MB) 8.6.  The heads of a part, whose entries and scales share
 // lines, run on one XCD; parts go to the XCDs in turn.
 template <class H, uint32_t kChunks, uint32_t kSteps>
 __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void score_kernel(SelectArgs a) {
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void score_ker
     score<H, kChunks, kSteps>(a, request, head, from, to, blocks, q8, q_scale, [&](uint32_t j) { return keys + j; });
 }
 
-// ... and chosen from: 256 rows of up to 2048 keys 7.2 us, 8 of 8192 9.0.
+// ... and chosen from: 256 rows of up to 2048 keys 6.0 us, 8 of 8192 8.5.
 template <uint32_t kHeld>
 __global__ __launch_bounds__(kMostThreads) void choose_kernel(SelectArgs a) {
     __shared__ ChooseShared shared;
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(kMostThreads) void choose_kernel(SelectArgs a) {
     }
 }
 
-// Short rows, a workgroup each, whose keys stay in LDS: 8 lists of 100 blocks 8.4 us.
+// Short rows, a workgroup each, whose keys stay in LDS: 8 lists of 100 blocks 7.3 us, 256 of 500 14.5.
 template <class H, uint32_t kChunks, uint32_t kHeld>
 __global__ __launch_bounds__(kScoreThreads, kChunks == 8 ? 2 : 4) void select_kernel(SelectArgs a) {
     __shared__ ChooseShared shared;
