@@ -5,7 +5,7 @@
 // with running m and sums, one pass over K and V.  What bounds it is memory: at sixteen heads an item, 16 flops a byte.
 // Two requests of 131 059 tokens, 8 kv heads of 128 (1.07 GB): 201 us, 5.3 TB/s, each byte read once; a kernel that only reads
 // the same rows takes 192 to 206.  32 of up to 2048 tokens, 40 heads of 128 (396 MB): 86 us, 4.6 TB/s.  One of 33 tokens, 40
-// heads: 6.5 us, the launch and trips to memory one after the other (lengths, tables, rows).
+// heads: 4.5 us, the launch and trips to memory one after the other (table, rows).
 //
 // The tiles of all items, 128 tokens each, are cut into equal spans, one for each workgroup, so that neither lengths nor their
 // number matter (short items are left whole); an item of several workgroups is joined by the last of them, in two levels if they
@@ -293,6 +293,7 @@ struct Pieces {
     uint32_t block;          // number; anything out of the pool, e.g. ~0: masked
     uint32_t inside, valid;  // token of the block; how many of its sixteen are there
 };
+template <bool kShort>
 __device__ __forceinline__ Pieces find_pieces(const AttendArgs& a, const Segment& s, uint32_t wave, uint32_t lane) {
     Pieces p{~0u, 0u, 0u};
     const uint32_t t = s.tile + lane / 2;
@@ -306,16 +307,20 @@ __device__ __forceinline__ Pieces find_pieces(const AttendArgs& a, const Segment
         place = (uint32_t)a.selected[((size_t)s.request * a.kv_heads + s.item / a.group_tiles) * a.keep + place];
     }
     if (place >= a.row_blocks) return p;
+    uint32_t block = 0;
+    if constexpr (kShort) block = (uint32_t)a.tables[s.request * a.table_row + place];   // on its way with the length
     const uint32_t len = clamped_len(a, len_of(a, s.request));
     const uint64_t token = (uint64_t)place * a.block_tokens + inside;
     if (token >= len) return p;
     p.valid = len - token < kPiece ? (uint32_t)(len - token) : kPiece;
     p.inside = inside;
-    p.block = (uint32_t)a.tables[s.request * a.table_row + place];   // (looked at when it is used)
+    if constexpr (!kShort) block = (uint32_t)a.tables[s.request * a.table_row + place];
+    p.block = block;   // (looked at when it is used)
     return p;
 }
 
-template <class H, uint32_t kDim, bool kExact>
+// kShort: a workgroup for each item of all requests, also of those without tokens, whose rows have room for at most 32 tiles.
+template <class H, uint32_t kDim, bool kExact, bool kShort>
 __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
     typedef Walk<H, kDim, kExact> W;
     __shared__ AttendShared<kDim> shared;
@@ -324,72 +329,79 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     const uint32_t per_request = a.kv_heads * a.group_tiles;
 
     // The tiles of all items
-    uint32_t some = 0, all = 0, longest = 0, tiles = 0;   // requests with any; all tiles; of a request; of request `lane`, or of the last 64
-    for (uint32_t b0 = 0; b0 < a.requests; b0 += 64) {
-        const uint32_t b = b0 + lane;
-        tiles = b < a.requests ? tiles_of(a, b) : 0;
-        all += __builtin_amdgcn_readlane(scan(tiles), 63);
-        some += __builtin_popcountll(__ballot(tiles != 0));
-        longest = tiles > longest ? tiles : longest;
-        // requests without tokens are answered here
-        uint64_t empty = __ballot(b < a.requests && tiles == 0 && b % gridDim.x == blockIdx.x);
-        for (; empty != 0; empty &= empty - 1) {
-            const uint32_t e = b0 + __builtin_ctzll(empty), heads = a.kv_heads * a.group;
-            for (uint32_t x = threadIdx.x; x < heads * a.head_dim; x += kThreads)
-                *(uint16_t*)(a.out + e * a.out_request + x / a.head_dim * a.out_head + 2 * (x % a.head_dim)) = 0;
-            for (uint32_t h = threadIdx.x; h < heads; h += kThreads) {
-                if (a.lse != nullptr) a.lse[(size_t)e * heads + h] = -INFINITY;
-                if (a.piece_lse != nullptr) a.head_lse[(size_t)e * heads + h] = -INFINITY;
+    // requests with any; all tiles; the most of a request; those of request `lane`, or of the last 64
+    uint32_t some = 0, all = 0, longest = 0, tiles = 0;
+    uint32_t groups = 1;
+    bool whole = false;
+    if constexpr (!kShort) {
+        for (uint32_t b0 = 0; b0 < a.requests; b0 += 64) {
+            const uint32_t b = b0 + lane;
+            tiles = b < a.requests ? tiles_of(a, b) : 0;
+            all += __builtin_amdgcn_readlane(scan(tiles), 63);
+            some += __builtin_popcountll(__ballot(tiles != 0));
+            longest = tiles > longest ? tiles : longest;
+            // requests without tokens are answered here
+            uint64_t empty = __ballot(b < a.requests && tiles == 0 && b % gridDim.x == blockIdx.x);
+            for (; empty != 0; empty &= empty - 1) {
+                const uint32_t e = b0 + __builtin_ctzll(empty), heads = a.kv_heads * a.group;
+                for (uint32_t x = threadIdx.x; x < heads * a.head_dim; x += kThreads)
+                    *(uint16_t*)(a.out + e * a.out_request + x / a.head_dim * a.out_head + 2 * (x % a.head_dim)) = 0;
+                for (uint32_t h = threadIdx.x; h < heads; h += kThreads) {
+                    if (a.lse != nullptr) a.lse[(size_t)e * heads + h] = -INFINITY;
+                    if (a.piece_lse != nullptr) a.head_lse[(size_t)e * heads + h] = -INFINITY;
+                }
             }
         }
+        all *= per_request;
+        some *= per_request;
+        if (all == 0) return;
+        longest = over_wave(longest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        whole = longest <= (some >= kManyItems ? kWholeTilesOfMany : kWholeTiles) && some <= gridDim.x;
+        // ... in the order of requests and heads, are cut into equal spans (of one tile more or less), or at the items' ends: this
+        // workgroup's is [from, to).
+        const uint32_t by_tiles = all / some <= kShortItem ? all : (all + 1) / 2, useful = by_tiles > some ? by_tiles : some;
+        // (of 256 channels, two workgroups have no room on a compute unit)
+        const bool alone = kDim == 256 || (all / some >= kLongItem && all >= kManyTiles * kCus);
+        groups = alone && gridDim.x > kCus ? kCus : gridDim.x;
+        if (groups > useful) groups = useful;
+        if (whole) groups = some;
+        if (blockIdx.x >= groups) return;
     }
-    all *= per_request;
-    some *= per_request;
-    if (all == 0) return;
-    longest = over_wave(longest, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-    const bool whole = longest <= (some >= kManyItems ? kWholeTilesOfMany : kWholeTiles) && some <= gridDim.x;
-    // ... in the order of requests and heads, are cut into equal spans (of one tile more or less), or at the items' ends: this
-    // workgroup's is [from, to).
-    const uint32_t by_tiles = all / some <= kShortItem ? all : (all + 1) / 2, useful = by_tiles > some ? by_tiles : some;
-    const bool alone = kDim == 256 || (all / some >= kLongItem && all >= kManyTiles * kCus);   // (of 256 channels, two have no room)
-    uint32_t groups = alone && gridDim.x > kCus ? kCus : gridDim.x;
-    if (groups > useful) groups = useful;
-    if (whole) groups = some;
-    if (blockIdx.x >= groups) return;
     const uint32_t share = all / groups, longer = all - share * groups;   // the first `longer` spans have one tile more
     auto start_of = [&](uint32_t w) { return w * share + (w < longer ? w : longer); };
     auto owner_of = [&](uint32_t tile) {
-        const uint32_t in_longer = longer * (share + 1), x = tile - longer;   // (of the others: less what the longer ones have more)
+        const uint32_t in_longer = longer * (share + 1), x = tile - longer;   // (x: less what the longer ones have more)
         return tile < in_longer ? tile / (share + 1) : x / share;
     };
     uint32_t from = start_of(blockIdx.x), to = start_of(blockIdx.x + 1);
-
-    // the request that the span begins in, and its first tile
     uint32_t request = 0, before = 0;
-    for (uint32_t b0 = 0, sum = 0, there = 0; b0 < a.requests; b0 += 64) {
-        if (a.requests > 64) tiles = b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
-        const uint32_t upto = sum + scan(tiles);
-        const uint64_t any = __ballot(tiles != 0);
-        const uint32_t nth = there + __builtin_popcountll(any & (2ull << lane) - 1);   // of those with any
-        const uint64_t past = __ballot(whole ? nth * per_request > blockIdx.x : upto * per_request > from);
-        if (past != 0) {
-            const uint32_t at = __builtin_ctzll(past);
-            request = b0 + at;
-            before = __builtin_amdgcn_readlane(upto - tiles, at) * per_request;
-            if (whole) {
-                const uint32_t its = __builtin_amdgcn_readlane(tiles, at), n = __builtin_amdgcn_readlane(nth, at) - 1;
-                from = before + (blockIdx.x - n * per_request) * its;
-                to = from + its;
+    if constexpr (!kShort) {
+        // the request that the span begins in, and its first tile
+        for (uint32_t b0 = 0, sum = 0, there = 0; b0 < a.requests; b0 += 64) {
+            if (a.requests > 64) tiles = b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
+            const uint32_t upto = sum + scan(tiles);
+            const uint64_t any = __ballot(tiles != 0);
+            const uint32_t nth = there + __builtin_popcountll(any & (2ull << lane) - 1);   // of those with any
+            const uint64_t past = __ballot(whole ? nth * per_request > blockIdx.x : upto * per_request > from);
+            if (past != 0) {
+                const uint32_t at = __builtin_ctzll(past);
+                request = b0 + at;
+                before = __builtin_amdgcn_readlane(upto - tiles, at) * per_request;
+                if (whole) {
+                    const uint32_t its = __builtin_amdgcn_readlane(tiles, at), n = __builtin_amdgcn_readlane(nth, at) - 1;
+                    from = before + (blockIdx.x - n * per_request) * its;
+                    to = from + its;
+                }
+                break;
             }
-            break;
+            sum = __builtin_amdgcn_readlane(upto, 63);
+            there += __builtin_popcountll(any);
         }
-        sum = __builtin_amdgcn_readlane(upto, 63);
-        there += __builtin_popcountll(any);
+        request = __builtin_amdgcn_readfirstlane(request);
+        before = __builtin_amdgcn_readfirstlane(before);
+        from = __builtin_amdgcn_readfirstlane(from);
+        to = __builtin_amdgcn_readfirstlane(to);
     }
-    request = __builtin_amdgcn_readfirstlane(request);
-    before = __builtin_amdgcn_readfirstlane(before);
-    from = __builtin_amdgcn_readfirstlane(from);
-    to = __builtin_amdgcn_readfirstlane(to);
 
     // the segment that begins at a tile
     auto segment_at = [&](uint32_t at, uint32_t request, uint32_t before) {
@@ -452,20 +464,27 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
     };
 
     uint32_t at = from;
-    Segment now = segment_at(at, request, before);
-    use_pieces(find_pieces(a, now, wave, lane), now);
+    Segment now;
+    if constexpr (kShort) {
+        const uint32_t most = ((a.selected == nullptr ? a.row_blocks : a.keep) * a.block_tokens + kTileTokens - 1) / kTileTokens;
+        request = blockIdx.x / per_request;
+        now = Segment{request, 0, most, blockIdx.x - request * per_request, 0, most};
+    } else {
+        now = segment_at(at, request, before);
+    }
+    use_pieces(find_pieces<kShort>(a, now, wave, lane), now);
     bool some_left = seek();
     walk.clear();
     load_query(now);
     if (some_left) ask();
     while (true) {
         at += now.tile_to - now.tile;
-        const bool more = at < to;
+        const bool more = !kShort && at < to;
         Segment next = now;
         Pieces next_pieces{~0u, 0u, 0u};
         if (more) {         // where the next segment's pieces lie is asked for while this one is walked over
             next = segment_at(at, now.request, now.before);
-            next_pieces = find_pieces(a, next, wave, lane);
+            next_pieces = find_pieces<kShort>(a, next, wave, lane);
         }
         const uint32_t head0 = now.item % a.group_tiles * 16, first_head = now.item / a.group_tiles * a.group + head0;
         const uint32_t heads = a.group - head0 < 16 ? a.group - head0 : 16;
@@ -545,7 +564,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
 
         const uint32_t item_from = now.before + now.item * now.tiles, item_to = item_from + now.tiles;
         uint32_t first_part = blockIdx.x, parts = 1;
-        if (item_from < from || item_to > to) {
+        if (!kShort && (item_from < from || item_to > to)) {
             first_part = owner_of(item_from);
             parts = owner_of(item_to - 1) - first_part + 1;
         }
@@ -713,15 +732,20 @@ __global__ __launch_bounds__(kThreads) void weights_kernel(AttendArgs a, const f
     }
 }
 
-template <class H>
+template <class H, bool kShort>
 void launch(const AttendArgs& a, uint32_t groups, hipStream_t stream) {
     const uint32_t d = a.head_dim;
-    if (d == 64) attend_kernel<H, 64, true><<<groups, kThreads, 0, stream>>>(a);
-    else if (d < 64) attend_kernel<H, 64, false><<<groups, kThreads, 0, stream>>>(a);
-    else if (d == 128) attend_kernel<H, 128, true><<<groups, kThreads, 0, stream>>>(a);
-    else if (d < 128) attend_kernel<H, 128, false><<<groups, kThreads, 0, stream>>>(a);
-    else if (d == 256) attend_kernel<H, 256, true><<<groups, kThreads, 0, stream>>>(a);
-    else attend_kernel<H, 256, false><<<groups, kThreads, 0, stream>>>(a);
+    if (d == 64) attend_kernel<H, 64, true, kShort><<<groups, kThreads, 0, stream>>>(a);
+    else if (d < 64) attend_kernel<H, 64, false, kShort><<<groups, kThreads, 0, stream>>>(a);
+    else if (d == 128) attend_kernel<H, 128, true, kShort><<<groups, kThreads, 0, stream>>>(a);
+    else if (d < 128) attend_kernel<H, 128, false, kShort><<<groups, kThreads, 0, stream>>>(a);
+    else if (d == 256) attend_kernel<H, 256, true, kShort><<<groups, kThreads, 0, stream>>>(a);
+    else attend_kernel<H, 256, false, kShort><<<groups, kThreads, 0, stream>>>(a);
+}
+template <class H>
+void launch(const AttendArgs& a, uint32_t groups, bool by_item, hipStream_t stream) {
+    if (by_item) launch<H, true>(a, groups, stream);
+    else launch<H, false>(a, groups, stream);
 }
 
 }  // namespace
@@ -782,9 +806,15 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     const uint64_t tiles = (walk_blocks * cache->block_tokens + kTileTokens - 1) / kTileTokens;
     const uint64_t items = (uint64_t)a.requests * a.kv_heads * a.group_tiles, most = tiles * items;
     const uint64_t useful = most > items ? most : items;
-    const uint32_t groups = useful > kAttendGroups ? kAttendGroups : (uint32_t)useful;
-    if (cache->half == PGCM_KV_F16) launch<F16>(a, groups, stream);
-    else launch<Bf16>(a, groups, stream);
+    // Tables with room for few tiles only: a workgroup for each item, which looks at no lengths but its own request's and cuts and
+    // joins nothing (one request of 33 tokens, 40 heads: 4.3 us and 6.4; 8 items of 6 tiles 8.7 and 9.6, of 8 tiles 10.0 and 9.6;
+    // 126 of up to 12 tiles 15.7 and 22.1, 1016 of 64 channels 39.0 and 42.0; 128 of 16 tiles 30.9 and 32.0, 256 of up to 16 of 256
+    // channels 52.9 and 50.8, 1280 of 128 channels 92.8 and 91.0).
+    const bool by_item = items < 1 << 24 &&   // (threads of a grid are counted in 32 bits)
+                         tiles <= (items < kManyItems ? 6u : items <= kCus / 2 ? 16u : 12u);
+    const uint32_t groups = by_item ? (uint32_t)items : useful > kAttendGroups ? kAttendGroups : (uint32_t)useful;
+    if (cache->half == PGCM_KV_F16) launch<F16>(a, groups, by_item, stream);
+    else launch<Bf16>(a, groups, by_item, stream);
     if (hip_noted(hipGetLastError())) return PGCM_ERR_HIP;
     if (weigh && args->row_blocks != 0) {
         weights_kernel<<<dim3((args->row_blocks + 63) / 64, args->requests), kThreads, 0, stream>>>(a, args->kept, args->weights,

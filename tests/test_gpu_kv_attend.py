@@ -1,5 +1,6 @@
 """pgcm_kv_attend against its definition in 64 bits: lengths from none to several tiles of several workgroups, blocks that
 are not there, whatever the pool holds elsewhere, orders of memory, groups of heads, selections, weights, graphs, streams."""
+import copy
 import math
 
 import numpy as np
@@ -29,6 +30,19 @@ def _run(r, q, scale=None, selected=None, kept=None, decay=1.0, weigh=False, **m
 
 
 def _check(r, q, scale=None, selected=None, kept=None, decay=1.0, weigh=False, **more):
+    """... and again with room for more tokens in the tables, which is worked on in another way"""
+    _check_once(r, q, scale, selected, kept, decay, weigh, **more)
+    wide = copy.copy(r)
+    wide.most += -(-2200 // r.block)
+    wide.tables = np.pad(r.tables, ((0, 0), (0, wide.most - r.most)), constant_values=-1)
+    if selected is not None:
+        selected = np.pad(selected, ((0, 0), (0, 0), (0, wide.most - r.most)), constant_values=-1)
+    if kept is not None:
+        kept = torch.nn.functional.pad(kept, (0, wide.most - r.most))
+    _check_once(wide, q, scale, selected, kept, decay, weigh, **more)
+
+
+def _check_once(r, q, scale, selected, kept, decay, weigh, **more):
     out, lse, weights = _run(r, q, scale, selected, kept, decay, weigh, **more)
     want = ref.attend(r, q, r.dim ** -0.5 if scale is None else scale, selected, kept, decay)
     ref.within(out, want[0], "out")
