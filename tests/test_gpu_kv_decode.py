@@ -77,3 +77,70 @@ def test_the_example_runs():
                          stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True, timeout=100)
     assert out.returncode == 0, out.stderr[-1500:]
     assert "all authentic" in out.stdout
+
+
+def test_a_step_captured_into_a_graph():
+    """all operators of a decode step in one graph, replayed with other inputs, lengths and tables, against the same calls
+    outside of it"""
+    import paper_2411_03357_amd as pgcm
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    n, kv, heads, dim, block, row = 2, 2, 8, 64, 16, 1300
+    half = torch.bfloat16
+    pool = torch.randn(n * row, 2, block, kv, dim, device="cuda", generator=gen).to(half)
+    cache = pgcm.KVCache(pool[:, 0], pool[:, 1])
+    tables = torch.arange(n * row, dtype=torch.int32, device="cuda").view(n, row)
+    blocks = tables.flatten().contiguous()
+    bounds = torch.zeros(n * row, kv, 2, dim, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(n * row, kv, device="cuda")
+    pgcm.kv_summarize(cache, blocks, torch.full_like(blocks, block), bounds, scales)
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    slots = torch.zeros(n, dtype=torch.int64, device="cuda")
+    positions, last, counts = torch.zeros_like(lens), torch.zeros_like(lens), torch.zeros_like(lens)
+    packed = torch.zeros(n, heads + 2 * kv, dim, dtype=half, device="cuda")
+    rope = torch.randn(32768, dim, device="cuda", generator=gen)
+    weights = torch.zeros(n, row, device="cuda")
+    q = torch.zeros(n, heads, dim, dtype=half, device="cuda")
+    out, sparse = torch.zeros_like(q), torch.zeros_like(q)
+    selected = torch.zeros(n, kv, 20, dtype=torch.int32, device="cuda")
+    evict = torch.tensor([3, 1], dtype=torch.int32, device="cuda")
+    victims = torch.zeros(n, 4, dtype=torch.int32, device="cuda")
+    space = pgcm.KVWorkspace()
+    space.reserve(n, heads, kv, dim, block, row)
+
+    def step():
+        pgcm.kv_append(cache, packed[:, :heads], packed[:, heads:heads + kv], packed[:, heads + kv:], positions, slots, q,
+                       rope=rope)
+        pgcm.kv_summarize(cache, last, counts, bounds, scales)
+        pgcm.kv_select(q, tables, lens, bounds, scales, block, selected, first=1, last=2, workspace=space)
+        pgcm.kv_attend(cache, q, tables, lens, sparse, selected=selected, workspace=space)
+        pgcm.kv_attend(cache, q, tables, lens, out, weights=weights, kept=weights, decay=0.9, workspace=space)
+        pgcm.kv_evict(weights, tables, lens, block, evict, victims, tables_out=tables, first=1, last=2, blocks=n * row)
+
+    changed = (pool, bounds, scales, tables, weights, q, out, sparse, selected, victims)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        for now in ([20000, 700], [1, 20800], [20001, 16], [12345, 19999]):
+            packed.copy_(torch.randn(packed.shape, device="cuda", generator=gen))
+            at = torch.tensor(now, device="cuda") - 1
+            lens.copy_(at + 1)
+            positions.copy_(at)
+            place = at // block
+            here = tables.gather(1, place[:, None])[:, 0].long()
+            slots.copy_(torch.where(here >= 0, here * block + at % block, -1))
+            last.copy_(here)
+            counts.copy_(at % block + 1)
+            before = [x.clone() for x in changed]
+            graph.replay()
+            got = [x.clone() for x in changed]
+            for x, y in zip(changed, before):
+                x.copy_(y)
+            step()
+            torch.cuda.synchronize()
+            for x, y in zip(changed, got):
+                assert torch.equal(x, y)
+            assert int((victims >= 0).sum()) > 0
+    space.destroy()
