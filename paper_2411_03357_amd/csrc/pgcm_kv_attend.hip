@@ -141,9 +141,9 @@ struct Rows : Layout<kDim> {
         typedef const __attribute__((address_space(1))) void* Global;
         typedef __attribute__((address_space(3))) void* Lds;
         if (n == 0) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 0, 0);
-        if (n == 1) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 1024, 0);
-        if (n == 2) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 2048, 0);
-        if (n == 3) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 3072, 0);
+        if (n == 1) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 1 * 1024, 0);
+        if (n == 2) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 2 * 1024, 0);
+        if (n == 3) __builtin_amdgcn_global_load_lds((Global)from, (Lds)to, 16, 3 * 1024, 0);
     }
     // k, v: addresses of the rows of the piece's first token; lds: K of both pieces, then V of both
     __device__ __forceinline__ void ask_piece(const AttendArgs& a, uint8_t* lds, uint32_t which, uint64_t k, uint64_t v) const {
