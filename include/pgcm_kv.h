@@ -50,9 +50,10 @@ typedef struct {
 
 /*
  * Workspace of pgcm_kv_attend and pgcm_kv_select on the current device.  Calls that use one object go on one stream,
- * or are ordered by the caller; one thread at a time uses it.  It grows when a call needs more (that call allocates;
- * on a stream that is being captured it fails with PGCM_ERR_CAPACITY instead) and never shrinks; what it outgrew lives
- * until it is destroyed, so a captured graph may be replayed until then, in the order of the object's other calls.
+ * or are ordered by the caller; any number of threads may make them.  It grows when a call needs more (that call
+ * allocates; on a stream that is being captured it fails with PGCM_ERR_CAPACITY instead) and never shrinks; what it
+ * outgrew lives until it is destroyed, so a captured graph may be replayed until then, in the order of the object's
+ * other calls.
  */
 typedef struct pgcm_kv pgcm_kv_t;
 int pgcm_kv_create(pgcm_kv_t **out);

@@ -74,6 +74,7 @@ int pgcm_kv_reserve(pgcm_kv_t* kv, uint32_t requests, uint32_t heads, uint32_t k
     if (const int rc = check_sizes(requests, heads, kv_heads, head_dim, block_tokens, row_blocks)) return rc;
     const Room a = attend_room(requests, heads, kv_heads, head_dim, (uint64_t)row_blocks * (block_tokens / kPiece));
     const size_t s = select_room(requests, kv_heads, row_blocks);
+    const std::lock_guard<std::mutex> held(kv->enqueue);
     return kv_ensure(kv, a.counters, a.scratch > s ? a.scratch : s, (hipStream_t)hip_stream);
 }
 

@@ -777,6 +777,7 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     const bool weigh = args->weights != nullptr;
     const uint64_t row_pieces = (uint64_t)args->row_blocks * (cache->block_tokens / kPiece);
     const Room room = attend_room(args->requests, args->heads, cache->kv_heads, cache->head_dim, weigh ? row_pieces : 0);
+    const std::lock_guard<std::mutex> held(kv->enqueue);
     if (const int rc = kv_ensure(kv, room.counters, room.scratch, stream)) return rc;
 
     AttendArgs a{};

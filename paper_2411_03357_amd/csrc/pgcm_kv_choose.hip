@@ -524,6 +524,7 @@ int pgcm_kv_select(pgcm_kv_t* kv, const pgcm_kv_select_args* args, void* hip_str
     if (!aligned(args->q, args->q_request, args->q_head) || !aligned(args->bounds)) return PGCM_ERR_ALIGN;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const size_t room = select_room(args->requests, args->kv_heads, args->row_blocks);
+    const std::lock_guard<std::mutex> held(kv->enqueue);
     if (const int rc = kv_ensure(kv, 0, room, stream)) return rc;
     SelectArgs a{};
     a.q = (const uint8_t*)args->q;

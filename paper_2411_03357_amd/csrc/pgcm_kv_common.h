@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
 #include <vector>
 
 #include "../../include/pgcm.h"
@@ -20,6 +21,7 @@ struct pgcm_kv {
         size_t bytes = 0;
     };
     int device = 0;
+    std::mutex enqueue;  // held while a call's launches are enqueued, which leave to each other what lies in scratch
     Memory counters, scratch;
     std::vector<void*> outgrown;  // a captured graph may still name them
 };
@@ -32,7 +34,7 @@ constexpr uint32_t kMaxHeads = 65535;
 constexpr uint32_t kXcds = 8;
 constexpr uint32_t kTileTokens = 128;  // tokens that a workgroup of attention takes at a step
 
-// At least so many bytes of zeroed counters and of scratch.
+// At least so many bytes of zeroed counters and of scratch; kv->enqueue is held.
 int kv_ensure(pgcm_kv* kv, size_t counters, size_t scratch, hipStream_t stream);
 
 inline bool aligned(const void* p, const int64_t a = 0, const int64_t b = 0, const int64_t c = 0) {

@@ -2,6 +2,7 @@
 are not there, whatever the pool holds elsewhere, orders of memory, groups of heads, selections, weights, graphs, streams."""
 import copy
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -292,6 +293,36 @@ def test_another_stream_and_threads():
         if not torch.equal(out, want):
             wrong.append(1)
     threads = [threading.Thread(target=work) for _ in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_threads_on_one_stream():
+    """calls of several launches and of growing sizes, on the stream's own workspace"""
+    jobs = []
+    for n, tokens in enumerate((300, 900, 2500, 6000)):
+        r = ref.Requests(30 + n, [tokens, 50], 2, 64, BF16)
+        cache, q = pgcm.KVCache(*r.on_gpu()), ref.numbers(30 + n, 2, 8, 64).to(BF16).cuda()
+        tables, lens = r.gpu_tables()
+        jobs.append((cache, q, tables, lens, torch.zeros_like(q), torch.zeros(2, r.most, device="cuda")))
+    want = []
+    for cache, q, tables, lens, out, weights in jobs:
+        pgcm.kv_attend(cache, q, tables, lens, out, weights=weights)
+        want.append((out.clone(), weights.clone()))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(job, expected):
+        cache, q, tables, lens, out, weights = job
+        for _ in range(200):
+            pgcm.kv_attend(cache, q, tables, lens, out, weights=weights)
+            if not (torch.equal(out, expected[0]) and torch.equal(weights, expected[1])):
+                wrong.append(q.shape)
+
+    threads = [threading.Thread(target=work, args=x) for x in zip(jobs, want)]
     for t in threads:
         t.start()
     for t in threads:
