@@ -106,8 +106,8 @@ typedef struct {
  * out = sum over the request's tokens that are on the device of softmax(scale q . k) v; a request without any gives zeros and
  * a lse of minus infinity.  What lies in the pool beyond a request's tokens is not used, whatever it holds.
  * weights[b][j] = decay * kept[b][j] + the weights of block j's tokens, summed over the heads.
- * Softmax weights are multiplied with v as sums of two halves each, and added up in binary32: what is left out of one is
- * 2^-16 of it (bfloat16) or 2^-38 of the head's largest (binary16) at most.
+ * Softmax weights are multiplied with v as sums of halves, and added up in binary32: three (bfloat16) leave nothing out, two
+ * (binary16) 2^-38 of the head's largest at most.
  */
 int pgcm_kv_attend(pgcm_kv_t *kv, const pgcm_kv_cache *cache, const pgcm_kv_attend_args *args, void *hip_stream);
 

@@ -111,15 +111,16 @@ struct F16 {
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
-    // x as the sum of two halves, the first towards zero
-    static __device__ __forceinline__ void split(const float (&x)[8], eight& high, eight& low) {
+    // x as the sum of halves of 11 bits, the first towards zero: all but 2^-22 of it
+    static constexpr uint32_t kHalves = 2;
+    static __device__ __forceinline__ void split(const float (&x)[8], eight (&halves)[kHalves]) {
 #pragma unroll
         for (uint32_t e = 0; e < 8; e += 2) {
             const auto h = __builtin_amdgcn_cvt_pkrtz(x[e], x[e + 1]);
-            high[e] = (one)h[0], high[e + 1] = (one)h[1];
+            halves[0][e] = (one)h[0], halves[0][e + 1] = (one)h[1];
         }
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) low[e] = (one)(x[e] - (float)high[e]);
+        for (uint32_t e = 0; e < 8; ++e) halves[1][e] = (one)(x[e] - (float)halves[0][e]);
     }
 };
 struct Bf16 {
@@ -130,16 +131,24 @@ struct Bf16 {
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
-    static __device__ __forceinline__ void split(const float (&x)[8], eight& high, eight& low) {
-        uint32_t words[4];
+    // x as the sum of halves of 8 bits, towards zero: all of it
+    static constexpr uint32_t kHalves = 3;
+    static __device__ __forceinline__ void split(const float (&x)[8], eight (&halves)[kHalves]) {
+        float left[8];
 #pragma unroll
-        for (uint32_t e = 0; e < 8; e += 2) {   // (the upper half of a float is its bfloat16 towards zero)
-            const uint32_t a = __builtin_bit_cast(uint32_t, x[e]), b = __builtin_bit_cast(uint32_t, x[e + 1]);
-            words[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-            low[e] = (one)(x[e] - __builtin_bit_cast(float, a & 0xFFFF0000u));
-            low[e + 1] = (one)(x[e + 1] - __builtin_bit_cast(float, b & 0xFFFF0000u));
+        for (uint32_t e = 0; e < 8; ++e) left[e] = x[e];
+#pragma unroll
+        for (uint32_t n = 0; n < kHalves; ++n) {
+            uint32_t words[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 8; e += 2) {   // (the upper half of a float is its bfloat16 towards zero)
+                const uint32_t a = __builtin_bit_cast(uint32_t, left[e]), b = __builtin_bit_cast(uint32_t, left[e + 1]);
+                words[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                left[e] -= __builtin_bit_cast(float, a & 0xFFFF0000u);
+                left[e + 1] -= __builtin_bit_cast(float, b & 0xFFFF0000u);
+            }
+            halves[n] = __builtin_bit_cast(eight, words);
         }
-        high = __builtin_bit_cast(eight, words);
     }
 };
 

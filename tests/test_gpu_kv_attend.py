@@ -328,3 +328,40 @@ def test_threads_on_one_stream():
     for t in threads:
         t.join()
     assert not wrong
+
+
+@pytest.mark.parametrize("half", [F16, BF16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_weights_count_in_32_bits(half, dim):
+    """values that cancel, channel by channel for one head each, so that what weights are off by is what is left.  Four tokens
+    with scores up to 1 and four with scores of 0, whose values make up the others' sum: of a first four channels a head, of
+    sixteen.  One channel of the keys counts, so that a score is off by 2^-23 of itself and the exponential's argument by as
+    much again; a weight by these, its exponential (2^-23) and what halves leave of it (binary16: 2^-22); then eight
+    additions, the total's eight and its reciprocal (2^-24 each)."""
+    heads, n, block = 16, 4, 16
+    rng = np.random.default_rng(31)
+    s = torch.from_numpy(rng.uniform(0.5, 1, n)).to(half).double()
+    f = torch.from_numpy(rng.uniform(0.5, 1, heads)).to(half).double()
+    v = torch.from_numpy(rng.standard_normal((2 * n, dim))).to(half).double()
+    w = torch.cat([(f[:, None] * s).exp(), torch.ones(heads, n, dtype=torch.float64)], 1)
+    for h in range(heads):
+        for c in range(4 * h, 4 * h + 4):
+            left = -(w[h, :n] @ v[:n, c])
+            for i in range(n, 2 * n):
+                v[i, c] = left.to(half).double()
+                left = left - v[i, c]
+    w = w / w.sum(1, keepdim=True)
+    want, size = w @ v, w @ v.abs()
+    off = (4 * float(f.max() * s.max()) + 2 + 2 + 9) * 2.0 ** -23
+    tol = ref.UNIT[half] * want.abs() + ref.LEAST[half] + 1.01 * off * size
+    k_cache = torch.zeros(1, block, 1, dim, dtype=half)
+    v_cache = torch.zeros_like(k_cache)
+    k_cache[0, :n, 0, 5], v_cache[0, :2 * n, 0] = s.to(half), v.to(half)
+    q = torch.zeros(1, heads, dim, dtype=half)
+    q[0, :, 5] = f.to(half)
+    for row in (1, 200):        # a workgroup for the item; tables with room for many tiles
+        tables = torch.zeros(1, row, dtype=torch.int32).cuda()
+        out = torch.empty_like(q, device="cuda")
+        pgcm.kv_attend(pgcm.KVCache(k_cache.cuda(), v_cache.cuda()), q.cuda(), tables,
+                       torch.tensor([2 * n], dtype=torch.int32).cuda(), out, scale=1.0)
+        ref.within(out[0], (want, tol), "out")
