@@ -105,6 +105,8 @@ typedef struct {
 /*
  * out = sum over the request's tokens that are on the device of softmax(scale q . k) v; a request without any gives zeros and
  * a lse of minus infinity.  What lies in the pool beyond a request's tokens is not used, whatever it holds.
+ * A value that is not finite makes its channel so: infinite, or NaN if infinities of both signs meet.  (Where its weight is
+ * less than 2^-100 of the head's largest, infinite or NaN.)
  * weights[b][j] = decay * kept[b][j] + the weights of block j's tokens, summed over the heads.
  * Softmax weights are multiplied with v as sums of halves, and added up in binary32: three (bfloat16) leave nothing out, two
  * (binary16) 2^-38 of the head's largest at most.

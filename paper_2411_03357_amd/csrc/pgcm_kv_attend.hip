@@ -153,7 +153,7 @@ struct Rows : Layout<kDim> {
 };
 
 // What a wavefront holds of a tile: K as the operand of the first product, V as rows.
-template <uint32_t kDim, bool kExact>
+template <class H, uint32_t kDim, bool kExact>
 struct Held : Layout<kDim> {
     typedef Layout<kDim> L;
     uint4 k[2][L::kSteps];
@@ -181,6 +181,19 @@ struct Held : Layout<kDim> {
                     v[p][j][0] = x.x, v[p][j][1] = x.y;
                 }
             }
+    }
+    // whether any of the wavefront's values is not finite: their sizes as whole numbers, two an instruction (memory hides it: two
+    // requests of 131 059 tokens take 199.6 us, without 200.3)
+    __device__ __forceinline__ bool odd() const {
+        u16x2 most = (u16x2)(uint16_t)0;
+#pragma unroll
+        for (uint32_t p = 0; p < L::kParts; ++p)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j)
+#pragma unroll
+                for (uint32_t w = 0; w < L::kWords; ++w)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[p][j][w] & 0x7FFF7FFFu));
+        return __any(most.x >= H::kInfinity || most.y >= H::kInfinity);
     }
     // rows of tokens that are not there count as zero, whatever they hold
     __device__ __forceinline__ void drop_v(uint32_t which, uint32_t valid, uint32_t g) {
@@ -217,7 +230,7 @@ struct Walk : Layout<kDim> {
             if (there && (kExact || d < a.head_dim)) q[c] = *(const uint4*)(row + 2 * d);
         }
     }
-    __device__ __forceinline__ void scores(float (&s)[8], const Held<kDim, kExact>& held, float scale, uint32_t valid0,
+    __device__ __forceinline__ void scores(float (&s)[8], const Held<H, kDim, kExact>& held, float scale, uint32_t valid0,
                                            uint32_t valid1, uint32_t g) const {
         f32x4 s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -258,7 +271,37 @@ struct Walk : Layout<kDim> {
             total += s[j];
         }
     }
-    __device__ __forceinline__ void add_v(const float (&s)[8], const Held<kDim, kExact>& held) {
+    // Eight rows' words of two channels as the left operand of one of them
+    static __device__ __forceinline__ typename H::eight channel(const uint32_t (&rows)[8], uint32_t second) {
+        const uint32_t pick = second ? 0x07060302u : 0x05040100u;
+        return as_eight<H>(make_uint4(__builtin_amdgcn_perm(rows[1], rows[0], pick), __builtin_amdgcn_perm(rows[3], rows[2], pick),
+                                      __builtin_amdgcn_perm(rows[5], rows[4], pick), __builtin_amdgcn_perm(rows[7], rows[6], pick)));
+    }
+    // Values that are not finite are added with a weight of 1, if theirs is not 0, and leave the rows: a half of a weight may be
+    // 0 where the weight is not, and 0 times infinity is no number.
+    __device__ __forceinline__ void add_odd(const float (&s)[8], Held<H, kDim, kExact>& held) {
+        typename H::eight any;
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) any[j] = (typename H::one)(s[j] != 0.f ? 1.f : 0.f);
+        constexpr uint32_t kInf = H::kInfinity;
+#pragma unroll
+        for (uint32_t p = 0; p < L::kParts; ++p)
+#pragma unroll
+            for (uint32_t w = 0; w < L::kWords; ++w) {
+                uint32_t odd[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {
+                    const uint32_t word = held.v[p][j][w];
+                    const uint32_t of = ((word & kInf) == kInf ? 0xFFFFu : 0u) | ((word & kInf << 16) == kInf << 16 ? 0xFFFF0000u : 0u);
+                    odd[j] = word & of;
+                    held.v[p][j][w] = word & ~of;
+                }
+                sum[p][2 * w] = H::product(channel(odd, 0), any, sum[p][2 * w]);
+                sum[p][2 * w + 1] = H::product(channel(odd, 1), any, sum[p][2 * w + 1]);
+            }
+    }
+    __device__ __forceinline__ void add_v(const float (&s)[8], Held<H, kDim, kExact>& held) {
+        if (__builtin_expect(held.odd(), false)) add_odd(s, held);
         // A weight goes to the matrix cores in halves, each of what the ones before leave: in bfloat16 all of its 24 bits, in
         // float16 at least 22.  (Two of 8 bits each were off by up to 2^-17 of a sum's size where values cancel, and three cost
         // little beside memory: two requests of 131 059 tokens 200.3 us, with two 199.2.)
@@ -269,11 +312,9 @@ struct Walk : Layout<kDim> {
         for (uint32_t p = 0; p < L::kParts; ++p)
 #pragma unroll
             for (uint32_t t = 0; t < L::kRun; ++t) {
-                const uint32_t pick = t % 2 ? 0x07060302u : 0x05040100u;
-                x[p][t] = as_eight<H>(make_uint4(__builtin_amdgcn_perm(held.v[p][1][t / 2], held.v[p][0][t / 2], pick),
-                                                 __builtin_amdgcn_perm(held.v[p][3][t / 2], held.v[p][2][t / 2], pick),
-                                                 __builtin_amdgcn_perm(held.v[p][5][t / 2], held.v[p][4][t / 2], pick),
-                                                 __builtin_amdgcn_perm(held.v[p][7][t / 2], held.v[p][6][t / 2], pick)));
+                const uint32_t rows[8] = {held.v[p][0][t / 2], held.v[p][1][t / 2], held.v[p][2][t / 2], held.v[p][3][t / 2],
+                                          held.v[p][4][t / 2], held.v[p][5][t / 2], held.v[p][6][t / 2], held.v[p][7][t / 2]};
+                x[p][t] = channel(rows, t % 2);
                 sum[p][t] = H::product(x[p][t], halves[0], sum[p][t]);
             }
 #pragma unroll
@@ -495,7 +536,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
         while (some_left) {
             const uint32_t here0 = valid0, here1 = valid1;
             const uint32_t piece0 = (now.tile + in_segment) * (kTileTokens / kPiece) + 2 * wave;
-            Held<kDim, kExact> held;
+            Held<H, kDim, kExact> held;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the tile's rows are in LDS
             held.take(a, lds, g, i);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // ... and have left it

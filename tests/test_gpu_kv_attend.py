@@ -365,3 +365,31 @@ def test_weights_count_in_32_bits(half, dim):
         pgcm.kv_attend(pgcm.KVCache(k_cache.cuda(), v_cache.cuda()), q.cuda(), tables,
                        torch.tensor([2 * n], dtype=torch.int32).cuda(), out, scale=1.0)
         ref.within(out[0], (want, tol), "out")
+
+
+@pytest.mark.parametrize("half", [F16, BF16])
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+def test_infinities_and_nan_that_are_attended_to(half, dim):
+    """a value that is infinite makes its channel infinite, one that is no number makes it none, and no other channel, head or
+    request sees it; alone in a request, whose weight is exactly 1, among others, and in several parts of a long one"""
+    r = ref.Requests(22, [1, 17, 300, 2500, 40], 2, dim, half)
+    at = lambda b, t: (int(r.tables[b, t // 16]), t % 16)
+    for b, t in ((0, 0), (1, 16), (2, 40), (2, 299), (3, 5), (3, 2499)):
+        i, inside = at(b, t)
+        r.v[i, inside, 0, 3], r.v[i, inside, 0, dim - 1] = math.inf, -math.inf
+        r.v[i, inside, 1, 6] = math.nan
+    i, inside = at(3, 1300)
+    r.v[i, inside, 0, 3] = -math.inf        # of both signs in one channel: no number
+    q = ref.numbers(22, 5, 6, dim).to(half)
+    (want, tol), _, _ = ref.attend(r, q, dim ** -0.5)
+    assert bool(want[:3, :3, 3].isposinf().all()) and bool(want[:4, :3, dim - 1].isneginf().all())
+    assert bool(want[3, :3, 3].isnan().all()) and bool(want[:4, 3:, 6].isnan().all())
+    assert int((~want.isfinite()).sum()) == 4 * 3 * 3
+    for row in (r.most, r.most + 2200 // 16):
+        wide = copy.copy(r)
+        wide.tables, wide.most = np.pad(r.tables, ((0, 0), (0, row - r.most)), constant_values=-1), row
+        out = _run(wide, q)[0].double().cpu()
+        assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.isposinf(), want.isposinf())
+        assert torch.equal(out.isneginf(), want.isneginf())
+        there = want.isfinite()
+        assert bool(((out - want).abs()[there] <= tol[there]).all())
