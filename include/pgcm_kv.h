@@ -94,7 +94,7 @@ typedef struct {
     const int32_t *lens;               /* DEVICE [requests]: tokens of each */
     const int32_t *selected;           /* DEVICE [requests][kv_heads][keep], or NULL: places in the request's row that this kv
                                           head reads, each at most once; what lies outside the request's blocks is passed over */
-    uint32_t keep;
+    uint32_t keep;                     /* 0: nothing is read */
     float decay;
     void *out;                         /* DEVICE halves [requests][heads][head_dim] */
     int64_t out_request, out_head;

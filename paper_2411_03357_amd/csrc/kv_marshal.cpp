@@ -21,6 +21,7 @@ struct KvCalls {
 // A CUDA tensor; strides of dimensions of one count as zero.
 struct Tensor {
     void* at = nullptr;
+    bool none = true;   // not taken
     int64_t shape[4] = {0, 0, 0, 0}, stride[4] = {0, 0, 0, 0};
 
     // of this type and number of dimensions, contiguous as a whole or in the last of them
@@ -36,11 +37,14 @@ struct Tensor {
             }
             if (whole ? !t.is_contiguous() : shape[dims - 1] > 1 && stride[dims - 1] != 1) return false;
             at = t.data_ptr();
+            none = false;
         } catch (...) {   // (a tensor without memory of its own)
             return false;
         }
         return true;
     }
+    // for what an address says to be there: a tensor without elements has none, and nothing of it is read
+    void* given() const { return at != nullptr ? at : none ? nullptr : (void*)4096; }
     bool is(int64_t a, int64_t b = -1, int64_t c = -1, int64_t d = -1) const {
         return shape[0] == a && (b < 0 || shape[1] == b) && (c < 0 || shape[2] == c) && (d < 0 || shape[3] == d);
     }
@@ -149,7 +153,7 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     a.q_token = q.stride[0], a.q_head = q.stride[1], a.k_token = k.stride[0], a.k_head = k.stride[1];
     a.v_token = v.stride[0], a.v_head = v.stride[1], a.q_out_token = q_out.stride[0], a.q_out_head = q_out.stride[1];
     a.positions = turned ? (const int32_t*)positions.at : nullptr, a.slots = (const int64_t*)slots.at;
-    a.q_weight = q_weight.at, a.k_weight = k_weight.at, a.rope = (const float*)rope.at;
+    a.q_weight = q_weight.at, a.k_weight = k_weight.at, a.rope = (const float*)rope.given();
     a.rope_positions = (uint32_t)rope.shape[0], a.rope_dim = (uint32_t)rope.shape[1];
     return called([&] { return g_kv.append(cache, &a, stream); });
 }
@@ -182,8 +186,8 @@ PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     a.q = q.at, a.q_request = q.stride[0], a.q_head = q.stride[1];
     a.out = out.at, a.out_request = out.stride[0], a.out_head = out.stride[1];
     a.tables = (const int32_t*)tables.at, a.table_row = tables.stride[0], a.lens = (const int32_t*)lens.at;
-    a.selected = (const int32_t*)selected.at, a.lse = (float*)lse.at;
-    a.weights = (float*)weights.at, a.kept = (const float*)kept.at;
+    a.selected = (const int32_t*)selected.given(), a.lse = (float*)lse.at;
+    a.weights = (float*)weights.given(), a.kept = (const float*)kept.given();
     return called([&] { return g_kv.attend(space, cache, &a, stream); });
 }
 

@@ -97,6 +97,11 @@ def _ptr(t, what, dtype, shape, contiguous=True):
     return t.data_ptr()
 
 
+def _given(at):
+    """for what an address says to be there: a tensor without elements has none, and nothing of it is read"""
+    return at or 4096
+
+
 def _strides(t):
     """strides of all dimensions but the last; a dimension of one has none that counts"""
     return [0 if n == 1 else s for n, s in zip(t.shape[:-1], t.stride())]
@@ -199,7 +204,7 @@ def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=N
     a.eps = eps
     if rope is not None:
         a.positions = _ptr(positions, "positions", torch.int32, (n,))
-        a.rope = _ptr(rope, "rope", torch.float32, rope.shape)
+        a.rope = _given(_ptr(rope, "rope", torch.float32, rope.shape))
         a.rope_positions, a.rope_dim = rope.shape
         a.adjacent = 1 if adjacent else 0
     _check(_lib().pgcm_kv_append(cache._at, C.addressof(a), h))
@@ -233,11 +238,11 @@ def kv_attend(cache, q, tables, lens, out, lse=None, scale=None, selected=None, 
         a.lse = _ptr(lse, "lse", torch.float32, (n, heads))
     if selected is not None:
         a.keep = selected.shape[-1]
-        a.selected = _ptr(selected, "selected", torch.int32, (n, cache.kv_heads, a.keep))
+        a.selected = _given(_ptr(selected, "selected", torch.int32, (n, cache.kv_heads, a.keep)))
     if weights is not None:
-        a.weights, a.decay = _ptr(weights, "weights", torch.float32, (n, row)), decay
+        a.weights, a.decay = _given(_ptr(weights, "weights", torch.float32, (n, row))), decay
     if kept is not None:
-        a.kept = _ptr(kept, "kept", torch.float32, (n, row))
+        a.kept = _given(_ptr(kept, "kept", torch.float32, (n, row)))
     _check(_lib().pgcm_kv_attend(space, cache._at, C.addressof(a), h))
 
 

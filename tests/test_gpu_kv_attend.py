@@ -393,3 +393,19 @@ def test_infinities_and_nan_that_are_attended_to(half, dim):
         assert torch.equal(out.isneginf(), want.isneginf())
         there = want.isfinite()
         assert bool(((out - want).abs()[there] <= tol[there]).all())
+
+
+@pytest.mark.parametrize("row", [4, 300])
+def test_selections_without_places(row):
+    """... are selections: nothing is attended to; and, like others, they go with no weights"""
+    q = torch.ones(2, 4, 64, dtype=F16, device="cuda")
+    pool = torch.ones(8, 16, 2, 64, dtype=F16, device="cuda")
+    tables = torch.zeros(2, row, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([40, 0], dtype=torch.int32, device="cuda")
+    none = torch.empty(2, 2, 0, dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, 9.0), torch.full((2, 4), 9.0, device="cuda")
+    pgcm.kv_attend(pgcm.KVCache(pool, pool), q, tables, lens, out, lse=lse, selected=none)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    with pytest.raises(pgcm.PgcmError) as e:
+        pgcm.kv_attend(pgcm.KVCache(pool, pool), q, tables, lens, out, selected=none, weights=torch.zeros(2, row, device="cuda"))
+    assert e.value.status == -1

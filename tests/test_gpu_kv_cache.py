@@ -160,3 +160,15 @@ def test_summarize(half, dim, block, kv):
     want = ref.summarize(where[4:5], [block])
     assert np.array_equal(bounds[4:5].cpu().numpy(), want[0]) and np.array_equal(scales[4:5].cpu().numpy(), want[1])
     assert int((bounds != 99).flatten(1).any(1).sum()) <= 1 and int((scales != 99).any(1).sum()) == 1
+
+
+def test_append_a_table_without_lines():
+    """... is no table that can be left out"""
+    x = torch.ones(2, 4, 64, dtype=F16, device="cuda")
+    pool = torch.zeros(2, 2, 16, 2, 64, dtype=F16, device="cuda")
+    at = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for shape in ((0, 64), (5, 0)):
+        with pytest.raises(pgcm.PgcmError) as e:
+            pgcm.kv_append(pgcm.KVCache(pool[:, 0], pool[:, 1]), None, x[:, :2], x[:, 2:], at, torch.tensor([1, 2]).cuda(), None,
+                           rope=torch.empty(shape, device="cuda"))
+        assert e.value.status == -1
