@@ -176,8 +176,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
             auto turn = [&](const float(&c)[8], const float(&s)[8]) {
 #pragma unroll
                 for (uint32_t e = 0; e < 8; ++e) {
-                    const float pair = (float)(a.adjacent ? x[e ^ 1] : y[e]);
-                    z[e] = (typename H::one)(((float)x[e] * c[e] + pair * s[e]) * by);
+                    const float pair = (float)(a.adjacent ? x[e ^ 1] : y[e]), own = (float)x[e] * c[e];
+                    z[e] = (typename H::one)((turned ? own + pair * s[e] : own) * by);   // (0 times infinity is no number)
                 }
             };
             if (k == 0) turn(own[0], other[0]);

@@ -162,6 +162,35 @@ def test_summarize(half, dim, block, kv):
     assert int((bounds != 99).flatten(1).any(1).sum()) <= 1 and int((scales != 99).any(1).sum()) == 1
 
 
+@pytest.mark.parametrize("half", [F16, BF16])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("dim,rope_dim", [(128, 0), (128, 128), (128, 64), (80, 48), (256, 32), (24, 16)])
+def test_append_infinities_and_nan(half, adjacent, dim, rope_dim):
+    """channels that are not rotated stay as they are beside any others, and a pair that is rotated sees its own two alone"""
+    tokens, heads, kv = 5, 4, 2
+    x = ref.numbers(dim + rope_dim, tokens, heads + 2 * kv, dim).to(half)
+    x[0, :, dim - 1], x[1, :, dim - 2], x[2, :, dim - 3] = math.inf, -math.inf, math.nan
+    x[3, :, 1], x[4, :, 2] = math.nan, math.inf
+    packed = x.cuda()
+    pool = torch.zeros(2, 2, 16, kv, dim, dtype=half, device="cuda")
+    out = torch.empty(tokens, heads, dim, dtype=half, device="cuda")
+    positions, slots = [3, 9, 1, 7, 8], [0, 17, 3, 31, 5]
+    table = _table(10, rope_dim) if rope_dim else None
+    pgcm.kv_append(pgcm.KVCache(pool[:, 0], pool[:, 1]), packed[:, :heads], packed[:, heads:heads + kv], packed[:, heads + kv:],
+                   torch.tensor(positions, dtype=torch.int32).cuda() if rope_dim else None, torch.tensor(slots).cuda(), out,
+                   rope=None if table is None else table.cuda(), adjacent=adjacent)
+    rows = pool.transpose(1, 2).reshape(32, 2, kv, dim).cpu()[slots]
+    want = ref.turned(x[:, :heads + kv], None, 0, table, positions, adjacent)
+    got = torch.cat([out.cpu(), rows[:, 0]], 1)
+    still = x[:, :heads + kv, rope_dim:]
+    assert torch.equal(got[..., rope_dim:].isnan(), still.isnan())
+    assert torch.equal(got[..., rope_dim:].nan_to_num(7.0), still.nan_to_num(7.0))
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    there = want.isfinite()
+    _near(got.where(there, 0.0), want.where(there, 0.0), None, half, dim, "q and k")
+    assert torch.equal(rows[:, 1].nan_to_num(7.0), x[:, heads + kv:].nan_to_num(7.0))
+
+
 def test_append_a_table_without_lines():
     """... is no table that can be left out"""
     x = torch.ones(2, 4, 64, dtype=F16, device="cuda")
