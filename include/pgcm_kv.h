@@ -109,7 +109,8 @@ typedef struct {
  * less than 2^-100 of the head's largest, infinite or NaN.)
  * weights[b][j] = decay * kept[b][j] + the weights of block j's tokens, summed over the heads.
  * Softmax weights are multiplied with v as sums of halves, and added up in binary32: three (bfloat16) leave nothing out, two
- * (binary16) 2^-38 of the head's largest at most.
+ * (binary16) 2^-22 of a weight at most, or 2^-38 of the head's largest where that is more.  In bfloat16 sums of values
+ * beyond 2^88 may leave the range of binary32.
  */
 int pgcm_kv_attend(pgcm_kv_t *kv, const pgcm_kv_cache *cache, const pgcm_kv_attend_args *args, void *hip_stream);
 
