@@ -146,10 +146,13 @@ typedef struct {
     int32_t *counts;                   /* DEVICE [requests][kv_heads], or NULL: how many */
 } pgcm_kv_select_args;
 /*
- * The score of a block is an upper bound of q . k over its tokens: with c = round(q * (127 / a)) of each head, a its largest
- * |q|, and s = a / 127 (as for the bounds),  max over the group's heads of (sum_d max(c low, c high) * scale) * s.
- * The sum is exact, the products are rounded to binary32 in this order.  The largest scores win, among equal ones the
- * first; and among the blocks at the ends, where keep is less than those, the first.
+ * The score of a block estimates the largest that q . k may be for keys within its bounds: with c = round(q * (127 / a)) of
+ * each head, a its largest |q|, and s = a / 127 (as for the bounds),  max over the group's heads of
+ * (sum_d max(c low, c high) * scale) * s.  The sum is exact, the products are rounded to binary32 in this order.  It is not a
+ * bound itself, as c, low and high are rounded to nearest: q . k is at most
+ * (sum_d (max(c low, c high) + (|c| + max(|low|, |high|)) / 2 + 1/4)) * scale * s.
+ * The largest scores win, among equal ones the first; and among the blocks at the ends, where keep is less than those, the
+ * first.
  */
 int pgcm_kv_select(pgcm_kv_t *kv, const pgcm_kv_select_args *args, void *hip_stream);
 
