@@ -40,10 +40,28 @@ def hipcc() -> str:
     return exe
 
 
+def _torch():
+    """the torch that is installed, or None: the cipher and its binding do without"""
+    try:
+        import torch
+    except ImportError:
+        return None
+    return torch
+
+
+def _built_for(torch) -> bytes:
+    return b"built for torch " + torch.__version__.encode() + b"\0"
+
+
 def is_stale() -> bool:
-    built = (LIB, MARSHAL, KV_MARSHAL)
+    torch = _torch()
+    built = (LIB, MARSHAL) if torch is None else (LIB, MARSHAL, KV_MARSHAL)
     if not all(os.path.exists(b) for b in built):
         return True
+    if torch is not None:
+        with open(KV_MARSHAL, "rb") as f:
+            if _built_for(torch) not in f.read():
+                return True
     t = min(os.path.getmtime(b) for b in built)
     deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["marshal.cpp", "kv_marshal.cpp"]] + \
         [os.path.abspath(__file__)]
@@ -66,11 +84,13 @@ def _host_build(source, target, *more) -> None:
 
 def build_marshal() -> None:
     _host_build("marshal.cpp", MARSHAL)
-    import torch
+    torch = _torch()
+    if torch is None:       # no tensors, so none of the operators that take them
+        return
     at = os.path.dirname(torch.__file__)
     _host_build("kv_marshal.cpp", KV_MARSHAL, "-isystem", os.path.join(at, "include"),
-                "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(), "-L" + os.path.join(at, "lib"),
-                "-ltorch_python", "-ltorch_cpu", "-lc10")
+                "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(), '-DBUILT_FOR="%s"' % torch.__version__,
+                "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10")
 
 
 def build(force: bool = True, verbose: bool = False) -> str:

@@ -302,6 +302,16 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
+// BUILT_FOR: torch.__version__ when this was compiled; what a tensor is in memory belongs to it
+const char kBuiltFor[] = "built for torch " BUILT_FOR;
+
 }  // namespace
 
-PyMODINIT_FUNC PyInit__kv_marshal() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__kv_marshal() {
+    PyObject* m = PyModule_Create(&module);
+    if (m != nullptr && PyModule_AddStringConstant(m, "built_for", kBuiltFor) != 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

@@ -51,6 +51,18 @@ _bound = None
 _marshal = None     # native marshalling (csrc/kv_marshal.cpp), bound to _bound
 
 
+def _load_marshal():
+    """the extension that reads tensors; one of another torch would read them wrongly"""
+    try:
+        from . import _kv_marshal as m
+    except ImportError as e:
+        raise ImportError("_kv_marshal.so is not built, or not for this torch: python -m paper_2411_03357_amd.build") from e
+    if m.built_for != "built for torch " + torch.__version__:
+        raise ImportError("_kv_marshal.so was %s, and this is torch %s: python -m paper_2411_03357_amd.build" %
+                           (m.built_for, torch.__version__))
+    return m
+
+
 def _lib():
     global _bound
     if _bound is None:
@@ -67,7 +79,7 @@ def _lib():
         for name in KV_EXPORTS:
             if name != "pgcm_kv_destroy":
                 getattr(lib, name).restype = C.c_int
-        from . import _kv_marshal as m
+        m = _load_marshal()
         m.bind(*[C.cast(getattr(lib, "pgcm_kv_" + n), _vp).value
                  for n in ("append", "attend", "summarize", "select", "evict")])
         global _marshal
