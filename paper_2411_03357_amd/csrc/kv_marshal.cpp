@@ -18,18 +18,26 @@ struct KvCalls {
     decltype(&pgcm_kv_evict) evict;
 } g_kv;
 
-// A CUDA tensor; strides of dimensions of one count as zero.
+// A cache as kv.py hands it over: with the device that it is on.
+struct Cache {
+    pgcm_kv_cache c;
+    int64_t device;
+};
+
+// A tensor on the current CUDA device; strides of dimensions of one count as zero.
 struct Tensor {
     void* at = nullptr;
     bool none = true;   // not taken
     int64_t shape[4] = {0, 0, 0, 0}, stride[4] = {0, 0, 0, 0};
 
     // of this type and number of dimensions, contiguous as a whole or in the last of them
-    bool take(PyObject* o, at::ScalarType dtype, int dims, bool whole) {
+    bool take(PyObject* o, int64_t device, at::ScalarType dtype, int dims, bool whole) {
         if (!THPVariable_Check(o)) return false;
         try {
             const at::Tensor& t = THPVariable_Unpack(o);
-            if (t.scalar_type() != dtype || t.dim() != dims || !t.is_cuda() || t.layout() != at::kStrided) return false;
+            if (t.scalar_type() != dtype || t.dim() != dims || !t.is_cuda() || t.get_device() != device ||
+                t.layout() != at::kStrided)
+                return false;
             const auto sizes = t.sizes(), strides = t.strides();
             for (int i = 0; i < dims; ++i) {
                 shape[i] = sizes[i];
@@ -50,10 +58,10 @@ struct Tensor {
     }
 };
 
-// Arguments one after the other; good() turns false for good at the first one that is unusual.
+// Arguments one after the other, the current device first; good() turns false for good at the first one that is unusual.
 class Arguments {
   public:
-    Arguments(PyObject* const* args, Py_ssize_t n) : args_(args), n_(n) {}
+    Arguments(PyObject* const* args, Py_ssize_t n) : args_(args), n_(n) { device_ = number(); }
     ~Arguments() {
         if (!good_) PyErr_Clear();
     }
@@ -65,6 +73,12 @@ class Arguments {
         void* p = PyLong_Check(o) ? PyLong_AsVoidPtr(o) : nullptr;
         good_ = good_ && PyLong_Check(o) && PyErr_Occurred() == nullptr;
         return p;
+    }
+    // on the current device
+    const pgcm_kv_cache* cache() {
+        const auto* cache = (const Cache*)address();
+        if (cache == nullptr || cache->device != device_) good_ = false;
+        return good_ ? &cache->c : nullptr;
     }
     uint32_t number() {
         PyObject* o = next();
@@ -88,7 +102,7 @@ class Arguments {
             if (!may_be_none) refuse();
             return false;
         }
-        if (!t->take(o, dtype, dims, whole)) refuse();
+        if (!t->take(o, device_, dtype, dims, whole)) refuse();
         return good_;
     }
     void need(bool is) { good_ = good_ && is; }
@@ -107,6 +121,7 @@ class Arguments {
     }
     PyObject* const* args_;
     Py_ssize_t n_, at_ = 0;
+    int64_t device_ = 0;
     bool good_ = true;
 };
 
@@ -121,11 +136,11 @@ PyObject* called(Call call) {
     return PyLong_FromLong(status);
 }
 
-// (cache, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope, adjacent, stream) -> status or None
+// (device, cache, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope, adjacent, stream) -> status or None
 PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Arguments in(args, nargs);
-    const auto* cache = (const pgcm_kv_cache*)in.address();
-    if (!in.good() || cache == nullptr) Py_RETURN_NONE;
+    const pgcm_kv_cache* cache = in.cache();
+    if (cache == nullptr) Py_RETURN_NONE;
     const at::ScalarType half = half_of(cache->half);
     const int64_t d = cache->head_dim, kv = cache->kv_heads;
     pgcm_kv_append_args a = {};
@@ -158,12 +173,12 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return called([&] { return g_kv.append(cache, &a, stream); });
 }
 
-// (workspace, cache, q, tables, lens, out, lse, scale, selected, weights, kept, decay, stream) -> status or None
+// (device, workspace, cache, q, tables, lens, out, lse, scale, selected, weights, kept, decay, stream) -> status or None
 PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Arguments in(args, nargs);
     auto* space = (pgcm_kv_t*)in.address();
-    const auto* cache = (const pgcm_kv_cache*)in.address();
-    if (!in.good() || cache == nullptr) Py_RETURN_NONE;
+    const pgcm_kv_cache* cache = in.cache();
+    if (cache == nullptr) Py_RETURN_NONE;
     const at::ScalarType half = half_of(cache->half);
     pgcm_kv_attend_args a = {};
     Tensor q, tables, lens, out, lse, selected, weights, kept;
@@ -191,11 +206,11 @@ PyObject* kv_attend(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return called([&] { return g_kv.attend(space, cache, &a, stream); });
 }
 
-// (cache, blocks, counts, bounds, scales, entries, stream) -> status or None
+// (device, cache, blocks, counts, bounds, scales, entries, stream) -> status or None
 PyObject* kv_summarize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Arguments in(args, nargs);
-    const auto* cache = (const pgcm_kv_cache*)in.address();
-    if (!in.good() || cache == nullptr) Py_RETURN_NONE;
+    const pgcm_kv_cache* cache = in.cache();
+    if (cache == nullptr) Py_RETURN_NONE;
     Tensor blocks, counts, bounds, scales, entries;
     in.tensor(&blocks, at::kInt, 1, true);
     in.tensor(&counts, at::kInt, 1, true);
@@ -213,7 +228,8 @@ PyObject* kv_summarize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     });
 }
 
-// (workspace, half, q, tables, lens, bounds, scales, block_tokens, selected, counts, first, last, stream) -> status or None
+// (device, workspace, half, q, tables, lens, bounds, scales, block_tokens, selected, counts, first, last, stream)
+// -> status or None
 PyObject* kv_select(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Arguments in(args, nargs);
     auto* space = (pgcm_kv_t*)in.address();
@@ -245,7 +261,8 @@ PyObject* kv_select(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return called([&] { return g_kv.select(space, &a, stream); });
 }
 
-// (weights, tables, lens, block_tokens, evict, victims, victim_blocks, tables_out, first, last, blocks, stream) -> status or None
+// (device, weights, tables, lens, block_tokens, evict, victims, victim_blocks, tables_out, first, last, blocks, stream)
+// -> status or None
 PyObject* kv_evict(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Arguments in(args, nargs);
     pgcm_kv_evict_args a = {};

@@ -19,6 +19,10 @@ class _Cache(C.Structure):
         [(n, _i64) for n in ("k_block", "k_token", "k_head", "v_block", "v_token", "v_head")]
 
 
+class _Placed(C.Structure):
+    _fields_ = [("cache", _Cache), ("device", _i64)]
+
+
 class _Append(C.Structure):
     _fields_ = [("tokens", _u32), ("heads", _u32), ("q", _vp), ("k", _vp), ("v", _vp)] + \
         [(n, _i64) for n in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head")] + \
@@ -47,6 +51,7 @@ class _Evict(C.Structure):
                 ("last", _u32), ("victims", _vp), ("victim_blocks", _vp), ("tables_out", _vp), ("table_out_row", _i64)]
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _bound = None
 _marshal = None     # native marshalling (csrc/kv_marshal.cpp), bound to _bound
 
@@ -95,12 +100,19 @@ def _native():
     return _marshal
 
 
-def _ptr(t, what, dtype, shape, contiguous=True):
-    """device address of a CUDA tensor of this type and shape; its channels, or all of it, contiguous"""
+def _same_device(device, what, current):
+    if device != current:
+        raise ValueError("%s is on cuda:%d, and the current device is cuda:%d" % (what, device, current))
+
+
+def _ptr(t, what, dtype, shape, contiguous=True, anywhere=False):
+    """device address of a CUDA tensor of this type and shape, on the current device; its channels, or all of it, contiguous"""
     if t.dtype != dtype or tuple(t.shape) != tuple(shape):
         raise ValueError("%s must be %s %s, not %s %s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     if not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor" % what)
+    if not anywhere:
+        _same_device(t.get_device(), what, _device())
     if contiguous:
         if not t.is_contiguous():
             raise ValueError("%s must be contiguous" % what)
@@ -129,8 +141,11 @@ class KVCache:
             raise ValueError("a cache is float16 or bfloat16 [blocks, block_tokens, kv_heads, head_dim]")
         self.k, self.v, self.dtype = k, v, k.dtype
         self.blocks, self.block_tokens, self.kv_heads, self.head_dim = k.shape
-        self._c = _Cache(_ptr(k, "k", k.dtype, k.shape, False), _ptr(v, "v", k.dtype, k.shape, False), _HALVES[k.dtype],
-                         *k.shape, 0, *_strides(k), *_strides(v))
+        at = [_ptr(x, what, k.dtype, k.shape, False, anywhere=True) for x, what in ((k, "k"), (v, "v"))]
+        self.device = k.get_device()
+        if v.get_device() != self.device:
+            raise ValueError("k and v must be on one device")
+        self._c = _Placed(_Cache(*at, _HALVES[k.dtype], *k.shape, 0, *_strides(k), *_strides(v)), self.device)
         self._at = C.addressof(self._c)
 
 
@@ -160,7 +175,6 @@ class KVWorkspace:
             pass
 
 
-_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _workspaces = {}    # (device, stream handle) -> KVWorkspace, of calls that name none
 _workspaces_lock = threading.Lock()
 
@@ -192,12 +206,13 @@ def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=N
     if not k.is_cuda:
         raise ValueError("k must be a CUDA tensor")
     h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_append(cache._at, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope,
-                                               1 if adjacent else 0, h)
+    status = (_marshal or _native()).kv_append(_device(), cache._at, q, k, v, positions, slots, q_out, q_weight,
+                                               k_weight, eps, rope, 1 if adjacent else 0, h)
     if status is not None:
         if status:
             _check(status)
         return
+    _same_device(cache.device, "the cache", _device())
     n, kv, d, half = k.shape[0], cache.kv_heads, cache.head_dim, cache.dtype
     heads = 0 if q is None else q.shape[1]
     a = _Append(n, heads)
@@ -233,12 +248,13 @@ def kv_attend(cache, q, tables, lens, out, lse=None, scale=None, selected=None, 
     if scale is None:
         scale = cache.head_dim ** -0.5
     space = (workspace or kv_workspace(h))._h
-    status = (_marshal or _native()).kv_attend(space, cache._at, q, tables, lens, out, lse, scale, selected, weights, kept,
-                                               decay, h)
+    status = (_marshal or _native()).kv_attend(_device(), space, cache._at, q, tables, lens, out, lse, scale, selected,
+                                               weights, kept, decay, h)
     if status is not None:
         if status:
             _check(status)
         return
+    _same_device(cache.device, "the cache", _device())
     n, row, tables_at, lens_at = _rows(tables, lens)
     d, half = cache.head_dim, cache.dtype
     heads = q.shape[1]
@@ -264,11 +280,12 @@ def kv_summarize(cache, blocks, counts, bounds, scales, entries=None, stream=Non
     if not blocks.is_cuda:
         raise ValueError("blocks must be a CUDA tensor")
     h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_summarize(cache._at, blocks, counts, bounds, scales, entries, h)
+    status = (_marshal or _native()).kv_summarize(_device(), cache._at, blocks, counts, bounds, scales, entries, h)
     if status is not None:
         if status:
             _check(status)
         return
+    _same_device(cache.device, "the cache", _device())
     n, m = blocks.shape[0], bounds.shape[0]
     _check(_lib().pgcm_kv_summarize(
         cache._at, n, _ptr(blocks, "blocks", torch.int32, (n,)), _ptr(counts, "counts", torch.int32, (n,)),
@@ -285,8 +302,8 @@ def kv_select(q, tables, lens, bounds, scales, block_tokens, selected, counts=No
         raise ValueError("q must be a CUDA tensor")
     h = _stream_handle(stream)
     space = (workspace or kv_workspace(h))._h
-    status = (_marshal or _native()).kv_select(space, _HALVES.get(q.dtype, 0), q, tables, lens, bounds, scales, block_tokens,
-                                               selected, counts, first, last, h)
+    status = (_marshal or _native()).kv_select(_device(), space, _HALVES.get(q.dtype, 0), q, tables, lens, bounds, scales,
+                                               block_tokens, selected, counts, first, last, h)
     if status is not None:
         if status:
             _check(status)
@@ -311,8 +328,8 @@ def kv_evict(weights, tables, lens, block_tokens, evict, victims, victim_blocks=
     if not weights.is_cuda:
         raise ValueError("weights must be a CUDA tensor")
     h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_evict(weights, tables, lens, block_tokens, evict, victims, victim_blocks, tables_out,
-                                              first, last, blocks, h)
+    status = (_marshal or _native()).kv_evict(_device(), weights, tables, lens, block_tokens, evict, victims, victim_blocks,
+                                              tables_out, first, last, blocks, h)
     if status is not None:
         if status:
             _check(status)
