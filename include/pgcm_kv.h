@@ -22,7 +22,8 @@
  * bfloat16; sums, softmax statistics and norms are held in binary32, and each output is rounded once.  Rows of halves
  * are read in pieces of 16 bytes: their pointers are 16-byte aligned and their strides multiples of 8 elements
  * (otherwise PGCM_ERR_ALIGN); head_dim is a multiple of 8 up to 256, block_tokens a multiple of 16 up to 4096.
- * Results do not depend on the order in which workgroups run.
+ * A call for which a launch would need 2^32 threads is refused: some 2^24 tokens, blocks' heads, lists or rows, 2^22 rows of
+ * more than 2048 blocks to evict from.  Results do not depend on the order in which workgroups run.
  */
 #ifndef PGCM_KV_H
 #define PGCM_KV_H

@@ -374,6 +374,7 @@ int pgcm_kv_append(const pgcm_kv_cache* cache, const pgcm_kv_append_args* args, 
     uint32_t ways = args->tokens >= 1024 ? 1 : (1024 + args->tokens - 1) / args->tokens;
     if (ways > passes) ways = passes;
     const uint32_t threads = 64 * waves;
+    if (!launchable(args->tokens, threads)) return PGCM_ERR_ARG;
     const dim3 grid(args->tokens, ways);
     if (cache->half == PGCM_KV_F16) append_kernel<F16><<<grid, threads, 0, (hipStream_t)hip_stream>>>(a);
     else append_kernel<Bf16><<<grid, threads, 0, (hipStream_t)hip_stream>>>(a);
@@ -399,6 +400,7 @@ int pgcm_kv_summarize(const pgcm_kv_cache* cache, uint32_t n, const int32_t* blo
     a.group_power = a.row_power;
     while (a.group_power < 6 && (4u << (a.group_power - a.row_power)) < a.block_tokens) ++a.group_power;
     const uint64_t threads = (uint64_t)n * a.kv_heads << a.group_power;
+    if (!launchable((threads + kThreads - 1) / kThreads, kThreads)) return PGCM_ERR_ARG;
     const uint32_t groups = (uint32_t)((threads + kThreads - 1) / kThreads);
     const hipStream_t stream = (hipStream_t)hip_stream;
     if (cache->half == PGCM_KV_F16) {

@@ -519,8 +519,8 @@ int pgcm_kv_select(pgcm_kv_t* kv, const pgcm_kv_select_args* args, void* hip_str
     if (args->q == nullptr || args->lens == nullptr || args->bounds == nullptr || args->scales == nullptr ||
         args->selected == nullptr || args->keep == 0 || args->keep > 0x7FFFFFFFu || args->entry_count == 0 ||
         args->entry_count > 0x7FFFFFFFu || (args->tables == nullptr && args->row_blocks != 0) || args->requests > 65535 ||
-        (uint64_t)args->requests * args->kv_heads > 0x7FFFFFFFull)
-        return PGCM_ERR_ARG;
+        !launchable((uint64_t)args->requests * args->kv_heads, kScoreThreads))
+        return PGCM_ERR_ARG;   // (longer rows, that take more threads, are fewer by check_sizes)
     if (!aligned(args->q, args->q_request, args->q_head) || !aligned(args->bounds)) return PGCM_ERR_ALIGN;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const size_t room = select_room(args->requests, args->kv_heads, args->row_blocks);
@@ -559,6 +559,7 @@ int pgcm_kv_evict(const pgcm_kv_evict_args* args, void* hip_stream) {
     // four wavefronts a row, or sixteen for longer ones (8 rows of 2000 blocks: 7.7 us and 8.2; of 4000 9.3 and 9.1)
     constexpr uint32_t kFew = 256;
     const hipStream_t stream = (hipStream_t)hip_stream;
+    if (!launchable(args->requests, a.row_blocks <= kFew * kSomeHeld ? kFew : kMostThreads)) return PGCM_ERR_ARG;
     if (a.row_blocks <= kFew * kFewHeld) evict_kernel<kFew, kFewHeld><<<args->requests, kFew, 0, stream>>>(a);
     else if (a.row_blocks <= kFew * kSomeHeld) evict_kernel<kFew, kSomeHeld><<<args->requests, kFew, 0, stream>>>(a);
     else if (a.row_blocks <= kMostThreads * kSomeHeld) evict_kernel<kMostThreads, kSomeHeld><<<args->requests, kMostThreads, 0, stream>>>(a);

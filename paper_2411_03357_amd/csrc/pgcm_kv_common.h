@@ -73,6 +73,9 @@ inline int check_cache(const pgcm_kv_cache* c) {
     return PGCM_OK;
 }
 
+// Threads of a launch are counted in 32 bits, in each dimension of the grid.
+inline bool launchable(uint64_t groups, uint32_t threads) { return groups * threads <= 0xFFFFFFFFull; }
+
 // ---- workspace
 struct Room {
     size_t counters, scratch;

@@ -178,3 +178,17 @@ def test_the_binding_checks_tensors():
         pgcm.kv_evict(w, torch.zeros(2, 5, dtype=torch.int64), torch.zeros(2, dtype=torch.int32), 16, w, w)
     with pytest.raises(ValueError):
         pgcm.kv_select(w, torch.zeros(2, dtype=torch.int32), w, w, w, 16, w)
+
+
+def test_what_no_launch_holds_is_refused():
+    """2^32 threads or more"""
+    lib, some, cache, one = kv._lib(), C.create_string_buffer(256), _cache(), _cache(kv_heads=1, head_dim=8)
+    for tokens in (1 << 26, (1 << 31) - 1):
+        assert lib.pgcm_kv_append(C.addressof(cache), C.byref(_append(tokens=tokens)), None) == ARG
+    for c, n in ((cache, 1 << 25), (cache, 1 << 30), (one, (1 << 31) - 1)):
+        assert lib.pgcm_kv_summarize(C.addressof(c), n, AT, AT, None, 10, AT, AT, None) == ARG
+    wide = dict(heads=1024, kv_heads=1024, row_blocks=1)
+    assert lib.pgcm_kv_select(some, C.byref(_select(requests=1 << 14, **wide)), None) == ARG
+    assert lib.pgcm_kv_select(some, C.byref(_select(requests=65535, **wide)), None) == ARG
+    for n, row in ((1 << 24, 1), ((1 << 31) - 1, 20), (1 << 24, 2048), (1 << 22, 2049)):
+        assert lib.pgcm_kv_evict(C.byref(_evict(requests=n, row_blocks=row)), None) == ARG
