@@ -177,11 +177,20 @@ class KVWorkspace:
 
 _workspaces = {}    # (device, stream handle) -> KVWorkspace, of calls that name none
 _workspaces_lock = threading.Lock()
+_PER_THREAD = 2     # the handle hipStreamPerThread: another stream in each thread
+_of_thread = threading.local()
 
 
 def kv_workspace(stream=None) -> KVWorkspace:
-    """the workspace that calls on this stream use unless they are given one"""
+    """the workspace that calls on this stream use unless they are given one.  It stays for the process, or, on
+    hipStreamPerThread, for the thread: a graph captured with it is replayed no longer than that.  Who destroys a stream
+    waits for its calls first, as a later stream may come by the same handle and with it by the same workspace."""
     key = (_device(), _stream_handle(stream))
+    if key[1] == _PER_THREAD:
+        got = _of_thread.__dict__.get(key)
+        if got is None:
+            got = _of_thread.__dict__[key] = KVWorkspace()
+        return got
     got = _workspaces.get(key)
     if got is None:
         with _workspaces_lock:
