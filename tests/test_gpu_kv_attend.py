@@ -409,3 +409,79 @@ def test_selections_without_places(row):
     with pytest.raises(pgcm.PgcmError) as e:
         pgcm.kv_attend(pgcm.KVCache(pool, pool), q, tables, lens, out, selected=none, weights=torch.zeros(2, row, device="cuda"))
     assert e.value.status == -1
+
+
+def _attend_on_gpu(pool, tables, lens, q, scale, heads_of):
+    """out, lse, weights in 64 bits of long requests, on the device, and how far each may be off: as in kv_reference, but for
+    the additions, of which a token passes through less than 1024, as wavefronts of 256 workgroups share a request's tokens"""
+    n, heads, dim = q.shape
+    blocks, _, block, kv, _ = pool.shape
+    f = torch.float64
+    out, lse = torch.zeros(n, heads, dim, dtype=f, device="cuda"), torch.full((n, heads), -math.inf, dtype=f, device="cuda")
+    out_tol, lse_tol = torch.zeros_like(out), torch.zeros_like(lse)
+    weights = torch.zeros(tables.shape, dtype=f, device="cuda")
+    weights_tol = torch.zeros_like(weights)
+    unit = ref.UNIT[pool.dtype]
+    for b, t in enumerate(lens):
+        place = torch.arange(-(-t // block), device="cuda")
+        place = place[tables[b, :place.numel()] >= 0]
+        token = (place[:, None] * block + torch.arange(block, device="cuda")).flatten()
+        there = token < t
+        if not bool(there.any()):
+            continue
+        at = tables[b, place].long()
+        for g in range(kv):
+            k, v = [pool[at, i, :, g].flatten(0, 1)[there].to(f) for i in (0, 1)]
+            mine = slice(g * heads_of, (g + 1) * heads_of)
+            x = q[b, mine].to(f)
+            s = (x @ k.T) * scale
+            e = (dim + 2) * 2.0 ** -24 * scale * (x.abs() @ k.abs().T).amax(1)
+            off = 2 * e + 1040 * 2.0 ** -24 + 2.0 ** -22 * (s.abs().amax(1) * 1.5 + 4)
+            lse[b, mine], lse_tol[b, mine] = torch.logsumexp(s, 1), off
+            p = (s - lse[b, mine, None]).exp()
+            out[b, mine] = p @ v
+            out_tol[b, mine] = unit * out[b, mine].abs() + ref.LEAST[pool.dtype] + (off + 2.0 ** -22)[:, None] * 1.01 * (p @ v.abs())
+            where = token[there] // block
+            weights[b].index_add_(0, where, p.sum(0))
+            weights_tol[b].index_add_(0, where, ((off + heads * 2.0 ** -24)[:, None] * p).sum(0))
+    return (out, out_tol), (lse, lse_tol), (weights, weights_tol)
+
+
+@pytest.mark.parametrize("dim,kv,group,half,lens", [
+    # spans of 36 tiles and more, over requests of all lengths: more than a segment each
+    (64, 4, 5, F16, [0, 150001, 5, 70007, 0, 33333, 16, 1, 46000, 129, 8000, 0]),
+    (128, 2, 8, BF16, [300000, 0, 17, 129, 200003, 60000, 0, 1, 4095]),
+    # 256 channels, a workgroup a compute unit: short spans, and long ones
+    (256, 2, 3, BF16, [90000, 40, 0, 30011, 128, 7, 2000]),
+    (256, 2, 17, F16, [200003, 0, 1000, 90001, 64]),
+])
+def test_long_requests_of_all_lengths(dim, kv, group, half, lens):
+    block = 32
+    gen = torch.Generator(device="cuda").manual_seed(dim + group)
+    most = max(-(-t // block) for t in lens) + 1
+    here = torch.zeros(len(lens), most, dtype=torch.bool)
+    for b, t in enumerate(lens):
+        here[b, :-(-t // block)] = True
+    here = here.cuda() & (torch.rand(here.shape, device="cuda", generator=gen) >= 0.05)
+    n = int(here.sum())
+    tables = torch.full(here.shape, -1, dtype=torch.int32, device="cuda")
+    tables[here] = torch.randperm(n + 3, device="cuda", generator=gen)[:n].to(torch.int32)
+    pool = torch.empty(n + 3, 2, block, kv, dim, dtype=half, device="cuda").normal_(generator=gen)
+    for b, t in enumerate(lens):        # what lies beyond a request is no number
+        j = t // block
+        if t % block and int(tables[b, j]) >= 0:
+            pool[int(tables[b, j]), :, t % block:] = math.nan
+    q = torch.empty(len(lens), kv * group, dim, dtype=half, device="cuda").normal_(0, 2.5, generator=gen)
+    out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+    weights = torch.full(tables.shape, 9.0, device="cuda")
+    cache, d_lens = pgcm.KVCache(pool[:, 0], pool[:, 1]), torch.tensor(lens, dtype=torch.int32).cuda()
+    pgcm.kv_attend(cache, q, tables, d_lens, out, lse=lse, weights=weights)
+    want = _attend_on_gpu(pool, tables, lens, q, dim ** -0.5, group)
+    for got, (value, tol), what in zip((out, lse, weights), want, ("out", "lse", "weights")):
+        ref.within(got, (value.cpu(), tol.cpu()), what)
+    again, alone = torch.empty_like(out), torch.empty_like(out)
+    pgcm.kv_attend(cache, q, tables, d_lens, again)
+    assert torch.equal(out, again)          # without weights, and to the last bit
+    for b in (1, len(lens) - 2):            # a request by itself, cut in other places
+        pgcm.kv_attend(cache, q[b:b + 1], tables[b:b + 1], d_lens[b:b + 1], alone[b:b + 1])
+        ref.within(alone[b], (want[0][0][b].cpu(), want[0][1][b].cpu()), "alone")
