@@ -150,3 +150,19 @@ def test_evict_nothing_asked_for():
     pgcm.kv_evict(w, tables, lens, 16, lens, victims, None, out)
     assert torch.equal(out, tables)
     pgcm.kv_evict(w[:0], tables[:0], lens[:0], 16, lens[:0], victims[:0])
+
+
+@pytest.mark.parametrize("dim,half", [(64, torch.bfloat16), (80, torch.float16), (256, torch.bfloat16)])
+def test_select_rows_of_a_workgroup_each(dim, half):
+    """as many lists as compute units, with room for 385 to 1024 blocks"""
+    rng = np.random.default_rng(dim)
+    lens = [int(v) for v in rng.integers(0, 16 * 300, 32)]
+    lens[3], lens[7], lens[11] = 16 * 1000 - 1, 0, 16 * 700
+    _select(dim + 1, lens, 8, 2, dim, 40, 1, 2, half, most=(1000, 385, 1024)[dim % 3])
+
+
+@pytest.mark.parametrize("dim,group", [(72, 5), (80, 17), (128, 2), (136, 1), (256, 3)])
+@pytest.mark.parametrize("lens,keep", [([16 * 599, 100], 30), ([16 * 5000 - 3, 0, 40, 16 * 700], 300), ([16 * 8190], 7)])
+def test_select_rows_in_parts(dim, group, lens, keep):
+    """scored by many workgroups, sixteen blocks a wavefront or four times as many, before the choice"""
+    _select(dim + keep, lens, 2 if keep != 300 else 4, group, dim, keep, 1, 1, torch.float16 if dim == 80 else torch.bfloat16)
