@@ -851,12 +851,20 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     const uint64_t tiles = (walk_blocks * cache->block_tokens + kTileTokens - 1) / kTileTokens;
     const uint64_t items = (uint64_t)a.requests * a.kv_heads * a.group_tiles, most = tiles * items;
     const uint64_t useful = most > items ? most : items;
-    // Tables with room for few tiles only: a workgroup for each item, which looks at no lengths but its own request's and cuts and
-    // joins nothing (one request of 33 tokens, 40 heads: 4.3 us and 6.4; 8 items of 6 tiles 8.7 and 9.6, of 8 tiles 10.0 and 9.6;
-    // 126 of up to 12 tiles 15.7 and 22.1, 1016 of 64 channels 39.0 and 42.0; 128 of 16 tiles 30.9 and 32.0, 256 of up to 16 of 256
-    // channels 52.9 and 50.8, 1280 of 128 channels 92.8 and 91.0).
-    const bool by_item = items < 1 << 24 &&   // (threads of a grid are counted in 32 bits)
-                         tiles <= (items < kManyItems ? 6u : items <= kCus / 2 ? 16u : 12u);
+    // Room for few tiles only: a workgroup for each item, which looks at no lengths but its own request's and cuts and joins nothing.
+    // Microseconds of that and of equal spans, requests as long as they may be and "ragged" ones (down to a sixteenth), 128 channels:
+    //   one request of 33 tokens, 40 heads 4.3 and 6.4; 8 items, 6 tiles 9.7 and 9.6, 8 tiles 11.6 and 9.7; 48, 8 tiles ragged 11.9 and 10.4
+    //   64 items, 10 tiles 14.4 and 16.3, ragged 14.0 and 13.0, 16 tiles 20.0 and 17.9, ragged 19.8 and 14.4
+    //   128 items, 12 tiles 23.2 and 24.0, ragged 16.4 and 15.7, 16 tiles 31.8 and 31.0; 256, 12 tiles 40.0 and 43.8, ragged 17.9 and 21.4
+    // Of selections, all of one length, with less to know for equal spans: 64 items, 12 tiles 16.3 and 16.6, 16 tiles 20.1 and 18.2;
+    // 96, 14 tiles 20.1 and 24.0, 16 tiles 24.5 and 24.6, 18 tiles 28.5 and 26.4; 128, 16 tiles 30.6 and 30.6; 256, 16 tiles 46 and 54.
+    // Of 256 channels, which have one workgroup a compute unit at a time, few items stay few: selections of 64, 12 tiles 33.7 and
+    // 24.8; of 128, 12 tiles 43.1 and 44.9.
+    const uint32_t few = a.head_dim > 128 ? kCus / 2 : kManyItems;
+    const uint32_t whole_tiles = items < few                  ? 6
+                                 : args->selected != nullptr ? (items < 96 ? 12 : 16)
+                                                             : (items < kCus / 2 ? 10 : 12);
+    const bool by_item = items < 1 << 24 && tiles <= whole_tiles;   // (threads of a grid are counted in 32 bits)
     const uint32_t groups = by_item ? (uint32_t)items : useful > kAttendGroups ? kAttendGroups : (uint32_t)useful;
     if (cache->half == PGCM_KV_F16) launch<F16>(a, groups, by_item, stream);
     else launch<Bf16>(a, groups, by_item, stream);
