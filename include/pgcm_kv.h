@@ -106,6 +106,7 @@ typedef struct {
 /*
  * out = sum over the request's tokens that are on the device of softmax(scale q . k) v; a request without any gives zeros and
  * a lse of minus infinity.  What lies in the pool beyond a request's tokens is not used, whatever it holds.
+ * A score that is NaN or plus infinity makes its head's results NaN, one of minus infinity has no weight.
  * A value that is not finite makes its channel so: infinite, or NaN if infinities of both signs meet.  (Where its weight is
  * less than 2^-100 of the head's largest, infinite or NaN.)
  * weights[b][j] = decay * kept[b][j] + the weights of block j's tokens, summed over the heads.

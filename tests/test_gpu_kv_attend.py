@@ -485,3 +485,34 @@ def test_long_requests_of_all_lengths(dim, kv, group, half, lens):
     for b in (1, len(lens) - 2):            # a request by itself, cut in other places
         pgcm.kv_attend(cache, q[b:b + 1], tables[b:b + 1], d_lens[b:b + 1], alone[b:b + 1])
         ref.within(alone[b], (want[0][0][b].cpu(), want[0][1][b].cpu()), "alone")
+
+
+@pytest.mark.parametrize("half", [F16, BF16])
+def test_scores_that_are_not_finite(half):
+    """minus infinity has no weight, and of a whole request gives none; what is plus infinity or no number spoils its head alone"""
+    r = ref.Requests(23, [40, 40, 2100], 1, 64, half)
+    q = ref.numbers(23, 3, 3, 64).to(half)
+    q[:, 0, 7], q[:, 1, 7], q[:, 2, 7] = 1, -1, 0.5
+    q[1, 2, 7] = 1
+    r.k[int(r.tables[0, 1]), 3, 0, 7] = math.inf
+    r.k[int(r.tables[2, 70]), 3, 0, 7] = -math.inf
+    for j in range(3):
+        r.k[int(r.tables[1, j]), :, 0, 7] = -math.inf
+    for row in (r.most, r.most + 200):
+        wide = copy.copy(r)
+        wide.tables, wide.most = np.pad(r.tables, ((0, 0), (0, row - r.most)), constant_values=-1), row
+        out, lse, _ = _run(wide, q)
+        bad = torch.tensor([[True, False, True], [False, True, False], [False, True, False]])
+        assert torch.equal(lse.isnan().cpu(), bad) and torch.equal(out.isnan().all(-1).cpu(), bad)
+        assert torch.equal(out.isnan().any(-1).cpu(), bad)
+        assert bool((lse[1, ::2] == -math.inf).all()) and bool((out[1, ::2] == 0).all())
+        for b, h, j in ((0, 1, 1), (2, 0, 70), (2, 2, 70)):     # the others: as if that token were not there
+            less = copy.copy(r)
+            less.k = r.k.clone()
+            less.k[int(r.tables[b, j]), 3, 0] = 0
+            want = ref.attend(less, q, 0.125)
+            p0 = (0.0 - want[1][0][b, h]).exp()                 # ... whose score of 0 is taken out again
+            v0 = r.v[int(r.tables[b, j]), 3, 0].double()
+            out_h = (want[0][0][b, h] - p0 * v0) / (1 - p0)
+            tol = (want[0][1][b, h] + ref.UNIT[half] * out_h.abs()) / (1 - p0)
+            ref.within(out[b, h], (out_h, tol), "out")
