@@ -3,9 +3,9 @@
 // Per request, kv head and group of up to sixteen of its query heads (an "item"):
 //   s[t][h] = scale k_t . q_h,   m = max s,   out = sum 2^(s - m) v_t / sum 2^(s - m)     (s in units of log 2)
 // with running m and sums, one pass over K and V.  What bounds it is memory: at sixteen heads an item, 16 flops a byte.
-// Two requests of 131 059 tokens, 8 kv heads of 128 (1.07 GB): 201 us, 5.3 TB/s, each byte read once; a kernel that only reads
-// the same rows takes 192 to 206.  32 of up to 2048 tokens, 40 heads of 128 (396 MB): 86 us, 4.6 TB/s.  One of 33 tokens, 40
-// heads: 4.5 us, the launch and trips to memory one after the other (table, rows).
+// Two requests of 131 059 tokens, 8 kv heads of 128 (1.07 GB): 200 us, 5.4 TB/s, each byte read once; a kernel that only reads
+// the same rows takes 183 to 230, by the order of its loads.  32 of up to 2048 tokens, 40 heads of 128 (396 MB): 86 us, 4.6
+// TB/s.  One of 33 tokens, 40 heads: 4.7 us, the launch and trips to memory one after the other (table, rows).
 //
 // The tiles of all items, 128 tokens each, are cut into equal spans, one for each workgroup, so that neither lengths nor their
 // number matter (short items are left whole); an item of several workgroups is joined by the last of them, in two levels if they
@@ -292,7 +292,8 @@ struct Walk : Layout<kDim> {
 #pragma unroll
                 for (uint32_t j = 0; j < 8; ++j) {
                     const uint32_t word = held.v[p][j][w];
-                    const uint32_t of = ((word & kInf) == kInf ? 0xFFFFu : 0u) | ((word & kInf << 16) == kInf << 16 ? 0xFFFF0000u : 0u);
+                    const uint32_t of = ((word & kInf) == kInf ? 0xFFFFu : 0u) |
+                                        ((word & kInf << 16) == kInf << 16 ? 0xFFFF0000u : 0u);
                     odd[j] = word & of;
                     held.v[p][j][w] = word & ~of;
                 }
@@ -851,15 +852,17 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     const uint64_t tiles = (walk_blocks * cache->block_tokens + kTileTokens - 1) / kTileTokens;
     const uint64_t items = (uint64_t)a.requests * a.kv_heads * a.group_tiles, most = tiles * items;
     const uint64_t useful = most > items ? most : items;
-    // Room for few tiles only: a workgroup for each item, which looks at no lengths but its own request's and cuts and joins nothing.
-    // Microseconds of that and of equal spans, requests as long as they may be and "ragged" ones (down to a sixteenth), 128 channels:
-    //   one request of 33 tokens, 40 heads 4.3 and 6.4; 8 items, 6 tiles 9.7 and 9.6, 8 tiles 11.6 and 9.7; 48, 8 tiles ragged 11.9 and 10.4
-    //   64 items, 10 tiles 14.4 and 16.3, ragged 14.0 and 13.0, 16 tiles 20.0 and 17.9, ragged 19.8 and 14.4
-    //   128 items, 12 tiles 23.2 and 24.0, ragged 16.4 and 15.7, 16 tiles 31.8 and 31.0; 256, 12 tiles 40.0 and 43.8, ragged 17.9 and 21.4
-    // Of selections, all of one length, with less to know for equal spans: 64 items, 12 tiles 16.3 and 16.6, 16 tiles 20.1 and 18.2;
-    // 96, 14 tiles 20.1 and 24.0, 16 tiles 24.5 and 24.6, 18 tiles 28.5 and 26.4; 128, 16 tiles 30.6 and 30.6; 256, 16 tiles 46 and 54.
-    // Of 256 channels, which have one workgroup a compute unit at a time, few items stay few: selections of 64, 12 tiles 33.7 and
-    // 24.8; of 128, 12 tiles 43.1 and 44.9.
+    // Room for few tiles only: a workgroup for each item, which looks at no lengths but its own request's and cuts and joins
+    // nothing.  Microseconds of that and of equal spans, requests as long as they may be and "ragged" ones (down to a
+    // sixteenth), 128 channels:
+    //   one request of 33 tokens, 40 heads 4.3 and 6.4; 8 items, 6 tiles 9.7 and 9.6, 8 tiles 11.6 and 9.7; 48, 8 tiles ragged
+    //   11.9 and 10.4; 64, 10 tiles 14.4 and 16.3, ragged 14.0 and 13.0, 16 tiles 20.0 and 17.9, ragged 19.8 and 14.4
+    //   128, 12 tiles 23.2 and 24.0, ragged 16.4 and 15.7, 16 tiles 31.8 and 31.0; 256, 12 tiles 40.0 and 43.8, ragged 17.9
+    //   and 21.4
+    // Of selections, all of one length, with less to know for equal spans: 64 items, 12 tiles 16.3 and 16.6, 16 tiles 20.1 and
+    // 18.2; 96, 14 tiles 20.1 and 24.0, 16 tiles 24.5 and 24.6, 18 tiles 28.5 and 26.4; 128, 16 tiles 30.6 and 30.6; 256, 16
+    // tiles 46 and 54.  Of 256 channels, with one workgroup a compute unit at a time: selections of 64, 12 tiles 33.7 and 24.8;
+    // of 128, 12 tiles 43.1 and 44.9.
     const uint32_t few = a.head_dim > 128 ? kCus / 2 : kManyItems;
     const uint32_t whole_tiles = items < few                  ? 6
                                  : args->selected != nullptr ? (items < 96 ? 12 : 16)
