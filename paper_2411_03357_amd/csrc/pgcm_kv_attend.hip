@@ -182,18 +182,23 @@ struct Held : Layout<kDim> {
                 }
             }
     }
-    // whether any of the wavefront's values is not finite: their sizes as whole numbers, two an instruction (memory hides it: two
-    // requests of 131 059 tokens take 199.6 us, without 200.3)
-    __device__ __forceinline__ bool odd() const {
-        u16x2 most = (u16x2)(uint16_t)0;
+    // Finite, or in some lane not if any of the wavefront's values is not: their products with whatever is at hand, as the matrix
+    // cores make them beside those of the scores, which wait for each other.  Rows that are not there, queries that are not
+    // finite and sums beyond the range of binary32 may make it infinite or NaN, which costs time alone.  (12 requests of up to
+    // 1000 tokens, 8 kv heads of 256: 19.9 us, by dot products with zero 20.6, without 19.1; two of 131 059 tokens equal.)
+    __device__ __forceinline__ float probe(typename H::eight by) const {
+        f32x4 sums[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (uint32_t p = 0; p < L::kParts; ++p)
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j)
-#pragma unroll
-                for (uint32_t w = 0; w < L::kWords; ++w)
-                    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[p][j][w] & 0x7FFF7FFFu));
-        return __any(most.x >= H::kInfinity || most.y >= H::kInfinity);
+            for (uint32_t j = 0; j < 8; j += 4 / L::kWords) {   // (as they came from LDS: no register moves)
+                const uint32_t n = j / (4 / L::kWords) % 2;
+                const uint4 x = L::kWords == 4 ? make_uint4(v[p][j][0], v[p][j][1], v[p][j][L::kWords - 2], v[p][j][L::kWords - 1])
+                                               : make_uint4(v[p][j][0], v[p][j][1], v[p][j + 1 & 7][0], v[p][j + 1 & 7][1]);
+                sums[n] = H::product(as_eight<H>(x), by, sums[n]);
+            }
+        sums[0] += sums[1];
+        return (sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3]);
     }
     // rows of tokens that are not there count as zero, whatever they hold
     __device__ __forceinline__ void drop_v(uint32_t which, uint32_t valid, uint32_t g) {
@@ -230,14 +235,17 @@ struct Walk : Layout<kDim> {
             if (there && (kExact || d < a.head_dim)) q[c] = *(const uint4*)(row + 2 * d);
         }
     }
-    __device__ __forceinline__ void scores(float (&s)[8], const Held<H, kDim, kExact>& held, float scale, uint32_t valid0,
-                                           uint32_t valid1, uint32_t g) const {
+    // ... and the values' probe, in the products' shadow
+    __device__ __forceinline__ float scores(float (&s)[8], const Held<H, kDim, kExact>& held, float scale, uint32_t valid0,
+                                            uint32_t valid1, uint32_t g) const {
         f32x4 s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (uint32_t c = 0; c < L::kSteps; ++c) {
             s0 = H::product(as_eight<H>(held.k[0][c]), as_eight<H>(q[c]), s0);
             s1 = H::product(as_eight<H>(held.k[1][c]), as_eight<H>(q[c]), s1);
         }
+        float probe = held.probe(as_eight<H>(q[0]));
+        asm volatile("" : "+v"(probe));   // (it would be made where it is looked at)
 #pragma unroll
         for (uint32_t r = 0; r < 4; ++r) s[r] = s0[r] * scale, s[4 + r] = s1[r] * scale;
         if (valid0 < kPiece || valid1 < kPiece) {
@@ -247,6 +255,7 @@ struct Walk : Layout<kDim> {
                 s[4 + r] = 4 * g + r < valid1 ? s[4 + r] : -INFINITY;
             }
         }
+        return probe;
     }
     // Sums are kept relative to 2^top, which makes the largest weight so far 2^H::kLargest when they were last brought up to
     // it, and at most 2^H::kOverflows before the next time: a new maximum rarely takes that.  The scores become weights.
@@ -301,8 +310,8 @@ struct Walk : Layout<kDim> {
                 sum[p][2 * w + 1] = H::product(channel(odd, 1), any, sum[p][2 * w + 1]);
             }
     }
-    __device__ __forceinline__ void add_v(const float (&s)[8], Held<H, kDim, kExact>& held) {
-        if (__builtin_expect(held.odd(), false)) add_odd(s, held);
+    __device__ __forceinline__ void add_v(const float (&s)[8], Held<H, kDim, kExact>& held, float probe) {
+        if (__builtin_expect(__any(!(fabsf(probe) < INFINITY)), false)) add_odd(s, held);
         // A weight goes to the matrix cores in halves, each of what the ones before leave: in bfloat16 all of its 24 bits, in
         // float16 at least 22.  (Two of 8 bits each were off by up to 2^-17 of a sum's size where values cancel, and three cost
         // little beside memory: two requests of 131 059 tokens 200.3 us, with two 199.2.)
@@ -550,7 +559,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
             }
             if (some_left || ahead) ask();
             float s[8];
-            walk.scores(s, held, a.scale, here0, here1, g);
+            const float probe = walk.scores(s, held, a.scale, here0, here1, g);
             walk.weigh(s);
             if (a.piece_lse != nullptr) {
                 const float w0 = over_rows_sum((s[0] + s[1]) + (s[2] + s[3]));
@@ -567,7 +576,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void attend_kernel(A
                 held.drop_v(0, here0, g);
                 held.drop_v(1, here1, g);
             }
-            walk.add_v(s, held);
+            walk.add_v(s, held, probe);
         }
         if (more && !turned) {
             use_pieces(next_pieces, next);

@@ -516,3 +516,12 @@ def test_scores_that_are_not_finite(half):
             out_h = (want[0][0][b, h] - p0 * v0) / (1 - p0)
             tol = (want[0][1][b, h] + ref.UNIT[half] * out_h.abs()) / (1 - p0)
             ref.within(out[b, h], (out_h, tol), "out")
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_large_finite_values(dim):
+    """... whose products with a query leave the range of binary32: they are looked at again, and count as they are"""
+    r = ref.Requests(24, [300, 1, 40], 2, dim, BF16)
+    r.v, r.k = r.v * 2.0 ** 80, r.k * 2.0 ** -60
+    q = (ref.numbers(24, 3, 6, dim) * 2.0 ** 60).to(BF16)
+    _check(r, q)
