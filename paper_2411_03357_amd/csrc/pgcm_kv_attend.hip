@@ -862,20 +862,22 @@ int pgcm_kv_attend(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_atte
     const uint64_t items = (uint64_t)a.requests * a.kv_heads * a.group_tiles, most = tiles * items;
     const uint64_t useful = most > items ? most : items;
     // Room for few tiles only: a workgroup for each item, which looks at no lengths but its own request's and cuts and joins
-    // nothing.  Microseconds of that and of equal spans, requests as long as they may be and "ragged" ones (down to a
-    // sixteenth), 128 channels:
-    //   one request of 33 tokens, 40 heads 4.3 and 6.4; 8 items, 6 tiles 9.7 and 9.6, 8 tiles 11.6 and 9.7; 48, 8 tiles ragged
-    //   11.9 and 10.4; 64, 10 tiles 14.4 and 16.3, ragged 14.0 and 13.0, 16 tiles 20.0 and 17.9, ragged 19.8 and 14.4
-    //   128, 12 tiles 23.2 and 24.0, ragged 16.4 and 15.7, 16 tiles 31.8 and 31.0; 256, 12 tiles 40.0 and 43.8, ragged 17.9
-    //   and 21.4
-    // Of selections, all of one length, with less to know for equal spans: 64 items, 12 tiles 16.3 and 16.6, 16 tiles 20.1 and
-    // 18.2; 96, 14 tiles 20.1 and 24.0, 16 tiles 24.5 and 24.6, 18 tiles 28.5 and 26.4; 128, 16 tiles 30.6 and 30.6; 256, 16
-    // tiles 46 and 54.  Of 256 channels, with one workgroup a compute unit at a time: selections of 64, 12 tiles 33.7 and 24.8;
-    // of 128, 12 tiles 43.1 and 44.9.
-    const uint32_t few = a.head_dim > 128 ? kCus / 2 : kManyItems;
-    const uint32_t whole_tiles = items < few                  ? 6
-                                 : args->selected != nullptr ? (items < 96 ? 12 : 16)
-                                                             : (items < kCus / 2 ? 10 : 12);
+    // nothing.  Microseconds of that and of the general kernel, for rows that are full and "ragged" ones (down to a sixteenth):
+    //   one request of 33 tokens, 40 heads of 128: 4.3 and 6.4
+    //   128 channels  8 items, 6 tiles 9.7 and 9.6, 8 tiles 11.6 and 9.7; 32, 6 tiles 10.2 and 10.5, ragged 9.6 and 10.4, 8 tiles
+    //                 12.1 and 11.6, ragged 11.5 and 10.6; 96, 8 tiles 12.7 and 15.3, ragged 12.1 and 15.1, 10 tiles 14.5 and
+    //                 17.9, ragged 14.0 and 13.3, 12 tiles 16.4 and 19.8, ragged 15.8 and 13.8; 64, 16 tiles 20.0 and 17.9,
+    //                 ragged 19.8 and 14.4; 160, 12 tiles 27.6 and 30.4, ragged 16.4 and 18.6; 256, 16 tiles 51.7 and 53.7,
+    //                 ragged 22.8 and 24.2, but 512 99.6 and 97.9, 46.4 and 45.9
+    //   256 channels  96 items, 8 tiles 27.4 and 30.7, ragged 20.4 and 25.4, 10 tiles 34.6 and 35.8, ragged 23.8 and 21.7; 160,
+    //                 12 tiles 50.3 and 56.3, ragged 30.6 and 29.6
+    // Lists of a selection are as good as full, and worth more tiles: 64 items, 12 tiles 16.3 and 16.6, 16 tiles 20.1 and 18.2;
+    // 96, 14 tiles 20.1 and 24.0, 16 tiles 24.5 and 24.6, 18 tiles 28.5 and 26.4; 128, 16 tiles 30.6 and 30.6; 256, 16 tiles 46
+    // and 54; of 256 channels 64 items, 12 tiles 33.7 and 24.8, 128, 12 tiles 43.1 and 44.9.
+    const bool wide = a.head_dim > 128, many = items >= kCus / 2;
+    const uint32_t whole_tiles = items < kManyItems          ? 6
+                                 : args->selected == nullptr ? (many ? 12 : wide ? 8 : 10)
+                                                             : (many || (items >= 96 && !wide) ? 16 : wide ? 10 : 12);
     const bool by_item = items < 1 << 24 && tiles <= whole_tiles;   // (threads of a grid are counted in 32 bits)
     const uint32_t groups = by_item ? (uint32_t)items : useful > kAttendGroups ? kAttendGroups : (uint32_t)useful;
     if (cache->half == PGCM_KV_F16) launch<F16>(a, groups, by_item, stream);
