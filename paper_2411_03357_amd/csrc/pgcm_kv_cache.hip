@@ -87,6 +87,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     const uint32_t half = a.rope_dim / 2;
     const bool turned = a.rope != nullptr && d < a.rope_dim;
     const bool halves = a.rope != nullptr && a.adjacent == 0;
+    const uint32_t taken = turned ? ~0u : 0u;  // of a pair's other channel
     uint32_t partner = part;                   // the lane with the other channels of the pairs
     if (halves && turned) partner = d < half ? part + half / 8 : part - half / 8;
     // weights of queries' channels and of keys', and those of the partner's
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) {
                 own[k][e] = (there ? (float)x[e] : 1.f) * c[e];
-                other[k][e] = (there ? (float)(a.adjacent ? x[e ^ 1] : y[e]) : 1.f) * s[e];
+                other[k][e] = turned ? (there ? (float)(a.adjacent ? x[e ^ 1] : y[e]) : 1.f) * s[e] : 0.f;
             }
         }
     }
@@ -147,37 +148,39 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
         if (step < steps) words = load(step);  // under way while this step is worked on
         const Head h = head_of(this_step);
         uint4 result = now;
-        if (this_step < of_q + of_k) {
-            const uint32_t k = this_step < of_q ? 0 : 1;
+        const uint32_t k = this_step < of_q ? 0 : 1;
+        const bool normed = (k == 0 ? a.q_weight : a.k_weight) != nullptr;
+        if (this_step < of_q + of_k && (normed || a.rope != nullptr)) {   // (others are copied)
             const typename H::eight x = as_eight<H>(now);
             float by = 1.f;
-            if ((k == 0 ? a.q_weight : a.k_weight) != nullptr) {
+            if (normed) {
                 float sum = 0.f;
 #pragma unroll
                 for (uint32_t e = 0; e < 8; ++e) sum += (float)x[e] * (float)x[e];
                 sum = over_lanes(sum, a.row_power, [](float x, float y) { return x + y; });
                 by = __builtin_amdgcn_rsqf(sum * a.by_dim + a.eps);   // (to one unit in the last place)
             }
-            typename H::eight y = x;
+            uint4 pairs = now;
             if (halves) {
-                uint4 far;
                 if (across) {
-                    far.x = __builtin_amdgcn_update_dpp(0, now.x, kAround, 0xF, 0xF, true);
-                    far.y = __builtin_amdgcn_update_dpp(0, now.y, kAround, 0xF, 0xF, true);
-                    far.z = __builtin_amdgcn_update_dpp(0, now.z, kAround, 0xF, 0xF, true);
-                    far.w = __builtin_amdgcn_update_dpp(0, now.w, kAround, 0xF, 0xF, true);
+                    pairs.x = __builtin_amdgcn_update_dpp(0, now.x, kAround, 0xF, 0xF, true);
+                    pairs.y = __builtin_amdgcn_update_dpp(0, now.y, kAround, 0xF, 0xF, true);
+                    pairs.z = __builtin_amdgcn_update_dpp(0, now.z, kAround, 0xF, 0xF, true);
+                    pairs.w = __builtin_amdgcn_update_dpp(0, now.w, kAround, 0xF, 0xF, true);
                 } else {
                     const uint32_t at = lane - part + partner;
-                    far.x = __shfl(now.x, at), far.y = __shfl(now.y, at), far.z = __shfl(now.z, at), far.w = __shfl(now.w, at);
+                    pairs.x = __shfl(now.x, at), pairs.y = __shfl(now.y, at), pairs.z = __shfl(now.z, at), pairs.w = __shfl(now.w, at);
                 }
-                y = as_eight<H>(far);
             }
+            // (channels that are not rotated take nothing from others, and infinity times nothing is no number)
+            pairs.x &= taken, pairs.y &= taken, pairs.z &= taken, pairs.w &= taken;
+            const typename H::eight y = as_eight<H>(pairs);
             typename H::eight z;
             auto turn = [&](const float(&c)[8], const float(&s)[8]) {
 #pragma unroll
                 for (uint32_t e = 0; e < 8; ++e) {
-                    const float pair = (float)(a.adjacent ? x[e ^ 1] : y[e]), own = (float)x[e] * c[e];
-                    z[e] = (typename H::one)((turned ? own + pair * s[e] : own) * by);   // (0 times infinity is no number)
+                    const float pair = (float)(a.adjacent ? y[e ^ 1] : y[e]);
+                    z[e] = (typename H::one)(((float)x[e] * c[e] + pair * s[e]) * by);
                 }
             };
             if (k == 0) turn(own[0], other[0]);

@@ -201,3 +201,23 @@ def test_append_a_table_without_lines():
             pgcm.kv_append(pgcm.KVCache(pool[:, 0], pool[:, 1]), None, x[:, :2], x[:, 2:], at, torch.tensor([1, 2]).cuda(), None,
                            rope=torch.empty(shape, device="cuda"))
         assert e.value.status == -1
+
+
+@pytest.mark.parametrize("half", [F16, BF16])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("dim,rope_dim", [(128, 0), (128, 48), (80, 16)])
+def test_append_copies_what_is_neither_normed_nor_rotated(half, adjacent, dim, rope_dim):
+    """numbers below the normal ones, infinities; without rotation to the last bit, zeros of both signs among them"""
+    bits = np.random.default_rng(dim).integers(-(1 << 15), 1 << 15, (9, 6, dim)).astype(np.int16)
+    bits[:, :, -1], bits[:, :, -2], bits[:, :, -3] = -32768, 0, 1
+    x = torch.from_numpy(bits).view(half)
+    x[x.isnan()] = -0.0
+    packed = x.cuda()
+    pool = torch.zeros(1, 2, 16, 2, dim, dtype=half, device="cuda")
+    out = torch.empty(9, 2, dim, dtype=half, device="cuda")
+    at = torch.zeros(9, dtype=torch.int32).cuda() if rope_dim else None
+    pgcm.kv_append(pgcm.KVCache(pool[:, 0], pool[:, 1]), packed[:, :2], packed[:, 2:4], packed[:, 4:], at,
+                   torch.arange(9).cuda(), out, rope=_table(3, rope_dim).cuda() if rope_dim else None, adjacent=adjacent)
+    for got, want in ((out, x[:, :2]), (pool[0, 0, :9], x[:, 2:4]), (pool[0, 1, :9], x[:, 4:])):
+        got, want = [x[..., rope_dim:].cpu().contiguous() for x in (got, want)]
+        assert torch.equal(got, want) and (rope_dim != 0 or torch.equal(got.view(torch.int16), want.view(torch.int16)))
