@@ -1,6 +1,7 @@
 // Native marshalling of the operators on KV blocks (kv.py): a torch extension, as what a tensor is takes five calls of the
 // interpreter to ask it and some nanoseconds to read (an append of nine tensors: 6.1 us of the host and 4.0).  Each call gives
 // the status, or None for anything unusual, which the Python code then names.
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -58,10 +59,22 @@ struct Tensor {
     }
 };
 
-// Arguments one after the other, the current device first; good() turns false for good at the first one that is unusual.
+// Arguments one after the other, the current device or None for it first; good() turns false for good at the first one that is
+// unusual.
 class Arguments {
   public:
-    Arguments(PyObject* const* args, Py_ssize_t n) : args_(args), n_(n) { device_ = number(); }
+    Arguments(PyObject* const* args, Py_ssize_t n) : args_(args), n_(n) {
+        if (n > 0 && args[0] == Py_None) {
+            ++at_;
+            try {
+                device_ = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index();
+            } catch (...) {   // (a torch without GPUs)
+                good_ = false;
+            }
+        } else {
+            device_ = number();
+        }
+    }
     ~Arguments() {
         if (!good_) PyErr_Clear();
     }

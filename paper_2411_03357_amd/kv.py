@@ -215,7 +215,7 @@ def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=N
     if not k.is_cuda:
         raise ValueError("k must be a CUDA tensor")
     h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_append(_device(), cache._at, q, k, v, positions, slots, q_out, q_weight,
+    status = (_marshal or _native()).kv_append(None, cache._at, q, k, v, positions, slots, q_out, q_weight,
                                                k_weight, eps, rope, 1 if adjacent else 0, h)
     if status is not None:
         if status:
@@ -257,7 +257,7 @@ def kv_attend(cache, q, tables, lens, out, lse=None, scale=None, selected=None, 
     if scale is None:
         scale = cache.head_dim ** -0.5
     space = (workspace or kv_workspace(h))._h
-    status = (_marshal or _native()).kv_attend(_device(), space, cache._at, q, tables, lens, out, lse, scale, selected,
+    status = (_marshal or _native()).kv_attend(None, space, cache._at, q, tables, lens, out, lse, scale, selected,
                                                weights, kept, decay, h)
     if status is not None:
         if status:
@@ -289,7 +289,7 @@ def kv_summarize(cache, blocks, counts, bounds, scales, entries=None, stream=Non
     if not blocks.is_cuda:
         raise ValueError("blocks must be a CUDA tensor")
     h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_summarize(_device(), cache._at, blocks, counts, bounds, scales, entries, h)
+    status = (_marshal or _native()).kv_summarize(None, cache._at, blocks, counts, bounds, scales, entries, h)
     if status is not None:
         if status:
             _check(status)
@@ -311,7 +311,7 @@ def kv_select(q, tables, lens, bounds, scales, block_tokens, selected, counts=No
         raise ValueError("q must be a CUDA tensor")
     h = _stream_handle(stream)
     space = (workspace or kv_workspace(h))._h
-    status = (_marshal or _native()).kv_select(_device(), space, _HALVES.get(q.dtype, 0), q, tables, lens, bounds, scales,
+    status = (_marshal or _native()).kv_select(None, space, _HALVES.get(q.dtype, 0), q, tables, lens, bounds, scales,
                                                block_tokens, selected, counts, first, last, h)
     if status is not None:
         if status:
@@ -337,7 +337,7 @@ def kv_evict(weights, tables, lens, block_tokens, evict, victims, victim_blocks=
     if not weights.is_cuda:
         raise ValueError("weights must be a CUDA tensor")
     h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_evict(_device(), weights, tables, lens, block_tokens, evict, victims, victim_blocks,
+    status = (_marshal or _native()).kv_evict(None, weights, tables, lens, block_tokens, evict, victims, victim_blocks,
                                               tables_out, first, last, blocks, h)
     if status is not None:
         if status:

@@ -58,7 +58,7 @@ def test_the_native_marshalling_compares_devices(monkeypatch, op):
     monkeypatch.setattr(pgcm.kv, "_device", lambda: 1)      # as if another device were the current one
     given = []
     native = kv._native()
-    watched = types.SimpleNamespace(**{"kv_" + n: lambda *a, n=n: given.append(getattr(native, "kv_" + n)(*a)) or given[-1]
+    watched = types.SimpleNamespace(**{"kv_" + n: lambda *a, n=n: given.append(getattr(native, "kv_" + n)(1, *a[1:])) or given[-1]
                                        for n in ("append", "attend", "summarize", "select", "evict")})
     monkeypatch.setattr(kv, "_marshal", watched)
     with pytest.raises(ValueError, match="is on cuda:0, and the current device is cuda:1"):
