@@ -1,0 +1,74 @@
+/*
+ * pgcm_kv8: KV blocks in 8 bits.  What a block's encryption, its way over the bus and its
+ * reading cost goes by its bytes (paper section 2.1 on what is swapped); in 8 bits they are half as many.
+ *
+ *   pgcm_kv8_append   norms of queries and keys per head, rotation, keys and values into their slots in 8 bits
+ *   pgcm_kv8_store    blocks of halves (pgcm_kv.h) to blocks in 8 bits
+ *   pgcm_kv8_load     ... and back
+ *
+ * A cache in 8 bits (pgcm_kv8_cache) has codes where pgcm_kv_cache has halves, and for each block and kv head a scale of its
+ * keys and one of its values: a value is its code times the scale.  For codes and scales in one piece, as one chunk for
+ * pgcm_encrypt_batch takes them, the scales' strides may step over the codes.
+ *
+ * Codes are whole numbers from -127 to 127 (PGCM_KV8_INT8) or numbers of 4 bits of exponent and 3 of fraction, up to 448
+ * (PGCM_KV8_E4M3).  Scales that this library writes are powers of two, 2^e with the least e from -100 on for which 2^e times
+ * 127 or 448 reaches the largest |x| of the block's tokens and of the head; a code is x / 2^e, rounded once, to nearest, ties to even.
+ * So reading back is exact in binary32, and in halves but for the ends of their range; and a scale that has to grow while a
+ * block fills doubles, so that the codes that are there are rounded again at most once for each doubling, which adds up to
+ * less than one step of the last scale in int8, and in e4m3 changes only codes that fall below its least normal number.
+ * If a value is infinite or NaN the head's scale of that block is NaN, and the codes that come with it are zero: nothing that is
+ * read from there is taken for a number.
+ *
+ * Conventions are those of pgcm.h and pgcm_kv.h, alignment among them: rows of codes are 16-byte aligned, with
+ * strides that are multiples of 16, head_dim is a multiple of 16 here.  Results do not depend on the order in which workgroups run.
+ */
+#ifndef PGCM_KV8_H
+#define PGCM_KV8_H
+
+#include "pgcm_kv.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { PGCM_KV8_INT8 = 0, PGCM_KV8_E4M3 = 1 } pgcm_kv8_code;
+
+typedef struct {
+    void *k, *v;                 /* DEVICE codes */
+    float *k_scales, *v_scales;  /* DEVICE */
+    uint32_t code;               /* pgcm_kv8_code */
+    uint32_t half;               /* pgcm_kv_half: of queries, keys and values that go in and of what comes out */
+    uint32_t blocks;             /* of the pool, at least 1 */
+    uint32_t block_tokens;
+    uint32_t kv_heads;
+    uint32_t head_dim;           /* a multiple of 16 up to 256 */
+    int64_t k_block, k_token, k_head; /* strides in codes */
+    int64_t v_block, v_token, v_head;
+    int64_t k_scale_block, k_scale_head, v_scale_block, v_scale_head; /* in floats */
+} pgcm_kv8_cache;
+
+/*
+ * As pgcm_kv_append, with k and v rounded once, to their codes.  Tokens of the call whose slots lie in one block follow each other
+ * in `slots`, each slot one more than the one before; a call names each block in one such run.  A run that begins with its
+ * block's first token starts the block anew; any other raises the block's scales, where its values need that, from what they
+ * are (never lowers them), and then the codes of the tokens before the run are rounded to the new scale.  What the block holds
+ * behind the run no longer counts.  A slot outside the pool is not written.
+ */
+int pgcm_kv8_append(const pgcm_kv8_cache *cache, const pgcm_kv_append_args *args, void *hip_stream);
+
+/*
+ * n blocks' first tokens, from `from` (block from_blocks[i], or blocks[i] if NULL) to `to` (block blocks[i]).  counts: DEVICE
+ * [n], tokens of each (cut to [0, block_tokens]), or NULL: all.  Both caches have the same sizes but for the number of blocks, and
+ * one `half`.  A block outside its pool is passed over; no block of `to` is named twice.  Store starts each block anew, with the
+ * scales of those tokens; places behind them are left as they are, in both directions.  Load rounds once to a half; what
+ * would exceed its range, at most by that rounding, becomes its largest number.
+ */
+int pgcm_kv8_store(const pgcm_kv8_cache *to, const pgcm_kv_cache *from, uint32_t n, const int32_t *blocks, const int32_t *counts,
+                   const int32_t *from_blocks, void *hip_stream);
+int pgcm_kv8_load(const pgcm_kv8_cache *from, const pgcm_kv_cache *to, uint32_t n, const int32_t *blocks, const int32_t *counts,
+                  const int32_t *to_blocks, void *hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* PGCM_KV8_H */

@@ -13,12 +13,16 @@ from .binding import (PgcmError, Key, expand_key, expand_key_bytes, encrypt_batc
 
 _KV = ("KVCache", "KVWorkspace", "kv_workspace", "kv_append", "kv_attend", "kv_summarize", "kv_select", "kv_evict",
        "KV_EXPORTS")
+_KV8 = ("KV8Cache", "kv8_append", "kv8_store", "kv8_load", "KV8_EXPORTS")
 
 
 def __getattr__(name):
     # the operators on KV blocks take torch tensors; what works without torch does not import it
-    if name not in _KV:
+    if name in _KV:
+        from . import kv as of
+    elif name in _KV8:
+        from . import kv8 as of
+    else:
         raise AttributeError("module %r has no attribute %r" % (__name__, name))
-    from . import kv
-    globals().update({n: getattr(kv, n) for n in _KV})
+    globals().update({n: getattr(of, n) for n in (_KV if name in _KV else _KV8)})
     return globals()[name]

@@ -11,15 +11,17 @@ LIB = os.path.join(HERE, "libpgcm.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 KV_MARSHAL = os.path.join(HERE, "_kv_marshal.so")    # a torch extension; the rest does without torch
 SOURCES = ["pgcm_kernels.hip", "pgcm_bitsliced.hip", "pgcm_host.hip", "pgcm_bounce.hip", "pgcm_pipe.hip",
-           "pgcm_seq.cpp", "pgcm_kv.hip", "pgcm_kv_attend.hip", "pgcm_kv_cache.hip", "pgcm_kv_choose.hip"]
+           "pgcm_seq.cpp", "pgcm_kv.hip", "pgcm_kv_attend.hip", "pgcm_kv_cache.hip", "pgcm_kv_choose.hip",
+           "pgcm_kv8_cache.hip"]
 HEADERS = ["pgcm_kernels.h", "pgcm_types.h", "pgcm_arrive.h", "pgcm_contexts.h", "pgcm_one_launch.h",
            "pgcm_spans.h", "pgcm_routes.h", "pgcm_host_ivs.h", "pgcm_bitsliced_gen.h",
-           "pgcm_kv_common.h",
+           "pgcm_kv_common.h", "pgcm_kv8_common.h",
            os.path.join("..", "..", "include", "pgcm.h"),
            os.path.join("..", "..", "include", "pgcm_seq.h"),
            os.path.join("..", "..", "include", "pgcm_bounce.h"),
            os.path.join("..", "..", "include", "pgcm_pipe.h"),
-           os.path.join("..", "..", "include", "pgcm_kv.h")]
+           os.path.join("..", "..", "include", "pgcm_kv.h"),
+           os.path.join("..", "..", "include", "pgcm_kv8.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",

@@ -1,4 +1,4 @@
-// Native marshalling of the operators on KV blocks (kv.py): a torch extension, as what a tensor is takes five calls of the
+// Native marshalling of the operators on KV blocks (kv.py, kv8.py): a torch extension, as what a tensor is takes five calls of the
 // interpreter to ask it and some nanoseconds to read (an append of nine tensors: 6.1 us of the host and 4.0).  Each call gives
 // the status, or None for anything unusual, which the Python code then names.
 #include <c10/core/impl/DeviceGuardImplInterface.h>
@@ -7,7 +7,7 @@
 #include <cstdint>
 
 #include "../../include/pgcm.h"
-#include "../../include/pgcm_kv.h"
+#include "../../include/pgcm_kv8.h"
 
 namespace {
 
@@ -18,10 +18,20 @@ struct KvCalls {
     decltype(&pgcm_kv_select) select;
     decltype(&pgcm_kv_evict) evict;
 } g_kv;
+struct Kv8Calls {
+    decltype(&pgcm_kv8_append) append;
+    decltype(&pgcm_kv8_store) store;
+    decltype(&pgcm_kv8_load) load;
+} g_kv8;
 
 // A cache as kv.py hands it over: with the device that it is on.
 struct Cache {
     pgcm_kv_cache c;
+    int64_t device;
+};
+
+struct Cache8 {
+    pgcm_kv8_cache c;
     int64_t device;
 };
 
@@ -88,11 +98,8 @@ class Arguments {
         return p;
     }
     // on the current device
-    const pgcm_kv_cache* cache() {
-        const auto* cache = (const Cache*)address();
-        if (cache == nullptr || cache->device != device_) good_ = false;
-        return good_ ? &cache->c : nullptr;
-    }
+    const pgcm_kv_cache* cache() { return placed<Cache>(); }
+    const pgcm_kv8_cache* cache8() { return placed<Cache8>(); }
     uint32_t number() {
         PyObject* o = next();
         if (o == nullptr || !PyLong_Check(o)) return refuse();
@@ -121,6 +128,12 @@ class Arguments {
     void need(bool is) { good_ = good_ && is; }
 
   private:
+    template <class Placed>
+    auto placed() -> decltype(&((const Placed*)nullptr)->c) {
+        const auto* cache = (const Placed*)address();
+        if (cache == nullptr || cache->device != device_) good_ = false;
+        return good_ ? &cache->c : nullptr;
+    }
     PyObject* next() {
         if (!good_ || at_ >= n_) {
             good_ = false;
@@ -149,10 +162,9 @@ PyObject* called(Call call) {
     return PyLong_FromLong(status);
 }
 
-// (device, cache, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope, adjacent, stream) -> status or None
-PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    Arguments in(args, nargs);
-    const pgcm_kv_cache* cache = in.cache();
+// the arguments of an append but for the cache, and the call with them
+template <class Cache, class Call>
+PyObject* append_to(Arguments& in, const Cache* cache, Call call) {
     if (cache == nullptr) Py_RETURN_NONE;
     const at::ScalarType half = half_of(cache->half);
     const int64_t d = cache->head_dim, kv = cache->kv_heads;
@@ -183,7 +195,38 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     a.positions = turned ? (const int32_t*)positions.at : nullptr, a.slots = (const int64_t*)slots.at;
     a.q_weight = q_weight.at, a.k_weight = k_weight.at, a.rope = (const float*)rope.given();
     a.rope_positions = (uint32_t)rope.shape[0], a.rope_dim = (uint32_t)rope.shape[1];
-    return called([&] { return g_kv.append(cache, &a, stream); });
+    return called([&] { return call(cache, &a, stream); });
+}
+
+// (device, cache, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope, adjacent, stream) -> status or None
+PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    Arguments in(args, nargs);
+    return append_to(in, in.cache(), g_kv.append);
+}
+PyObject* kv8_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    Arguments in(args, nargs);
+    return append_to(in, in.cache8(), g_kv8.append);
+}
+
+// (device, cache8, cache, blocks, counts, others, stream) -> status or None
+template <bool kStore>
+PyObject* kv8_move(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    Arguments in(args, nargs);
+    const pgcm_kv8_cache* cache8 = in.cache8();
+    const pgcm_kv_cache* cache = cache8 == nullptr ? nullptr : in.cache();
+    if (cache == nullptr) Py_RETURN_NONE;
+    Tensor blocks, counts, others;
+    in.tensor(&blocks, at::kInt, 1, true);
+    const int64_t n = blocks.shape[0];
+    if (in.tensor(&counts, at::kInt, 1, true, true)) in.need(counts.is(n));
+    if (in.tensor(&others, at::kInt, 1, true, true)) in.need(others.is(n));
+    void* stream = in.address();
+    in.need(n <= 0xFFFFFFFFll);
+    if (!in.all_taken()) Py_RETURN_NONE;
+    return called([&] {
+        return (kStore ? g_kv8.store : g_kv8.load)(cache8, cache, (uint32_t)n, (const int32_t*)blocks.at,
+                                                   (const int32_t*)counts.at, (const int32_t*)others.at, stream);
+    });
 }
 
 // (device, workspace, cache, q, tables, lens, out, lse, scale, selected, weights, kept, decay, stream) -> status or None
@@ -317,6 +360,19 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
+// bind8(the addresses of Kv8Calls, in their order)
+PyObject* bind8(PyObject*, PyObject* args) {
+    PyObject* f[3];
+    if (!PyArg_ParseTuple(args, "OOO", &f[0], &f[1], &f[2])) return nullptr;
+    void* at[3];
+    for (int i = 0; i < 3; ++i) at[i] = PyLong_AsVoidPtr(f[i]);
+    if (PyErr_Occurred()) return nullptr;
+    g_kv8.append = reinterpret_cast<decltype(g_kv8.append)>(at[0]);
+    g_kv8.store = reinterpret_cast<decltype(g_kv8.store)>(at[1]);
+    g_kv8.load = reinterpret_cast<decltype(g_kv8.load)>(at[2]);
+    Py_RETURN_NONE;
+}
+
 template <PyObject* (*kCall)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyCFunction fast() {
     return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kCall));
@@ -328,6 +384,10 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"kv_summarize", fast<kv_summarize>(), METH_FASTCALL, nullptr},
                          {"kv_select", fast<kv_select>(), METH_FASTCALL, nullptr},
                          {"kv_evict", fast<kv_evict>(), METH_FASTCALL, nullptr},
+                         {"bind8", bind8, METH_VARARGS, nullptr},
+                         {"kv8_append", fast<kv8_append>(), METH_FASTCALL, nullptr},
+                         {"kv8_store", fast<kv8_move<true>>(), METH_FASTCALL, nullptr},
+                         {"kv8_load", fast<kv8_move<false>>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -207,20 +207,8 @@ def _rows(tables, lens, what="tables"):
         _ptr(lens, "lens", torch.int32, tables.shape[:1])
 
 
-def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=None, eps=1e-6, rope=None, adjacent=False,
-              stream=None):
-    """pgcm_kv_append: q, q_out [tokens, heads, head_dim] (or None: keys and values alone), k, v [tokens, kv_heads,
-    head_dim], of the cache's type with contiguous channels; positions int32, slots int64 [tokens]; weights [head_dim]; rope
-    float32 [positions, rope_dim], cosines then sines.  positions may be None if rope is."""
-    if not k.is_cuda:
-        raise ValueError("k must be a CUDA tensor")
-    h = _stream_handle(stream)
-    status = (_marshal or _native()).kv_append(None, cache._at, q, k, v, positions, slots, q_out, q_weight,
-                                               k_weight, eps, rope, 1 if adjacent else 0, h)
-    if status is not None:
-        if status:
-            _check(status)
-        return
+def _append_args(cache, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope, adjacent):
+    """what the native marshalling left, or what is wrong with it"""
     _same_device(cache.device, "the cache", _device())
     n, kv, d, half = k.shape[0], cache.kv_heads, cache.head_dim, cache.dtype
     heads = 0 if q is None else q.shape[1]
@@ -243,6 +231,24 @@ def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=N
         a.rope = _given(_ptr(rope, "rope", torch.float32, rope.shape))
         a.rope_positions, a.rope_dim = rope.shape
         a.adjacent = 1 if adjacent else 0
+    return a
+
+
+def kv_append(cache, q, k, v, positions, slots, q_out, q_weight=None, k_weight=None, eps=1e-6, rope=None, adjacent=False,
+              stream=None):
+    """pgcm_kv_append: q, q_out [tokens, heads, head_dim] (or None: keys and values alone), k, v [tokens, kv_heads,
+    head_dim], of the cache's type with contiguous channels; positions int32, slots int64 [tokens]; weights [head_dim]; rope
+    float32 [positions, rope_dim], cosines then sines.  positions may be None if rope is."""
+    if not k.is_cuda:
+        raise ValueError("k must be a CUDA tensor")
+    h = _stream_handle(stream)
+    status = (_marshal or _native()).kv_append(None, cache._at, q, k, v, positions, slots, q_out, q_weight,
+                                               k_weight, eps, rope, 1 if adjacent else 0, h)
+    if status is not None:
+        if status:
+            _check(status)
+        return
+    a = _append_args(cache, q, k, v, positions, slots, q_out, q_weight, k_weight, eps, rope, adjacent)
     _check(_lib().pgcm_kv_append(cache._at, C.addressof(a), h))
 
 

@@ -1,0 +1,299 @@
+"""KV blocks in 8 bits on the GPU against their definitions: whole blocks to codes and back, and appending."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_03357_amd as pgcm
+import kv8_reference as ref
+import kv_reference as ref16
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [  # block tokens, kv heads, channels
+    (16, 1, 16), (16, 3, 64), (32, 8, 128), (16, 40, 128), (48, 5, 80), (64, 2, 256), (256, 1, 144)]
+
+
+def _cache8(parts, half):
+    return pgcm.KV8Cache(*parts, half)
+
+
+def _numbers(seed, *shape, half):
+    """values of many sizes, each head's largest among them"""
+    x = ref16.numbers(seed, *shape) * 2.0 ** ref16.numbers(seed + 1, *shape[:-1], 1, std=3.0)
+    return x.to(half)
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32).cuda()
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("half", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("size", SIZES)
+def test_store_and_load(size, half, code):
+    block, kv, dim = size
+    for pieces in (True, False):
+        cpu = ref.pool8(1, 7, block, kv, dim, code, pieces, heads_first=True)
+        gpu = ref.on_gpu(cpu, block, kv, dim, code, pieces)
+        pool = _numbers(3, 6, 2, block, kv, dim, half=half)
+        on = pool.cuda()
+        # out of either pool: passed over; an empty one starts anew all the same
+        blocks, others, counts = [5, 0, 9, 3, 6, 2], [0, 5, 1, 7, 3, 4], [block, 1, block, block, 0, block + 9]
+        pgcm.kv8_store(_cache8(gpu, half), pgcm.KVCache(on[:, 0], on[:, 1]), _ints(blocks), _ints(counts), _ints(others))
+        for i in (0, 1):
+            want = ref.Blocks8(cpu[i], cpu[2 + i])
+            for b, o, c in zip(blocks, others, counts):
+                if b < 7 and o < 6:
+                    want.start(b, pool[o, i, :max(0, min(c, block))].double().numpy())
+            want.same(gpu[i], gpu[2 + i], "kv"[i])
+        # ... and back, over other values
+        back = _numbers(4, 8, 2, block, kv, dim, half=half)
+        got = back.cuda()
+        blocks, others, counts = [5, 1, -1, 2, 4, 6], [7, 0, 1, 8, 3, 4], [block, 3, block, block, -2, block + 9]
+        pgcm.kv8_load(_cache8(gpu, half), pgcm.KVCache(got[:, 0], got[:, 1]), _ints(blocks), _ints(counts), _ints(others))
+        for b, o, c in zip(blocks, others, counts):
+            if 0 <= b < 7 and o < 8:
+                c = max(0, min(c, block))
+                for i in (0, 1):
+                    values = gpu[i][b, :c].float().cpu().double().numpy() * gpu[2 + i][b].cpu().double().numpy()[:, None]
+                    back[o, i, :c] = ref.halves(values, half)
+        assert torch.equal(got.cpu(), back)
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("half", [torch.float16, torch.bfloat16])
+def test_what_is_read_back_is_off_by_half_a_step(half, code):
+    pool = _numbers(9, 50, 2, 16, 4, 128, half=half).cuda()
+    gpu = ref.on_gpu(ref.pool8(1, 50, 16, 4, 128, code), 16, 4, 128, code, True)
+    back = torch.empty_like(pool)
+    all_of = torch.arange(50, dtype=torch.int32, device="cuda")
+    pgcm.kv8_store(_cache8(gpu, half), pgcm.KVCache(pool[:, 0], pool[:, 1]), all_of)
+    pgcm.kv8_load(_cache8(gpu, half), pgcm.KVCache(back[:, 0], back[:, 1]), all_of)
+    for i in (0, 1):
+        x, y = pool[:, i].double(), back[:, i].double()
+        scale = gpu[2 + i].double()[:, None, :, None]
+        # a step of int8 is the scale; one of e4m3 is 2^-3 of the value's power of two at most, 2^-9 scales below the normal ones;
+        # then the half's own rounding, below its normal numbers 2^-25
+        off = scale / 2 if code == torch.int8 else torch.maximum(x.abs() * 2.0 ** -4, scale * 2.0 ** -10)
+        assert bool(((x - y).abs() <= off * 1.0000001 + (2.0 ** -25 if half == torch.float16 else 0)).all())
+        # the scale is the least: half of it would not reach
+        assert bool((x.abs().amax((1, 3)) > ref.TOP[code] / 2 * gpu[2 + i].double()).all())
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("half", [torch.float16, torch.bfloat16])
+def test_ends_of_the_range(half, code):
+    """zeros, the least numbers, the largest, borders of a power of two, and what is not finite"""
+    top, least = torch.finfo(half).max, 2.0 ** (-24 if half == torch.float16 else -133)
+    rows = [0.0, least, -least, top, -top, 1.0, -1.984375, 1.9921875, 1.75, 1.8125, 2.0 ** -14, 3.5, -math.inf, math.inf, math.nan]
+    n = len(rows)
+    pool = torch.zeros(n, 2, 16, 2, 64, dtype=torch.float64)
+    for i, x in enumerate(rows):
+        pool[i, :, 7, 1, 33] = x
+        pool[i, :, :, 0, :] = x / 4
+        pool[i, :, 3, 1, :] = x / 1024
+    pool = pool.to(half)
+    on = pool.cuda()
+    cpu = ref.pool8(5, n, 16, 2, 64, code)
+    gpu = ref.on_gpu(cpu, 16, 2, 64, code, True)
+    every = torch.arange(n, dtype=torch.int32, device="cuda")
+    pgcm.kv8_store(_cache8(gpu, half), pgcm.KVCache(on[:, 0], on[:, 1]), every)
+    back = torch.empty_like(on)
+    pgcm.kv8_load(_cache8(gpu, half), pgcm.KVCache(back[:, 0], back[:, 1]), every)
+    for i in (0, 1):
+        want = ref.Blocks8(cpu[i], cpu[2 + i])
+        for b in range(n):
+            want.start(b, pool[b, i].double().numpy())
+        want.same(gpu[i], gpu[2 + i])
+        values = ref.halves(want.codes * want.scales[:, None, :, None], half)
+        got = back[:, i].cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(values))
+        assert torch.equal(got[~torch.isnan(got)], values[~torch.isnan(values)])
+        assert bool(torch.isnan(got[-3:]).all()) and not bool(torch.isnan(got[:-3]).any())
+
+
+def _packed(seed, n, heads, kv, dim, half):
+    x = _numbers(seed, n, heads + 2 * kv, dim, half=half)
+    return x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:]
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("half", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("size", SIZES)
+def test_append_without_norms(size, half, code):
+    """values as they are: codes are exact.  Runs of all lengths, across blocks and on from inside one, some tokens nowhere"""
+    block, kv, dim = size
+    heads = 2 * kv
+    cpu = ref.pool8(2, 9, block, kv, dim, code)
+    gpu = ref.on_gpu(cpu, block, kv, dim, code, True)
+    want = [ref.Blocks8(cpu[i], cpu[2 + i]) for i in (0, 1)]
+    calls = [
+        # (block, first place, tokens); None: a token without a place
+        [(3, 0, block), (1, 0, 5), None, (7, 2, 1), (0, block - 1, 1), (8, block // 2, block // 2), None],
+        [(1, 5, 1), (3, 0, 1), (7, 3, block - 3)],
+        [(1, 6, 9), (3, 1, 3), (4, 1, block - 1)],
+        [None], [(1, 15, 1)]]
+    for c, runs in enumerate(calls):
+        slots = [s for r in runs for s in ([-1] if r is None else [r[0] * block + r[1] + j for j in range(r[2])])]
+        if c == 0:
+            slots[-1] = 9 * block    # just behind the pool
+        n = len(slots)
+        q, k, v = _packed(10 + c, n, heads, kv, dim, half)
+        if c == 1:
+            k, v = k * 64, v * 0.01
+        x = torch.cat([q, k, v], 1).cuda()
+        q_out = torch.empty(n, heads, dim, dtype=half, device="cuda")
+        pgcm.kv8_append(_cache8(gpu, half), x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:], None,
+                        torch.tensor(slots).cuda(), q_out)
+        at = 0
+        for r in runs:
+            if r is not None:
+                for i, y in enumerate((k, v)):
+                    want[i].append(r[0], r[1], y[at:at + r[2]].double().numpy())
+            at += 1 if r is None else r[2]
+        assert torch.equal(q_out.cpu(), q)
+        for i in (0, 1):
+            want[i].same(gpu[i], gpu[2 + i], "call %d %s" % (c, "kv"[i]))
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+def test_a_block_filled_token_by_token(code):
+    """the codes stay within one step of int8 (e4m3: half of one of the value's, or a step of the least) of what went in"""
+    half, block, kv, dim = torch.bfloat16, 64, 2, 128
+    gpu = ref.on_gpu(ref.pool8(4, 2, block, kv, dim, code), block, kv, dim, code, True)
+    x = (ref16.numbers(21, block, 2, kv, dim) * 2.0 ** (torch.arange(block) / 7.0)[:, None, None, None]).to(half)
+    on = x.cuda()
+    for t in range(block):
+        pgcm.kv8_append(_cache8(gpu, half), None, on[t:t + 1, 0], on[t:t + 1, 1], None, torch.tensor([block + t]).cuda(), None)
+    for i in (0, 1):
+        scale = gpu[2 + i][1].cpu().double()[:, None]
+        assert scale.flatten().tolist() == [2.0 ** ref.power(float(a), code) for a in x[:, i].double().abs().amax((0, 2))]
+        off = (gpu[i][1].cpu().double() * scale - x[:, i].double()).abs()
+        assert bool((off <= (scale if code == torch.int8 else torch.maximum(x[:, i].double().abs() / 16, scale * 2.0 ** -9))).all())
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+def test_what_is_not_finite_stays_until_the_block_starts_anew(code):
+    half, block, kv, dim = torch.bfloat16, 16, 2, 64
+    cpu = ref.pool8(6, 1, block, kv, dim, code)
+    gpu = ref.on_gpu(cpu, block, kv, dim, code, True)
+    want = [ref.Blocks8(cpu[i], cpu[2 + i]) for i in (0, 1)]
+    for c, (inside, tokens) in enumerate([(0, 3), (3, 1), (4, 2), (6, 1), (0, 1), (1, 1)]):
+        _, k, v = _packed(30 + c, tokens, 2, kv, dim, half)
+        if c == 1:
+            k[0, 1, 5] = math.nan
+        if c == 2:
+            v[1, 0, 60] = -math.inf
+        pgcm.kv8_append(_cache8(gpu, half), None, k.cuda(), v.cuda(), None, torch.arange(inside, inside + tokens).cuda(), None)
+        for i, y in enumerate((k, v)):
+            want[i].append(0, inside, y.double().numpy())
+            want[i].same(gpu[i], gpu[2 + i], "call %d" % c)
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("half", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim, rope_dim, adjacent, weighted", [(128, 128, False, True), (64, 64, True, True), (80, 48, False, True),
+                                                               (256, 256, False, True), (128, 128, False, False),
+                                                               (144, 144, True, False), (128, None, False, True)])
+def test_append_with_norms_and_rotation(dim, rope_dim, adjacent, weighted, half, code):
+    kv, heads, block, n = 3, 6, 16, 45
+    eps = 1e-5
+    gpu = ref.on_gpu(ref.pool8(7, 6, block, kv, dim, code), block, kv, dim, code, True)
+    q, k, v = _packed(40, n, heads, kv, dim, half)
+    weights = [(1 + 0.2 * ref16.numbers(41 + i, dim)).to(half) if weighted else None for i in (0, 1)]
+    positions = [(7 * t) % 90 for t in range(n)]
+    positions[20] = 90      # outside the table
+    table = None
+    if rope_dim is not None:
+        angle = torch.arange(90).double()[:, None] * 100.0 ** (-torch.arange(0, rope_dim, 2).double() / rope_dim)
+        table = torch.cat([angle.cos(), angle.sin()], 1).float()
+    slots = torch.arange(block, block + n)
+    q_out = torch.empty(n, heads, dim, dtype=half, device="cuda")
+    x = torch.cat([q, k, v], 1).cuda()
+    pgcm.kv8_append(_cache8(gpu, half), x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:],
+                    None if table is None else _ints(positions), slots.cuda(), q_out,
+                    q_weight=None if not weighted else weights[0].cuda(), k_weight=None if not weighted else weights[1].cuda(),
+                    eps=eps, rope=None if table is None else table.cuda(), adjacent=adjacent)
+    # sums of dim squares, their mean, root and quotient, the factors and two products: each a rounding of 2^-24 or two
+    def off(y, of):
+        # of a pair's larger part, which the smaller one is a difference of; a norm adds (dim + 8) roundings to each
+        return (dim + 24) * 2.0 ** -24 * of.abs().nan_to_num(0.0).amax(-1, keepdim=True) * 2   # (channels not rotated stay numbers)
+    want_q = ref16.turned(q, weights[0], eps, table, positions, adjacent)
+    unit = ref16.UNIT[half]
+    near = (q_out.cpu().double() - want_q).abs() <= unit * want_q.abs() + ref16.LEAST[half] + off(want_q, want_q)
+    assert bool((near | torch.isnan(want_q)).all()) and torch.equal(torch.isnan(q_out.cpu()), torch.isnan(want_q))
+    want_k = ref16.turned(k, weights[1], eps, table, positions, adjacent)
+    for i, want in enumerate((want_k, v.double())):
+        for b in range(3):
+            rows = want[b * block:(b + 1) * block]
+            for h in range(kv):
+                a, scale = float(rows[:, h].abs().max()), float(gpu[2 + i][1 + b, h])
+                if not math.isfinite(a):
+                    assert math.isnan(scale) and bool((gpu[i][1 + b, :rows.shape[0], h].float() == 0).all())
+                    continue
+                slack = 0.0 if i else 2 * (dim + 24) * 2.0 ** -24
+                assert scale in {2.0 ** ref.power(a * (1 + s), code) for s in (-slack, 0, slack)}
+                got = gpu[i][1 + b, :rows.shape[0], h].cpu().double() * scale
+                step = scale / 2 if code == torch.int8 else torch.maximum(rows[:, h].abs() / 16, torch.tensor(scale * 2.0 ** -10))
+                assert bool(((got - rows[:, h]).abs() <= step + slack * a).all())
+
+
+def test_a_captured_append_and_load():
+    """replayed several times with other values, between eager work, against the eager results"""
+    half, code, block, kv, dim, n = torch.bfloat16, torch.int8, 16, 4, 128, 40
+    cpu = ref.pool8(8, 5, block, kv, dim, code)
+    gpu, eager = [ref.on_gpu(cpu, block, kv, dim, code, True) for _ in range(2)]
+    x = torch.zeros(n, 2, kv, dim, dtype=half, device="cuda")
+    pools = [torch.zeros(5, 2, block, kv, dim, dtype=half, device="cuda") for _ in range(2)]
+    slots, every = torch.arange(3, 3 + n).cuda(), torch.arange(5, dtype=torch.int32, device="cuda")
+
+    def step(parts, pool):
+        cache = _cache8(parts, half)
+        pgcm.kv8_append(cache, None, x[:, 0], x[:, 1], None, slots, None)
+        pgcm.kv8_load(cache, pgcm.KVCache(pool[:, 0], pool[:, 1]), every)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(gpu, pools[0])
+    for turn in range(4):
+        x.copy_(_numbers(60 + turn, n, 2, kv, dim, half=half).cuda())
+        step(eager, pools[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(pools[0], pools[1])
+        for a, b in zip(gpu, eager):
+            assert torch.equal(a.float(), b.float())
+
+
+def test_blocks_leave_in_eight_bits_through_the_cipher():
+    """store, encrypt a block's codes and scales as one chunk, decrypt elsewhere, load: what a swap of half the bytes is"""
+    half, code, block, kv, dim = torch.float16, torch.int8, 16, 4, 128
+    pool = _numbers(70, 3, 2, block, kv, dim, half=half).cuda()
+    size = 2 * block * kv * dim + 8 * kv
+    whole = torch.zeros(3, size, dtype=torch.uint8, device="cuda")
+    codes, scales = ref.views(whole, block, kv, dim, code)
+    cache8 = pgcm.KV8Cache(*codes, *scales, half)
+    every = torch.arange(3, dtype=torch.int32, device="cuda")
+    pgcm.kv8_store(cache8, pgcm.KVCache(pool[:, 0], pool[:, 1]), every)
+    before = whole.clone()
+    key = pgcm.expand_key(bytes(range(32)))
+    ivs = torch.arange(36, dtype=torch.uint8, device="cuda")
+    out, tags, ok = torch.zeros_like(whole), torch.zeros(48, dtype=torch.uint8, device="cuda"), torch.zeros(3, dtype=torch.uint8,
+                                                                                                        device="cuda")
+    def at(t):
+        return np.array([t[i].data_ptr() for i in range(3)], np.uint64)
+    lens = np.full(3, size, np.uint64)
+    pgcm.encrypt_batch(key, ivs, None, None, at(whole), lens, at(out), tags)
+    whole.zero_()
+    pgcm.decrypt_verify_batch(key, ivs, None, None, at(out), lens, at(whole), tags, ok)
+    assert bool(ok.all()) and torch.equal(whole, before)
+    back = torch.empty_like(pool)
+    pgcm.kv8_load(cache8, pgcm.KVCache(back[:, 0], back[:, 1]), every)
+    want = [ref.Blocks8(c.cpu(), s.cpu()) for c, s in zip(codes, scales)]
+    for i in (0, 1):
+        for b in range(3):
+            want[i].start(b, pool[b, i].cpu().double().numpy())
+        assert torch.equal(back[:, i].cpu(), ref.halves(want[i].codes * want[i].scales[:, None, :, None], half))
