@@ -1,10 +1,13 @@
 /*
- * pgcm_kv8: KV blocks in 8 bits.  What a block's encryption, its way over the bus and its
+ * pgcm_kv8: KV blocks in 8 bits, and attention with a window.  What a block's encryption, its way over the bus and its
  * reading cost goes by its bytes (paper section 2.1 on what is swapped); in 8 bits they are half as many.
  *
  *   pgcm_kv8_append   norms of queries and keys per head, rotation, keys and values into their slots in 8 bits
  *   pgcm_kv8_store    blocks of halves (pgcm_kv.h) to blocks in 8 bits
  *   pgcm_kv8_load     ... and back
+ *   pgcm_kv8_attend   attention of new tokens of each request over blocks in 8 bits
+ *   pgcm_kv_window    ... over blocks of halves, one or many new tokens of each request; both with a sliding window and a few
+ *                     first tokens that stay visible
  *
  * A cache in 8 bits (pgcm_kv8_cache) has codes where pgcm_kv_cache has halves, and for each block and kv head a scale of its
  * keys and one of its values: a value is its code times the scale.  For codes and scales in one piece, as one chunk for
@@ -19,7 +22,7 @@
  * If a value is infinite or NaN the head's scale of that block is NaN, and the codes that come with it are zero: nothing that is
  * read from there is taken for a number.
  *
- * Conventions are those of pgcm.h and pgcm_kv.h, alignment among them: rows of codes are 16-byte aligned, with
+ * Conventions are those of pgcm.h and pgcm_kv.h, workspaces and alignment among them: rows of codes are 16-byte aligned, with
  * strides that are multiples of 16, head_dim is a multiple of 16 here.  Results do not depend on the order in which workgroups run.
  */
 #ifndef PGCM_KV8_H
@@ -42,7 +45,7 @@ typedef struct {
     uint32_t block_tokens;
     uint32_t kv_heads;
     uint32_t head_dim;           /* a multiple of 16 up to 256 */
-    int64_t k_block, k_token, k_head; /* strides in codes */
+    int64_t k_block, k_token, k_head; /* strides in codes; those of tokens in [0, 2^25] for pgcm_kv8_attend */
     int64_t v_block, v_token, v_head;
     int64_t k_scale_block, k_scale_head, v_scale_block, v_scale_head; /* in floats */
 } pgcm_kv8_cache;
@@ -67,6 +70,44 @@ int pgcm_kv8_store(const pgcm_kv8_cache *to, const pgcm_kv_cache *from, uint32_t
                    const int32_t *from_blocks, void *hip_stream);
 int pgcm_kv8_load(const pgcm_kv8_cache *from, const pgcm_kv_cache *to, uint32_t n, const int32_t *blocks, const int32_t *counts,
                   const int32_t *to_blocks, void *hip_stream);
+
+typedef struct {
+    uint32_t requests, heads;          /* heads: query heads, a multiple of kv_heads: head h reads kv head h / (heads / kv_heads) */
+    uint32_t tokens;                   /* rows of q and out; `requests` if starts is NULL */
+    uint32_t most;                     /* no request has more new tokens; 1 if starts is NULL */
+    const int32_t *starts;             /* DEVICE [requests + 1], ascending: request b's new tokens are rows starts[b] up to
+                                          starts[b + 1] (cut to [0, tokens], and to `most` rows); NULL: row b */
+    const void *q;                     /* DEVICE halves [tokens][heads][head_dim] */
+    int64_t q_token, q_head;
+    const int32_t *tables;             /* DEVICE [requests][row_blocks], rows table_row elements apart */
+    int64_t table_row;
+    uint32_t row_blocks;
+    float scale;                       /* of q . k; finite */
+    const int32_t *lens;               /* DEVICE [requests]: tokens of each, the new ones, its last ones, among them */
+    uint32_t window;                   /* how many tokens a token sees, itself among them; 0: all */
+    uint32_t sinks;                    /* ... and so many first tokens of its request */
+    void *out;                         /* DEVICE halves [tokens][heads][head_dim]; not q */
+    int64_t out_token, out_head;
+    float *lse;                        /* DEVICE [tokens][heads], or NULL: log of the sum of exp(scale q . k) */
+} pgcm_kv_window_args;
+/*
+ * The new token at place p of its request (the last one's place is its length - 1) attends to the tokens t <= p that are on the
+ * device and for which t > p - window or t < sinks: out = sum softmax(scale q . k) v.  A token that sees none gives zeros and a
+ * lse of minus infinity.  Rows of q that no request has are not read, and those of out and lse left as they are.
+ * What lies in the pool beyond what a token sees has no part in its results, whatever it holds.
+ * A score that is NaN or plus infinity makes its row's results NaN, one of minus infinity has no weight.  A value that is not finite
+ * makes its channel infinite or NaN in the rows that see it.
+ * One new token of each request, and always in pgcm_kv8_attend: softmax weights are multiplied with values as sums of halves,
+ * which leave nothing out over bfloat16 blocks of halves, else 2^-22 of a weight at most, or 2^-38 of the row's largest where
+ * that is more.  More of them over blocks of halves: a weight is rounded once, to a half, before it is multiplied with
+ * values (relative to a weight of at most 1, and in binary16 to 2^-25 of that); their sum is not.
+ * In pgcm_kv8_attend a query is multiplied as a power of two times binary16 numbers, its largest channel near 2^14: what of a
+ * bfloat16 channel lies below 2^-38 of that one is rounded away, and a row whose largest is below 2^-126 counts as zero.
+ */
+int pgcm_kv8_attend(pgcm_kv_t *kv, const pgcm_kv8_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);
+int pgcm_kv_window(pgcm_kv_t *kv, const pgcm_kv_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);
+/* Room of a workspace for calls of both with at most these sizes. */
+int pgcm_kv_window_reserve(pgcm_kv_t *kv, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, void *hip_stream);
 
 #ifdef __cplusplus
 }

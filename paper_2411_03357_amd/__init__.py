@@ -13,7 +13,7 @@ from .binding import (PgcmError, Key, expand_key, expand_key_bytes, encrypt_batc
 
 _KV = ("KVCache", "KVWorkspace", "kv_workspace", "kv_append", "kv_attend", "kv_summarize", "kv_select", "kv_evict",
        "KV_EXPORTS")
-_KV8 = ("KV8Cache", "kv8_append", "kv8_store", "kv8_load", "KV8_EXPORTS")
+_KV8 = ("KV8Cache", "kv8_append", "kv8_store", "kv8_load", "kv8_attend", "kv_window", "kv_window_reserve", "KV8_EXPORTS")
 
 
 def __getattr__(name):

@@ -22,6 +22,8 @@ struct Kv8Calls {
     decltype(&pgcm_kv8_append) append;
     decltype(&pgcm_kv8_store) store;
     decltype(&pgcm_kv8_load) load;
+    decltype(&pgcm_kv8_attend) attend;
+    decltype(&pgcm_kv_window) window;
 } g_kv8;
 
 // A cache as kv.py hands it over: with the device that it is on.
@@ -208,6 +210,48 @@ PyObject* kv8_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return append_to(in, in.cache8(), g_kv8.append);
 }
 
+// the arguments of attention with a window but for the workspace and the cache, and the call with them
+template <class Cache, class Call>
+PyObject* attend_in_window(Arguments& in, pgcm_kv_t* space, const Cache* cache, Call call) {
+    if (cache == nullptr) Py_RETURN_NONE;
+    const at::ScalarType half = half_of(cache->half);
+    pgcm_kv_window_args a = {};
+    Tensor q, tables, lens, out, lse, starts;
+    in.tensor(&q, half, 3, false);
+    in.tensor(&tables, at::kInt, 2, false);
+    in.tensor(&lens, at::kInt, 1, true);
+    in.tensor(&out, half, 3, false);
+    const int64_t n = tables.shape[0], row = tables.shape[1], rows = q.shape[0], heads = q.shape[1], d = cache->head_dim;
+    if (in.tensor(&lse, at::kFloat, 2, true, true)) in.need(lse.is(rows, heads));
+    a.scale = in.real();
+    a.window = in.number(), a.sinks = in.number();
+    if (in.tensor(&starts, at::kInt, 1, true, true)) in.need(starts.is(n + 1));
+    else in.need(rows == n);
+    a.most = in.number();
+    void* stream = in.address();
+    in.need(q.is(rows, heads, d) && lens.is(n) && out.is(rows, heads, d) && n <= 0xFFFFFFFFll && row <= 0xFFFFFFFFll &&
+            rows <= 0xFFFFFFFFll && heads <= 0xFFFFFFFFll);
+    if (!in.all_taken()) Py_RETURN_NONE;
+    a.requests = (uint32_t)n, a.heads = (uint32_t)heads, a.tokens = (uint32_t)rows, a.row_blocks = (uint32_t)row;
+    a.q = q.at, a.q_token = q.stride[0], a.q_head = q.stride[1];
+    a.out = out.at, a.out_token = out.stride[0], a.out_head = out.stride[1];
+    a.tables = (const int32_t*)tables.at, a.table_row = tables.stride[0], a.lens = (const int32_t*)lens.at;
+    a.starts = (const int32_t*)starts.at, a.lse = (float*)lse.at;
+    return called([&] { return call(space, cache, &a, stream); });
+}
+
+// (device, workspace, cache, q, tables, lens, out, lse, scale, window, sinks, starts, most, stream) -> status or None
+PyObject* kv8_attend(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    Arguments in(args, nargs);
+    auto* space = (pgcm_kv_t*)in.address();
+    return attend_in_window(in, space, in.cache8(), g_kv8.attend);
+}
+PyObject* kv_window(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    Arguments in(args, nargs);
+    auto* space = (pgcm_kv_t*)in.address();
+    return attend_in_window(in, space, in.cache(), g_kv8.window);
+}
+
 // (device, cache8, cache, blocks, counts, others, stream) -> status or None
 template <bool kStore>
 PyObject* kv8_move(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -362,14 +406,16 @@ PyObject* bind(PyObject*, PyObject* args) {
 
 // bind8(the addresses of Kv8Calls, in their order)
 PyObject* bind8(PyObject*, PyObject* args) {
-    PyObject* f[3];
-    if (!PyArg_ParseTuple(args, "OOO", &f[0], &f[1], &f[2])) return nullptr;
-    void* at[3];
-    for (int i = 0; i < 3; ++i) at[i] = PyLong_AsVoidPtr(f[i]);
+    PyObject* f[5];
+    if (!PyArg_ParseTuple(args, "OOOOO", &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+    void* at[5];
+    for (int i = 0; i < 5; ++i) at[i] = PyLong_AsVoidPtr(f[i]);
     if (PyErr_Occurred()) return nullptr;
     g_kv8.append = reinterpret_cast<decltype(g_kv8.append)>(at[0]);
     g_kv8.store = reinterpret_cast<decltype(g_kv8.store)>(at[1]);
     g_kv8.load = reinterpret_cast<decltype(g_kv8.load)>(at[2]);
+    g_kv8.attend = reinterpret_cast<decltype(g_kv8.attend)>(at[3]);
+    g_kv8.window = reinterpret_cast<decltype(g_kv8.window)>(at[4]);
     Py_RETURN_NONE;
 }
 
@@ -388,6 +434,8 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"kv8_append", fast<kv8_append>(), METH_FASTCALL, nullptr},
                          {"kv8_store", fast<kv8_move<true>>(), METH_FASTCALL, nullptr},
                          {"kv8_load", fast<kv8_move<false>>(), METH_FASTCALL, nullptr},
+                         {"kv8_attend", fast<kv8_attend>(), METH_FASTCALL, nullptr},
+                         {"kv_window", fast<kv_window>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,13 +1,14 @@
-"""ctypes binding for include/pgcm_kv8.h: KV blocks in 8 bits, same names, argument marshalling only."""
+"""ctypes binding for include/pgcm_kv8.h: KV blocks in 8 bits and attention with a window, same names, argument marshalling only."""
 import ctypes as C
 
 import torch
 
 from . import kv as _kv
 from .binding import _check, _stream_handle
-from .kv import _HALVES, _append_args, _device, _i64, _ptr, _same_device, _strides, _u32, _vp
+from .kv import _HALVES, _append_args, _f32, _i64, _ptr, _rows, _same_device, _strides, _u32, _vp, kv_workspace
 
-KV8_EXPORTS = ("pgcm_kv8_append", "pgcm_kv8_store", "pgcm_kv8_load")
+KV8_EXPORTS = ("pgcm_kv8_append", "pgcm_kv8_store", "pgcm_kv8_load", "pgcm_kv8_attend", "pgcm_kv_window",
+               "pgcm_kv_window_reserve")
 
 _CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
@@ -17,6 +18,13 @@ class _Cache8(C.Structure):
         [(n, _u32) for n in ("code", "half", "blocks", "block_tokens", "kv_heads", "head_dim")] + \
         [(n, _i64) for n in ("k_block", "k_token", "k_head", "v_block", "v_token", "v_head", "k_scale_block", "k_scale_head",
                              "v_scale_block", "v_scale_head")]
+
+
+class _Window(C.Structure):
+    _fields_ = [(n, _u32) for n in ("requests", "heads", "tokens", "most")] + \
+        [("starts", _vp), ("q", _vp), ("q_token", _i64), ("q_head", _i64), ("tables", _vp), ("table_row", _i64),
+         ("row_blocks", _u32), ("scale", _f32), ("lens", _vp), ("window", _u32), ("sinks", _u32), ("out", _vp),
+         ("out_token", _i64), ("out_head", _i64), ("lse", _vp)]
 
 
 class _Placed8(C.Structure):
@@ -34,9 +42,12 @@ def _lib():
         lib.pgcm_kv8_append.argtypes = [_vp, _vp, _vp]
         lib.pgcm_kv8_store.argtypes = [_vp, _vp, _u32, _vp, _vp, _vp, _vp]
         lib.pgcm_kv8_load.argtypes = [_vp, _vp, _u32, _vp, _vp, _vp, _vp]
+        lib.pgcm_kv8_attend.argtypes = [_vp] * 4
+        lib.pgcm_kv_window.argtypes = [_vp] * 4
+        lib.pgcm_kv_window_reserve.argtypes = [_vp] + [_u32] * 3 + [_vp]
         for name in KV8_EXPORTS:
             getattr(lib, name).restype = C.c_int
-        m.bind8(*[C.cast(getattr(lib, "pgcm_kv8_" + n), _vp).value for n in ("append", "store", "load")])
+        m.bind8(*[C.cast(getattr(lib, n), _vp).value for n in KV8_EXPORTS[:5]])
         _marshal, _bound = m, lib
     return _bound
 
@@ -95,8 +106,8 @@ def _move(name, cache8, cache, blocks, counts, others, stream):
     h = _stream_handle(stream)
     status = getattr(_marshal or _native(), name)(None, cache8._at, cache._at, blocks, counts, others, h)
     if status is None:
-        _same_device(cache8.device, "the cache in 8 bits", _device())
-        _same_device(cache.device, "the cache", _device())
+        _same_device(cache8.device, "the cache in 8 bits", _kv._device())
+        _same_device(cache.device, "the cache", _kv._device())
         n = blocks.shape[0]
         status = getattr(_lib(), "pgcm_" + name)(
             cache8._at, cache._at, n, _ptr(blocks, "blocks", torch.int32, (n,)),
@@ -114,3 +125,57 @@ def kv8_store(cache8, cache, blocks, counts=None, from_blocks=None, stream=None)
 def kv8_load(cache8, cache, blocks, counts=None, to_blocks=None, stream=None):
     """pgcm_kv8_load: from cache8 to cache; blocks (of cache8), counts, to_blocks int32 [n]"""
     _move("kv8_load", cache8, cache, blocks, counts, to_blocks, stream)
+
+
+def _attend(name, cache, q, tables, lens, out, lse, scale, window, sinks, starts, most, workspace, stream):
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    h = _stream_handle(stream)
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    if most is None:
+        most = 1 if starts is None else q.shape[0]
+    space = (workspace or kv_workspace(h))._h
+    status = getattr(_marshal or _native(), name)(None, space, cache._at, q, tables, lens, out, lse, scale, window, sinks, starts,
+                                                  most, h)
+    if status is None:
+        _same_device(cache.device, "the cache", _kv._device())
+        n, row, tables_at, lens_at = _rows(tables, lens)
+        d, half = cache.head_dim, cache.dtype
+        rows, heads = (n if starts is None else q.shape[0]), q.shape[1]
+        if not all(0 <= x < 1 << 32 for x in (window, sinks, most)):
+            raise ValueError("window, sinks and most are numbers of 32 bits")
+        a = _Window(n, heads, rows, most)
+        if starts is not None:
+            a.starts = _ptr(starts, "starts", torch.int32, (n + 1,))
+        a.q = _ptr(q, "q", half, (rows, heads, d), False)
+        a.q_token, a.q_head = _strides(q)
+        a.tables, a.row_blocks, a.lens = tables_at, row, lens_at
+        a.table_row, = _strides(tables)
+        a.scale, a.window, a.sinks = scale, window, sinks
+        a.out = _ptr(out, "out", half, (rows, heads, d), False)
+        a.out_token, a.out_head = _strides(out)
+        if lse is not None:
+            a.lse = _ptr(lse, "lse", torch.float32, (rows, heads))
+        status = getattr(_lib(), "pgcm_" + name)(space, cache._at, C.addressof(a), h)
+    if status:
+        _check(status)
+
+
+def kv8_attend(cache, q, tables, lens, out, lse=None, scale=None, window=0, sinks=0, starts=None, most=None, workspace=None,
+               stream=None):
+    """pgcm_kv8_attend: q, out [tokens, heads, head_dim] of the cache's half; tables int32 [requests, row_blocks]; lens int32
+    [requests], new tokens included; lse float32 [tokens, heads]; starts int32 [requests + 1]: a request's new tokens are rows
+    starts[b] up to starts[b + 1], at most `most` of them; None: a row for each.  scale: 1 / sqrt(head_dim) if None; window 0: all."""
+    _attend("kv8_attend", cache, q, tables, lens, out, lse, scale, window, sinks, starts, most, workspace, stream)
+
+
+def kv_window(cache, q, tables, lens, out, lse=None, scale=None, window=0, sinks=0, starts=None, most=None, workspace=None,
+              stream=None):
+    """pgcm_kv_window: the same over blocks of halves (KVCache)"""
+    _attend("kv_window", cache, q, tables, lens, out, lse, scale, window, sinks, starts, most, workspace, stream)
+
+
+def kv_window_reserve(workspace, heads, kv_heads, head_dim, stream=None):
+    """pgcm_kv_window_reserve: sizes a KVWorkspace ahead of time, as a captured graph needs"""
+    _check(_lib().pgcm_kv_window_reserve(workspace._h, heads, kv_heads, head_dim, _stream_handle(stream)))

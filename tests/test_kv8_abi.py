@@ -94,6 +94,40 @@ def test_append_refuses():
     assert lib.pgcm_kv8_append(at, C.byref(_append(tokens=0, k=None)), None) == 0
 
 
+def _window(**change):
+    a = kv8._Window(3, 4, 5, 3, AT, AT, 512, 128, AT, 20, 20, 0.1, AT, 100, 4, AT, 512, 128, None)
+    for name, value in change.items():
+        setattr(a, name, value)
+    return a
+
+
+def test_attention_refuses():
+    lib, some = kv8._lib(), C.create_string_buffer(256)
+    for call, cache, other in ((lib.pgcm_kv8_attend, _cache8, BAD_CACHES + UNALIGNED_CACHES),
+                               (lib.pgcm_kv_window, _cache, [dict(k=None), dict(half=2), dict(reserved=1), dict(v=AT + 8)])):
+        good = cache()
+        at = C.addressof(good)
+        assert call(None, at, C.byref(_window()), None) == ARG
+        assert call(some, None, C.byref(_window()), None) == ARG
+        assert call(some, at, None, None) == ARG
+        for bad in other:
+            assert call(some, C.byref(cache(**bad)), C.byref(_window()), None) in (ARG, ALIGN), bad
+        for bad in (dict(q=None), dict(out=None), dict(lens=None), dict(tables=None), dict(scale=math.nan), dict(scale=math.inf),
+                    dict(heads=3), dict(heads=0), dict(heads=70000), dict(row_blocks=1 << 28), dict(requests=1 << 31),
+                    dict(tokens=1 << 31), dict(most=0), dict(starts=None), dict(starts=None, tokens=3),
+                    dict(starts=None, most=1), dict(requests=60000, row_blocks=1 << 26)):
+            assert call(some, at, C.byref(_window(**bad)), None) == ARG, bad
+        for bad in (dict(k_token=-128), dict(k_token=1 << 26), dict(v_token=-128), dict(v_token=1 << 26)):
+            assert call(some, C.byref(cache(**bad)), C.byref(_window()), None) == ARG, bad
+        for bad in (dict(q=AT + 4), dict(q_token=4), dict(q_head=1), dict(out=AT + 8), dict(out_token=2), dict(out_head=12)):
+            assert call(some, at, C.byref(_window(**bad)), None) == ALIGN, bad
+        assert call(some, at, C.byref(_window(requests=0, q=None)), None) == 0
+        assert call(some, at, C.byref(_window(tokens=0, q=None)), None) == 0
+    assert lib.pgcm_kv_window_reserve(None, 4, 2, 128, None) == ARG
+    for bad in ((4, 3, 128), (0, 1, 128), (4, 2, 12), (4, 2, 264)):
+        assert lib.pgcm_kv_window_reserve(some, *bad, None) == ARG, bad
+
+
 def test_tensors_on_the_host_are_refused():
     with pytest.raises(ValueError, match="CUDA"):
         pgcm.KV8Cache(*ref.pool8(1, 2, 16, 2, 64, torch.int8))
@@ -105,6 +139,9 @@ def test_tensors_on_the_host_are_refused():
     for move in (pgcm.kv8_store, pgcm.kv8_load):
         with pytest.raises(ValueError, match="CUDA"):
             move(None, None, torch.zeros(1, dtype=torch.int32))
+    for call in (pgcm.kv8_attend, pgcm.kv_window):
+        with pytest.raises(ValueError, match="CUDA"):
+            call(None, x, None, None, None)
 
 
 @pytest.mark.parametrize("code", ref.CODES)
