@@ -12,7 +12,8 @@ MARSHAL = os.path.join(HERE, "_marshal.so")
 KV_MARSHAL = os.path.join(HERE, "_kv_marshal.so")    # a torch extension; the rest does without torch
 SOURCES = ["pgcm_kernels.hip", "pgcm_bitsliced.hip", "pgcm_host.hip", "pgcm_bounce.hip", "pgcm_pipe.hip",
            "pgcm_seq.cpp", "pgcm_kv.hip", "pgcm_kv_attend.hip", "pgcm_kv_cache.hip", "pgcm_kv_choose.hip",
-           "pgcm_kv8_cache.hip", "pgcm_kv_window.hip", "pgcm_kv_window_few.hip"]
+           "pgcm_kv8_cache.hip", "pgcm_kv_window.hip", "pgcm_kv_window_few.hip",
+           "pgcm_kv_window_many.hip"]
 HEADERS = ["pgcm_kernels.h", "pgcm_types.h", "pgcm_arrive.h", "pgcm_contexts.h", "pgcm_one_launch.h",
            "pgcm_spans.h", "pgcm_routes.h", "pgcm_host_ivs.h", "pgcm_bitsliced_gen.h",
            "pgcm_kv_common.h", "pgcm_kv8_common.h", "pgcm_kv_window.h",

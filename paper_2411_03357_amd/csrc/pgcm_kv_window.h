@@ -63,4 +63,5 @@ namespace pgcm_kv_impl {
 int window_few(pgcm_kv* kv, WindowArgs& a, uint32_t half, uint32_t code, hipStream_t stream);
 int window_many(pgcm_kv* kv, WindowArgs& a, uint32_t half, hipStream_t stream);
 Room window_few_room(uint32_t heads, uint32_t kv_heads, uint32_t head_dim);
+Room window_many_room(uint32_t head_dim);
 }  // namespace pgcm_kv_impl

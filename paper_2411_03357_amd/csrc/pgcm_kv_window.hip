@@ -65,13 +65,15 @@ int pgcm_kv_window(pgcm_kv_t* kv, const pgcm_kv_cache* cache, const pgcm_kv_wind
     a.k_block = 2 * cache->k_block, a.k_token = 2 * cache->k_token, a.k_head = 2 * cache->k_head;
     a.v_block = 2 * cache->v_block, a.v_token = 2 * cache->v_token, a.v_head = 2 * cache->v_head;
     const std::lock_guard<std::mutex> held(kv->enqueue);
-    return window_few(kv, a, cache->half, ~0u, (hipStream_t)hip_stream);
+    return a.most == 1 ? window_few(kv, a, cache->half, ~0u, (hipStream_t)hip_stream)
+                       : window_many(kv, a, cache->half, (hipStream_t)hip_stream);
 }
 
 int pgcm_kv_window_reserve(pgcm_kv_t* kv, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, void* hip_stream) {
     if (kv == nullptr) return PGCM_ERR_ARG;
     if (const int rc = check_sizes(1, heads, kv_heads, head_dim, kPiece, 1)) return rc;
-    const Room room = window_few_room(heads, kv_heads, head_dim);
+    const Room few = window_few_room(heads, kv_heads, head_dim), many = window_many_room(head_dim);
+    const Room room{few.counters, few.scratch > many.scratch ? few.scratch : many.scratch};
     const std::lock_guard<std::mutex> held(kv->enqueue);
     return kv_ensure(kv, room.counters, room.scratch, (hipStream_t)hip_stream);
 }

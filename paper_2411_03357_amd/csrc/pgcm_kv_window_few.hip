@@ -475,8 +475,9 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
         most = over_rows_max(most);
         // Sums are kept relative to 2^top, which makes the largest weight so far 2^M::kLargest when they were last brought up to
         // it, and at most 2^M::kOverflows before the next time: a new maximum rarely takes that.
-        if (__any(most > top + M::kOverflows || (top == -INFINITY && most > top))) {
-            const float now = fmaxf(most - M::kLargest, top), keep = exp2_from(top, now);
+        const bool over = most > top + M::kOverflows || (top == -INFINITY && most > top);
+        if (__any(over)) {   // (what other heads need changes nothing in a head)
+            const float now = over ? fmaxf(most - M::kLargest, top) : top, keep = exp2_from(top, now);
             top = now;
             total *= keep;
 #pragma unroll

@@ -86,6 +86,27 @@ def test_new_tokens(kind, window, sinks):
     ref.check(pgcm, b, _q(14, sum(news), 8, 128, kind[0]), news, window, sinks, spare=5, most=64)
 
 
+@pytest.mark.parametrize("half", HALVES)
+@pytest.mark.parametrize("kv, group, dim, block", [(1, 1, 8, 16), (3, 5, 64, 32), (2, 16, 80, 48), (2, 17, 128, 64), (1, 40, 256, 16),
+                                                   (1, 3, 144, 16), (8, 1, 120, 16), (1, 2, 48, 4096), (1, 130, 24, 16)])
+def test_rows_of_all_heads_and_sizes(half, kv, group, dim, block):
+    lens, news = [300, 70, 0, 500], [150, 70, 3, 90]
+    b = ref.Blocks(41, lens, kv, dim, half, block=block, holes=0.1 if block == 16 else 0.0)
+    q = _q(42, sum(news), kv * group, dim, half)
+    for window, sinks in ((0, 0), (100, 20), (3, 0)):
+        ref.check(pgcm, b, q, news, window, sinks, spare=1)
+
+
+@pytest.mark.parametrize("half", HALVES)
+@pytest.mark.parametrize("lens, news, kv, group, dim, window, sinks", [
+    ([9000, 800], [40, 100], 2, 4, 128, 0, 0), ([9000, 800], [40, 100], 2, 4, 128, 5000, 700), ([20000], [2], 1, 1, 64, 0, 0),
+    ([7001], [200], 1, 3, 256, 6000, 3), ([4000, 33, 4100], [5, 33, 8], 1, 8, 80, 0, 0), ([6000], [64], 1, 4, 128, 1500, 4)])
+def test_rows_in_parts(half, lens, news, kv, group, dim, window, sinks):
+    """few rows and much to see: cut along what they see, with holes"""
+    b = ref.Blocks(43, lens, kv, dim, half, holes=0.2)
+    ref.check(pgcm, b, _q(44, sum(news), kv * group, dim, half), news, window, sinks, spare=2)
+
+
 @kinds
 def test_one_row_of_some_requests(kind):
     lens, news = [300, 5, 0, 129, 64], [1, 0, 1, 1, 0]
