@@ -9,7 +9,10 @@ namespace pgcm_kv_impl {
 namespace {
 
 constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kRowsHeld = 16;   // a unit's tokens in registers; of longer ones, so many at a time, twice
+constexpr int64_t kMostAppendStride = 1 << 23;
 constexpr uint32_t kTogether = 4;    // tokens whose loads are under way together
+constexpr uint32_t kStepsAtOnce = 3; // of queries
 
 struct Side8 {   // keys or values of a cache in 8 bits
     uint8_t* at;
@@ -26,7 +29,9 @@ struct Append8Args {
     Side8 side[2];
     uint64_t pool_tokens;
     uint32_t tokens, heads, kv_heads, head_dim, block_tokens, rope_positions, rope_dim, adjacent, row_power;
+    uint32_t kv_ways, spread;   // workgroups that share a window's keys and values; windows that a block may have
     float eps, by_dim;  // by_dim: 1 / head_dim
+    double by_block;    // 1 / block_tokens
 };
 
 // Over the 2^power lanes of a row, so that each has the result.
@@ -58,6 +63,21 @@ __device__ __forceinline__ uint32_t over_row(uint32_t most, uint32_t power) {
         return float_of(bits_of(x) > bits_of(y) ? bits_of(x) : bits_of(y));
     }));
 }
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 as_two(uint32_t x) { return __builtin_bit_cast(u16x2, x); }
+// |x| of halves in the order of their bits
+__device__ __forceinline__ u16x2 larger(u16x2 most, uint4 x) {
+    const uint32_t words[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (uint32_t n = 0; n < 4; ++n) most = __builtin_elementwise_max(most, as_two(words[n] & 0x7FFF7FFFu));
+    return most;
+}
+// the larger one's as a float's
+template <class H>
+__device__ __forceinline__ uint32_t as_float_bits(u16x2 most) {
+    const uint16_t x = most.x > most.y ? most.x : most.y;
+    return bits_of((float)__builtin_bit_cast(typename H::one, x));
+}
 template <class H>
 __device__ __forceinline__ void floats_of(uint4 words, float (&x)[8]) {
     const typename H::eight y = as_eight<H>(words);
@@ -68,8 +88,6 @@ template <class C>
 __device__ __forceinline__ uint2 eight_codes(const float (&x)[8], float by) {
     return make_uint2(C::codes(x[0], x[1], x[2], x[3], by), C::codes(x[4], x[5], x[6], x[7], by));
 }
-// 2^-e for a scale 2^e, 0 for one that is NaN (the codes are zero then: NaN times 0 is looked for)
-__device__ __forceinline__ float inverse(float scale) { return scale == scale ? 1.f / scale : 0.f; }
 
 // Norm and rotation, as a lane needs them: x by w c + y by w' s   (by: of the norm; y, w': the other channel of the pair and its
 // weight; s with its sign)
@@ -94,12 +112,21 @@ struct Turn {
     struct Weights {
         float own[8], other[8];
     };
-    __device__ __forceinline__ Weights weights(const uint8_t* from, bool adjacent) const {
+    // a weight's own channels and the partner's
+    struct Raw {
+        uint4 own, other;
+    };
+    __device__ __forceinline__ Raw raw_weights(const uint8_t* from) const {
+        Raw r{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (from != nullptr && mine) r.own = *(const uint4*)(from + 2 * d), r.other = *(const uint4*)(from + 16 * partner);
+        return r;
+    }
+    static __device__ __forceinline__ Weights weights(const Raw& raw, bool there, bool adjacent) {
         Weights w;
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) w.own[e] = w.other[e] = 1.f;
-        if (from != nullptr && mine) {
-            const typename H::eight x = as_eight<H>(*(const uint4*)(from + 2 * d)), y = as_eight<H>(*(const uint4*)(from + 16 * partner));
+        if (there) {
+            const typename H::eight x = as_eight<H>(raw.own), y = as_eight<H>(raw.other);
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) w.own[e] = (float)x[e], w.other[e] = (float)(adjacent ? x[e ^ 1] : y[e]);
         }
@@ -143,7 +170,8 @@ struct Turn {
         for (uint32_t e = 0; e < 8; ++e) f.own[e] *= l.known ? c[e] : NAN, f.other[e] *= l.known ? s[e] : NAN;
         return f;
     }
-    __device__ __forceinline__ void apply(const Append8Args& a, uint4 now, const Weights& f, bool normed, float (&z)[8]) const {
+    // z: but for the norm's factor, which is returned
+    __device__ __forceinline__ float apply(const Append8Args& a, uint4 now, const Weights& f, bool normed, float (&z)[8]) const {
         const typename H::eight x = as_eight<H>(now);
         float by = 1.f;
         if (normed) {
@@ -164,143 +192,325 @@ struct Turn {
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) {
             const float pair = (float)(a.adjacent ? y[e ^ 1] : y[e]);
-            z[e] = ((float)x[e] * f.own[e] + pair * f.other[e]) * by;
+            z[e] = (float)x[e] * f.own[e] + pair * f.other[e];
         }
+        return by;
     }
 };
 
-// A unit's scale for these values, bits of the largest |x| in `most`, `before` what it was (0: none)
+// The scale for these values, as bits like all here: `most` of the largest |x|, `before` of what the scale was (0: none).  Scales
+// are not below zero, so they are in the order of their bits, and NaN stays.
 template <class C>
-__device__ __forceinline__ float scale_for(uint32_t most, float before) {
-    if (most >= kNotFinite || !(before == before)) return NAN;
-    return fmaxf(power_of_two(C::power(most)), before);
+__device__ __forceinline__ uint32_t scale_for(uint32_t most, uint32_t before) {
+    const int32_t needed = most >= kNotFinite ? (int32_t)0x7FC00000 : (C::power(most) + 127) << 23;
+    return (uint32_t)(needed > (int32_t)before ? needed : (int32_t)before);
+}
+// 1 / scale, exactly for the powers of two that this library writes; for NaN anything, and the codes are to be zero
+__device__ __forceinline__ float inverse(uint32_t scale) {
+    if (__builtin_expect((scale & 0x7FFFFFu) != 0 || scale >= 0x7E800000u, false)) return 1.f / float_of(scale);
+    return float_of(0x7F000000u - scale);
+}
+__device__ __forceinline__ bool is_lost(uint32_t scale) { return scale > kNotFinite; }
+
+// Where a unit's codes go, lane by lane
+struct To {
+    uint8_t* at;       // of the first token
+    int64_t token;
+    bool wanted;       // the lane has channels of a head
+};
+// A unit of halves, m tokens from `from` on: their codes, and the scale's bits
+template <class H, class C>
+__device__ __forceinline__ uint32_t convert_unit(const uint8_t* from, int64_t from_token, uint32_t m, const To& to, uint32_t row_power) {
+    uint4 held[kRowsHeld];
+    auto take = [&](uint32_t j0) {
+#pragma unroll
+        for (uint32_t n = 0; n < kRowsHeld; ++n) {
+            if (n % kTogether == 0 && j0 + n >= m) break;   // (the same for all lanes)
+            held[n] = make_uint4(0, 0, 0, 0);
+            if (to.wanted && j0 + n < m) held[n] = *(const uint4*)(from + (j0 + n) * from_token);
+        }
+    };
+    u16x2 largest = (u16x2)(unsigned short)0;
+    for (uint32_t j0 = 0; j0 < m; j0 += kRowsHeld) {
+        take(j0);
+#pragma unroll
+        for (uint32_t n = 0; n < kRowsHeld; ++n) {
+            if (n % kTogether == 0 && j0 + n >= m) break;
+            largest = larger(largest, held[n]);
+        }
+    }
+    const uint32_t scale = scale_for<C>(over_row(as_float_bits<H>(largest), row_power), 0);
+    const float by = float_of(0x7F000000u - scale);   // (a power of two, or NaN)
+    const bool lost = is_lost(scale);
+    for (uint32_t j0 = 0; j0 < m; j0 += kRowsHeld) {
+        if (m > kRowsHeld) take(j0);
+#pragma unroll
+        for (uint32_t n = 0; n < kRowsHeld; ++n) {
+            if (n % kTogether == 0 && j0 + n >= m) break;
+            float x[8];
+            floats_of<H>(held[n], x);
+            uint2 codes = eight_codes<C>(x, by);
+            if (lost) codes = make_uint2(0, 0);
+            if (to.wanted && j0 + n < m) *(uint2*)(to.at + (j0 + n) * to.token) = codes;
+        }
+    }
+    return scale;
 }
 
-// A workgroup (or several: blockIdx.y) a token.  It takes its token's queries, and a share of the units of its run: a block's new
-// tokens have as many workgroups as there are tokens, which take its units in turn.
-template <class H, class C>
-__global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
-    const uint32_t token = blockIdx.x, lane = threadIdx.x % 64;
-    const Turn<H> turn(a);
-    const uint32_t heads_at_once = 64u >> a.row_power, in_step = lane >> a.row_power;
-    const uint32_t of_q = (a.heads + heads_at_once - 1) / heads_at_once, of_kv = (a.kv_heads + heads_at_once - 1) / heads_at_once;
-    const uint32_t waves = blockDim.x / 64, stride = waves * gridDim.y;
-    uint32_t task = __builtin_amdgcn_readfirstlane(blockIdx.y * waves + threadIdx.x / 64);
+// Of floor(x / by) and the rest, x below 2^52
+struct Split {
+    uint64_t whole;
+    uint32_t rest;
+};
+__device__ __forceinline__ Split split_by(uint64_t x, uint32_t by, double one_by) {   // one_by: 1 / by
+    uint64_t q = (uint64_t)((double)x * one_by);   // off by one at most
+    int64_t r = (int64_t)(x - q * by);
+    if (r < 0) r += by, --q;
+    if (r >= (int64_t)by) r -= by, ++q;
+    return Split{q, (uint32_t)r};
+}
 
-    const int64_t slot = a.slots[token];
-    const bool stored = (uint64_t)slot < a.pool_tokens;
-    const uint64_t block = stored ? (uint64_t)slot / a.block_tokens : 0;
-    const uint32_t inside = stored ? (uint32_t)((uint64_t)slot - block * a.block_tokens) : 0;
-    // the run: how many tokens before this one, and behind it, have the slots next to its own, in the block
-    uint32_t before = 0, behind = 0;
-    if (stored) {
-        auto count = [&](bool back) {
-            const uint32_t room = back ? inside : a.block_tokens - 1 - inside, there = back ? token : a.tokens - 1 - token;
-            const uint32_t most = room < there ? room : there;
-            for (uint32_t n = 0; n < most; n += 64) {
-                const uint32_t j = n + lane + 1;
-                const bool next = j <= most && (back ? a.slots[token - j] == slot - j : a.slots[token + j] == slot + j);
-                const uint64_t all = __ballot(next);
-                if (~all != 0) return n + (uint32_t)__builtin_ctzll(~all);
-            }
-            return most;
-        };
-        before = __builtin_amdgcn_readfirstlane(count(true));
-        behind = __builtin_amdgcn_readfirstlane(count(false));
-    }
-    const uint32_t m = before + 1 + behind, units = stored ? 2 * of_kv : 0;
-    const uint32_t my_units = units > before ? (units - 1 - before) / m + 1 : 0, tasks = of_q + my_units;
+__device__ __forceinline__ uint64_t of_first_lane(uint64_t x) {
+    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)x), high = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (uint64_t)high << 32 | low;
+}
 
-    if (task < of_q) {
-        const typename Turn<H>::Weights w =
-            turn.factors(a, turn.line(a, a.rope == nullptr ? 0 : a.positions[token]), turn.weights(a.q_weight, a.adjacent != 0));
-        for (; task < of_q; task += stride) {
-            const uint32_t h = task * heads_at_once + in_step;
-            const bool wanted = turn.mine && h < a.heads;
-            uint4 words = make_uint4(0, 0, 0, 0);
-            if (wanted) words = *(const uint4*)(a.q + token * a.q_token + h * a.q_head + 2 * turn.d);
-            if (a.q_weight != nullptr || a.rope != nullptr) {   // (others are copied)
-                float z[8];
-                turn.apply(a, words, w, a.q_weight != nullptr, z);
-                typename H::eight y;
+// Keys and values of a run, m tokens from `first` on, to `block` from place `inside` on: heads [head_from, head_to), a wavefront
+// of the workgroup one at a time.  A lane's rows are tokens side by side, kHeld times as many held in registers (a "chunk"): so a
+// head's largest value is found in the wavefront.  The factors that norm and rotation multiply a chunk's tokens with are made once
+// for all heads, in LDS.  Runs of several chunks are taken twice, for their largest values and for their codes.
+constexpr uint32_t kHeadsAtOnce = 32;    // of a wavefront, whose largest values are kept over a run
+template <uint32_t kHeld>
+struct AppendShared {
+    float4 factors[kHeld][4][64];        // of a lane's row: own, then other
+    uint32_t largest[kWaves][kHeadsAtOnce][2];
+};
+template <class H, class C, uint32_t kHeld>
+__device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& turn, AppendShared<kHeld>& shared, uint32_t first,
+                                           uint32_t m, uint64_t block, uint32_t inside, uint32_t head_from, uint32_t head_to,
+                                           const typename Turn<H>::Raw& raw, int32_t near_position, uint32_t near_from) {
+    const uint32_t lane = turn.lane, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t rows = 64u >> a.row_power, in_step = lane >> a.row_power, chunk = kHeld * rows;
+    const bool worked = a.k_weight != nullptr || a.rope != nullptr, normed = a.k_weight != nullptr;
+    const bool once = m <= chunk;
+    // where the lane's channels lie from a step's first token on
+    const uint32_t k_off = in_step * (uint32_t)a.k_token + 2 * turn.d, v_off = in_step * (uint32_t)a.v_token + 2 * turn.d;
+    const uint32_t code_off[2] = {in_step * (uint32_t)a.side[0].token + turn.d, in_step * (uint32_t)a.side[1].token + turn.d};
+    for (uint32_t group = head_from; group < head_to; group += kHeadsAtOnce * kWaves) {
+        // twice: the largest values alone, then the codes
+        for (uint32_t x = once ? m : 0; x < 2 * m; x = x < m && x + chunk > m ? m : x + chunk) {
+            const bool writes = x >= m;
+            const uint32_t j0 = once ? 0 : writes ? x - m : x, left = m - j0;
+            uint4 k[kHeld], v[kHeld];
+            float old_at[2] = {0.f, 0.f};   // the scales that were there
+            auto take = [&](uint32_t h) {
 #pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) y[e] = (typename H::one)z[e];
-                words = as_words<H>(y);
-            }
-            if (wanted) *(uint4*)(a.q_out + token * a.q_out_token + h * a.q_out_head + 2 * turn.d) = words;
-        }
-    }
-    if (task >= tasks) return;
-    const typename Turn<H>::Weights k_weights = turn.weights(a.k_weight, a.adjacent != 0);
-    const uint32_t first = token - before, first_inside = inside - before;
-    for (; task < tasks; task += stride) {
-        const uint32_t unit = before + (task - of_q) * m, which = unit / of_kv, h = (unit - which * of_kv) * heads_at_once + in_step;
-        const Side8& side = a.side[which];
-        const bool is_k = which == 0, there = h < a.kv_heads, wanted = turn.mine && there;
-        const uint8_t* from = (is_k ? a.k + h * a.k_head : a.v + h * a.v_head) + 2 * turn.d;
-        const int64_t from_token = is_k ? a.k_token : a.v_token;
-        uint8_t* const to = side.at + block * side.block + h * side.head + turn.d;
-        float* const scale_at = side.scales + block * side.scale_block + h * side.scale_head;
-        const float old = first_inside != 0 && there ? *scale_at : 0.f;
-        const bool worked = is_k && (a.k_weight != nullptr || a.rope != nullptr);
-
-        float x[kTogether][8];
-        auto take = [&](uint32_t j0) {
-            uint4 words[kTogether];
-            typename Turn<H>::Line lines[kTogether];
-#pragma unroll
-            for (uint32_t n = 0; n < kTogether; ++n) {
-                const uint32_t t = first + (j0 + n < m ? j0 + n : j0);
-                words[n] = make_uint4(0, 0, 0, 0);
-                if (wanted) words[n] = *(const uint4*)(from + t * from_token);
-                if (worked) lines[n] = turn.line(a, a.rope == nullptr ? 0 : a.positions[t]);
-            }
-#pragma unroll
-            for (uint32_t n = 0; n < kTogether; ++n) {
-                if (worked) turn.apply(a, words[n], turn.factors(a, lines[n], k_weights), a.k_weight != nullptr, x[n]);
-                else floats_of<H>(words[n], x[n]);
-            }
-        };
-        uint32_t most = 0;
-        for (uint32_t j = 0; j < m; j += kTogether) {
-            take(j);
-#pragma unroll
-            for (uint32_t n = 0; n < kTogether; ++n) most = larger(most, x[n]);
-        }
-        if (!wanted) most = 0;   // (lanes beyond the head's channels)
-        most = over_row(most, a.row_power);
-        const float scale = scale_for<C>(most, old), by = inverse(scale);
-        const bool lost = !(scale == scale);
-        for (uint32_t j = 0; j < m; j += kTogether) {
-            if (m > kTogether) take(j);
-#pragma unroll
-            for (uint32_t n = 0; n < kTogether; ++n) {
-                uint2 codes = eight_codes<C>(x[n], by);
-                if (lost) codes = make_uint2(0, 0);
-                if (wanted && j + n < m) *(uint2*)(to + (first_inside + j + n) * side.token) = codes;
-            }
-        }
-        if (first_inside != 0) {
-            const float ratio = old * by;
-            const bool again = wanted && !lost && scale != old;
-            if (__any(again)) {
-                for (uint32_t t = 0; t < first_inside; t += kTogether) {
-                    uint2 words[kTogether];
-#pragma unroll
-                    for (uint32_t n = 0; n < kTogether; ++n)
-                        words[n] = again && t + n < first_inside ? *(const uint2*)(to + (t + n) * side.token) : make_uint2(0, 0);
-#pragma unroll
-                    for (uint32_t n = 0; n < kTogether; ++n) {
-                        float low[4], high[4];
-                        C::values(words[n].x, low), C::values(words[n].y, high);
-                        const uint2 codes = make_uint2(C::codes(low[0], low[1], low[2], low[3], ratio),
-                                                       C::codes(high[0], high[1], high[2], high[3], ratio));
-                        if (again && t + n < first_inside) *(uint2*)(to + (t + n) * side.token) = codes;
+                for (uint32_t n = 0; n < kHeld; ++n) {
+                    k[n] = v[n] = make_uint4(0, 0, 0, 0);
+                    if (n * rows < left && turn.mine && n * rows + in_step < left) {
+                        const uint32_t t = first + j0 + n * rows;
+                        k[n] = *(const uint4*)(a.k + h * a.k_head + t * a.k_token + k_off);
+                        v[n] = *(const uint4*)(a.v + h * a.v_head + t * a.v_token + v_off);
                     }
+                }
+#pragma unroll
+                for (uint32_t e = 0; e < 2; ++e)
+                    if (writes && inside != 0) old_at[e] = a.side[e].scales[block * a.side[e].scale_block + h * a.side[e].scale_head];
+            };
+            if (group + wave < head_to) take(group + wave);     // under way while the factors are made
+            if (worked) {
+                __syncthreads();   // (all have left those of before)
+                for (uint32_t n = wave; n < kHeld && n * rows < left; n += kWaves) {
+                    const uint32_t j = n * rows + in_step, t = first + j0 + j;
+                    int32_t position = __shfl(near_position, t - near_from);
+                    if (t - near_from >= 64) position = a.rope != nullptr && j < left ? a.positions[t] : 0;
+                    const typename Turn<H>::Line line = turn.line(a, position);
+                    const typename Turn<H>::Weights f = turn.factors(a, line, turn.weights(raw, normed, a.adjacent != 0));
+                    shared.factors[n][0][lane] = make_float4(f.own[0], f.own[1], f.own[2], f.own[3]);
+                    shared.factors[n][1][lane] = make_float4(f.own[4], f.own[5], f.own[6], f.own[7]);
+                    shared.factors[n][2][lane] = make_float4(f.other[0], f.other[1], f.other[2], f.other[3]);
+                    shared.factors[n][3][lane] = make_float4(f.other[4], f.other[5], f.other[6], f.other[7]);
+                }
+                __syncthreads();
+            }
+            for (uint32_t i = 0; i < kHeadsAtOnce; ++i) {
+                const uint32_t h = group + i * kWaves + wave;
+                if (h >= head_to) break;
+                if (i != 0) take(h);
+                uint32_t old[2];
+#pragma unroll
+                for (uint32_t e = 0; e < 2; ++e) old[e] = __builtin_amdgcn_readfirstlane(bits_of(old_at[e]));
+                float z[kHeld][8], by[kHeld];
+                uint32_t most[2] = {0, 0};
+                u16x2 most_v = (u16x2)(unsigned short)0;
+#pragma unroll
+                for (uint32_t n = 0; n < kHeld; ++n) {
+                    by[n] = 1.f;
+                    if (n * rows >= left) continue;   // (the same for all lanes)
+                    if (worked) {
+                        const float4 f0 = shared.factors[n][0][lane], f1 = shared.factors[n][1][lane];
+                        const float4 f2 = shared.factors[n][2][lane], f3 = shared.factors[n][3][lane];
+                        const typename Turn<H>::Weights f{{f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w},
+                                                          {f2.x, f2.y, f2.z, f2.w, f3.x, f3.y, f3.z, f3.w}};
+                        by[n] = turn.apply(a, k[n], f, normed, z[n]);
+                    } else {
+                        floats_of<H>(k[n], z[n]);
+                    }
+                    const uint32_t of_row = bits_of(float_of(larger(0, z[n])) * by[n]) & 0x7FFFFFFFu;
+                    if (turn.mine && n * rows + in_step < left && of_row > most[0]) most[0] = of_row;
+                    most_v = larger(most_v, v[n]);
+                }
+                most[1] = as_float_bits<H>(most_v);
+#pragma unroll
+                for (uint32_t e = 0; e < 2; ++e) {
+                    most[e] = over_wave(most[e], [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+                    if (once) continue;
+                    uint32_t* const kept = &shared.largest[wave][i][e];   // (the wavefront's own)
+                    if (!writes) *kept = j0 != 0 && *kept > most[e] ? *kept : most[e];
+                    else most[e] = *kept;
+                }
+                if (!writes) continue;
+#pragma unroll
+                for (uint32_t e = 0; e < 2; ++e) {
+                    const Side8& side = a.side[e];
+                    const uint32_t scale = scale_for<C>(__builtin_amdgcn_readfirstlane(most[e]), old[e]);
+                    const float inv = inverse(scale);
+                    const bool lost = is_lost(scale);
+                    uint8_t* const at = side.at + block * side.block + h * side.head;
+#pragma unroll
+                    for (uint32_t n = 0; n < kHeld; ++n) {
+                        if (n * rows >= left) continue;
+                        float y[8];
+                        if (e == 0) {
+#pragma unroll
+                            for (uint32_t c = 0; c < 8; ++c) y[c] = z[n][c];
+                        } else {
+                            floats_of<H>(v[n], y);
+                        }
+                        uint2 codes = eight_codes<C>(y, e == 0 ? by[n] * inv : inv);
+                        if (lost) codes = make_uint2(0, 0);
+                        if (turn.mine && n * rows + in_step < left)
+                            *(uint2*)(at + (inside + j0 + n * rows) * side.token + code_off[e]) = codes;
+                    }
+                    // with the first chunk: the codes that are there to the new scale
+                    if (j0 == 0 && inside != 0 && !lost && scale != old[e]) {
+                        const float ratio = float_of(old[e]) * inv;
+                        for (uint32_t t = 0; t < inside; t += kTogether * rows) {
+                            uint2 words[kTogether];
+#pragma unroll
+                            for (uint32_t n = 0; n < kTogether; ++n) {
+                                words[n] = make_uint2(0, 0);
+                                if (turn.mine && t + n * rows + in_step < inside)
+                                    words[n] = *(const uint2*)(at + (t + n * rows) * side.token + code_off[e]);
+                            }
+#pragma unroll
+                            for (uint32_t n = 0; n < kTogether; ++n) {
+                                float low[4], high[4];
+                                C::values(words[n].x, low), C::values(words[n].y, high);
+                                const uint2 codes = make_uint2(C::codes(low[0], low[1], low[2], low[3], ratio),
+                                                               C::codes(high[0], high[1], high[2], high[3], ratio));
+                                if (turn.mine && t + n * rows + in_step < inside)
+                                    *(uint2*)(at + (t + n * rows) * side.token + code_off[e]) = codes;
+                            }
+                        }
+                    }
+                    // ... and the scale with the last, as each reads what it was
+                    if (left <= chunk && lane == 0) side.scales[block * side.scale_block + h * side.scale_head] = float_of(scale);
                 }
             }
         }
-        if (turn.part == 0 && there) *scale_at = scale;
+    }
+}
+
+// The runs that begin in a window of tokens are taken by its kv_ways workgroups, whole, their heads in equal shares; the window's
+// queries by the workgroups of blockIdx.y >= kv_ways, a token and some of its heads a wavefront.
+constexpr uint32_t kWindow = 16;
+template <class H, class C, uint32_t kHeld>
+__global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
+    __shared__ AppendShared<kHeld> shared;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    // windows a block apart follow each other, so that those in which a prompt's runs begin are spread over all XCDs
+    const uint32_t apart = gridDim.x / a.spread, window = (blockIdx.x % apart * a.spread + blockIdx.x / apart) * kWindow;
+    const Turn<H> turn(a);
+    const uint32_t rows = 64u >> a.row_power, in_step = lane >> a.row_power;
+
+    if (blockIdx.y >= a.kv_ways) {
+        // a wavefront a token and some of its steps
+        const uint32_t turns = (blockIdx.y - a.kv_ways) * kWaves + wave, token = window + turns % kWindow;
+        const uint32_t ways = (gridDim.y - a.kv_ways) * kWaves / kWindow;
+        const uint32_t of_q = (a.heads + rows - 1) / rows;
+        uint32_t task = turns / kWindow;
+        if (token >= a.tokens || task >= of_q || task >= ways) return;
+        uint4 words[kStepsAtOnce];
+        auto take = [&](uint32_t first) {
+#pragma unroll
+            for (uint32_t n = 0; n < kStepsAtOnce; ++n) {
+                const uint32_t h = (first + n * ways) * rows + in_step;
+                words[n] = make_uint4(0, 0, 0, 0);
+                if (turn.mine && h < a.heads) words[n] = *(const uint4*)(a.q + token * a.q_token + h * a.q_head + 2 * turn.d);
+            }
+        };
+        take(task);
+        const typename Turn<H>::Raw raw = turn.raw_weights(a.q_weight);
+        const typename Turn<H>::Weights w = turn.factors(a, turn.line(a, a.rope == nullptr ? 0 : constant(a.positions, token)),
+                                                         turn.weights(raw, a.q_weight != nullptr, a.adjacent != 0));
+        for (; task < of_q; task += kStepsAtOnce * ways) {
+            uint4 now[kStepsAtOnce];
+#pragma unroll
+            for (uint32_t n = 0; n < kStepsAtOnce; ++n) now[n] = words[n];
+            if (task + kStepsAtOnce * ways < of_q) take(task + kStepsAtOnce * ways);   // under way while these are worked on
+#pragma unroll
+            for (uint32_t n = 0; n < kStepsAtOnce; ++n) {
+                if (task + n * ways >= of_q) break;
+                const uint32_t h = (task + n * ways) * rows + in_step;
+                if (a.q_weight != nullptr || a.rope != nullptr) {   // (others are copied)
+                    float z[8];
+                    const float by = turn.apply(a, now[n], w, a.q_weight != nullptr, z);
+                    typename H::eight y;
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) y[e] = (typename H::one)(z[e] * by);
+                    now[n] = as_words<H>(y);
+                }
+                if (turn.mine && h < a.heads) *(uint4*)(a.q_out + token * a.q_out_token + h * a.q_out_head + 2 * turn.d) = now[n];
+            }
+        }
+        return;
+    }
+
+    // Where runs begin: lane l looks at token window - 1 + l.
+    auto slot_at = [&](uint32_t t) { return t < a.tokens ? a.slots[t] : (int64_t)-1; };
+    auto begins = [&](uint32_t t, int64_t slot, int64_t slot_before) {   // ... or nothing does
+        return t >= a.tokens || t == 0 || (uint64_t)slot >= a.pool_tokens || slot != slot_before + 1 ||
+               split_by((uint64_t)slot, a.block_tokens, a.by_block).rest == 0;
+    };
+    const int64_t near = window + lane >= 1 ? slot_at(window + lane - 1) : -1;
+    const uint64_t marks = __ballot(begins(window + lane - 1, near, __shfl_up(near, 1))) & ~1ull;
+    // ... and its position; what is asked for here is there when the runs are known
+    const uint32_t near_from = window - 1;
+    const int32_t near_position = a.rope != nullptr && near_from + lane < a.tokens ? a.positions[near_from + lane] : 0;
+    const typename Turn<H>::Raw raw = turn.raw_weights(a.k_weight);
+    // bit i: token window + i begins a run that is stored
+    const uint64_t in_pool = __ballot((uint64_t)near < a.pool_tokens && window + lane - 1 < a.tokens);
+    uint64_t in_window = (marks & in_pool) >> 1 & ((1ull << kWindow) - 1);
+    const uint32_t tasks = (uint32_t)__builtin_popcountll(in_window) * a.kv_heads;   // heads of all runs
+    const uint32_t from = (uint32_t)((uint64_t)tasks * blockIdx.y / a.kv_ways), to = (uint32_t)((uint64_t)tasks * (blockIdx.y + 1) / a.kv_ways);
+    for (uint32_t task = 0; in_window != 0 && task < to; in_window &= in_window - 1, task += a.kv_heads) {
+        if (task + a.kv_heads <= from) continue;
+        const uint32_t at = __builtin_ctzll(in_window), first = window + at;
+        const uint64_t slot = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)((uint64_t)near >> 32), at + 1) << 32 |
+                              (uint32_t)__builtin_amdgcn_readlane((uint32_t)near, at + 1);
+        uint32_t m = 0;
+        if (const uint64_t later = marks >> 1 & ~((2ull << at) - 1); later != 0) {
+            m = __builtin_ctzll(later) - at;
+        } else {
+            for (uint32_t t = window + 63; m == 0; t += 64) {
+                const uint64_t next = __ballot(begins(t + lane, slot_at(t + lane), slot_at(t + lane - 1)));
+                if (next != 0) m = t + __builtin_ctzll(next) - first;
+            }
+        }
+        const Split place = split_by(slot, a.block_tokens, a.by_block);
+        append_run<H, C, kHeld>(a, turn, shared, first, m, of_first_lane(place.whole), __builtin_amdgcn_readfirstlane(place.rest),
+                                from > task ? from - task : 0, to - task < a.kv_heads ? to - task : a.kv_heads, raw, near_position, near_from);
     }
 }
 
@@ -353,38 +563,8 @@ template <class H, class C>
 __global__ __launch_bounds__(kThreads) void store8_kernel(MoveArgs a) {
     Unit u;
     if (!unit_of(a, u)) return;
-    uint4 words[kTogether];
-    auto take = [&](uint32_t t) {
-#pragma unroll
-        for (uint32_t n = 0; n < kTogether; ++n) {
-            words[n] = make_uint4(0, 0, 0, 0);
-            if (u.wanted && t + n < u.count) words[n] = *(const uint4*)(u.half + (t + n) * u.half_token);
-        }
-    };
-    uint32_t most = 0;
-    float x[8];
-    for (uint32_t t = 0; t < u.count; t += kTogether) {
-        take(t);
-#pragma unroll
-        for (uint32_t n = 0; n < kTogether; ++n) {
-            floats_of<H>(words[n], x);
-            most = larger(most, x);
-        }
-    }
-    most = over_row(most, a.row_power);
-    const float scale = scale_for<C>(most, 0.f), by = inverse(scale);
-    const bool lost = !(scale == scale);
-    for (uint32_t t = 0; t < u.count; t += kTogether) {
-        if (u.count > kTogether) take(t);
-#pragma unroll
-        for (uint32_t n = 0; n < kTogether; ++n) {
-            floats_of<H>(words[n], x);
-            uint2 codes = eight_codes<C>(x, by);
-            if (lost) codes = make_uint2(0, 0);
-            if (u.wanted && t + n < u.count) *(uint2*)(u.codes + (t + n) * u.code_token) = codes;
-        }
-    }
-    if (u.part == 0 && u.there) *u.scale = scale;
+    const uint32_t scale = convert_unit<H, C>(u.half, u.half_token, u.count, To{u.codes, u.code_token, u.wanted}, a.row_power);
+    if (u.part == 0 && u.there) *u.scale = float_of(scale);
 }
 
 template <class H, class C>
@@ -482,6 +662,9 @@ int pgcm_kv8_append(const pgcm_kv8_cache* cache, const pgcm_kv_append_args* args
         !aligned(args->v, args->v_token, args->v_head) || !aligned(args->q_out, args->q_out_token, args->q_out_head) ||
         !aligned(args->q_weight) || !aligned(args->k_weight) || !aligned(args->rope))
         return PGCM_ERR_ALIGN;
+    // (lanes' places within the tokens that a wavefront has side by side are counted in 32 bits)
+    for (const int64_t stride : {args->k_token, args->v_token, cache->k_token, cache->v_token})
+        if (stride < 0 || stride > kMostAppendStride) return PGCM_ERR_ARG;
     Append8Args a{};
     a.q = (const uint8_t*)args->q, a.k = (const uint8_t*)args->k, a.v = (const uint8_t*)args->v;
     a.q_weight = (const uint8_t*)args->q_weight, a.k_weight = (const uint8_t*)args->k_weight;
@@ -496,23 +679,40 @@ int pgcm_kv8_append(const pgcm_kv8_cache* cache, const pgcm_kv_append_args* args
     a.block_tokens = cache->block_tokens;
     a.rope_positions = args->rope_positions, a.rope_dim = args->rope_dim, a.adjacent = args->adjacent;
     a.row_power = row_power_of(dim);
-    a.eps = args->eps, a.by_dim = 1.f / (float)dim;
-    const uint32_t at_once = 64u >> a.row_power;
-    const uint32_t tasks = (a.heads + at_once - 1) / at_once + 2 * ((a.kv_heads + at_once - 1) / at_once);
-    const uint32_t passes = (tasks + kWaves - 1) / kWaves;
-    uint32_t ways = args->tokens >= 1024 ? 1 : (1024 + args->tokens - 1) / args->tokens;
-    if (ways > passes) ways = passes;
-    if (!launchable(args->tokens, kThreads)) return PGCM_ERR_ARG;
-    const dim3 grid(args->tokens, ways);
+    a.eps = args->eps, a.by_dim = 1.f / (float)dim, a.by_block = 1.0 / cache->block_tokens;
+    const uint32_t windows = (args->tokens + kWindow - 1) / kWindow, in_window = args->tokens < kWindow ? args->tokens : kWindow;
+    // about kGroups workgroups of either kind where there is that much to do
+    constexpr uint32_t kGroups = 1024;
+    auto ways = [&](uint64_t most) {   // of so many wavefronts' work
+        const uint64_t groups = (most + kWaves - 1) / kWaves;
+        return windows >= kGroups || groups <= 1 ? 1u : (uint32_t)(kGroups / windows < groups ? kGroups / windows : groups);
+    };
+    // (a prompt's runs begin in as many windows as there are blocks: the others' workgroups have nothing to do)
+    const uint64_t of_kv = (uint64_t)in_window * a.kv_heads;
+    a.spread = cache->block_tokens / kWindow < windows ? cache->block_tokens / kWindow : windows;
+    const uint64_t most_ways = (of_kv + kWaves - 1) / kWaves, some_ways = (uint64_t)ways(of_kv) * a.spread;
+    a.kv_ways = (uint32_t)(some_ways < most_ways ? some_ways : most_ways);
+    const uint32_t at_once = 64u >> a.row_power, of_q = (a.heads + at_once - 1) / at_once;
+    uint32_t q_ways = of_q == 0 ? 0 : ways((uint64_t)kWindow * of_q);
+    if (q_ways != 0) q_ways = (q_ways + kWindow / kWaves - 1) / (kWindow / kWaves) * (kWindow / kWaves);   // all tokens in each round
+    const uint32_t groups = (windows + a.spread - 1) / a.spread * a.spread;
+    if (!launchable(groups, kThreads)) return PGCM_ERR_ARG;
+    const dim3 grid(groups, a.kv_ways + q_ways);
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const bool f16 = cache->half == PGCM_KV_F16;
-    if (cache->code == PGCM_KV8_INT8) {
-        if (f16) append8_kernel<F16, Int8><<<grid, kThreads, 0, stream>>>(a);
-        else append8_kernel<Bf16, Int8><<<grid, kThreads, 0, stream>>>(a);
-    } else {
-        if (f16) append8_kernel<F16, E4m3><<<grid, kThreads, 0, stream>>>(a);
-        else append8_kernel<Bf16, E4m3><<<grid, kThreads, 0, stream>>>(a);
-    }
+    // blocks of sixteen tokens fit four steps of up to 128 channels; others are worth more registers
+    const bool longer = cache->block_tokens > 4 * at_once, f16 = cache->half == PGCM_KV_F16;
+    auto launch = [&](auto code) {
+        typedef decltype(code) C;
+        if (longer) {
+            if (f16) append8_kernel<F16, C, 8><<<grid, kThreads, 0, stream>>>(a);
+            else append8_kernel<Bf16, C, 8><<<grid, kThreads, 0, stream>>>(a);
+        } else {
+            if (f16) append8_kernel<F16, C, 4><<<grid, kThreads, 0, stream>>>(a);
+            else append8_kernel<Bf16, C, 4><<<grid, kThreads, 0, stream>>>(a);
+        }
+    };
+    if (cache->code == PGCM_KV8_INT8) launch(Int8());
+    else launch(E4m3());
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 

@@ -29,6 +29,11 @@ inline uint32_t row_power_of(uint32_t head_dim) {
 }
 
 // ---- device side
+// What nothing writes to while the kernel runs may come through the scalar cache.
+template <class T>
+__device__ __forceinline__ T constant(const T* at, size_t n) {
+    return ((const __attribute__((address_space(4))) T*)(uintptr_t)at)[n];
+}
 constexpr int32_t kLeastPower = -100;   // of a scale
 constexpr uint32_t kNotFinite = 0x7F800000u;
 

@@ -23,10 +23,6 @@ struct WindowArgs {
 
 // ---- device side
 
-// What nothing writes to while the kernel runs may come through the scalar cache.
-__device__ __forceinline__ int32_t constant(const int32_t* at, size_t n) {
-    return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)at)[n];
-}
 __device__ __forceinline__ uint32_t clamped(int32_t x, uint32_t most) {
     return x <= 0 ? 0u : (uint32_t)x < most ? (uint32_t)x : most;
 }
