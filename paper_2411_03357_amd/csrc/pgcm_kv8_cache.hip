@@ -270,11 +270,6 @@ __device__ __forceinline__ Split split_by(uint64_t x, uint32_t by, double one_by
     return Split{q, (uint32_t)r};
 }
 
-__device__ __forceinline__ uint64_t of_first_lane(uint64_t x) {
-    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)x), high = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
-    return (uint64_t)high << 32 | low;
-}
-
 // Keys and values of a run, m tokens from `first` on, to `block` from place `inside` on: heads [head_from, head_to), a wavefront
 // of the workgroup one at a time.  A lane's rows are tokens side by side, kHeld times as many held in registers (a "chunk"): so a
 // head's largest value is found in the wavefront.  The factors that norm and rotation multiply a chunk's tokens with are made once
@@ -479,12 +474,12 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
 
     // Where runs begin: lane l looks at token window - 1 + l.
     auto slot_at = [&](uint32_t t) { return t < a.tokens ? a.slots[t] : (int64_t)-1; };
-    auto begins = [&](uint32_t t, int64_t slot, int64_t slot_before) {   // ... or nothing does
-        return t >= a.tokens || t == 0 || (uint64_t)slot >= a.pool_tokens || slot != slot_before + 1 ||
-               split_by((uint64_t)slot, a.block_tokens, a.by_block).rest == 0;
+    auto begins = [&](uint32_t t, int64_t slot, int64_t slot_before, uint32_t inside) {   // ... or nothing does
+        return t >= a.tokens || t == 0 || (uint64_t)slot >= a.pool_tokens || slot != slot_before + 1 || inside == 0;
     };
     const int64_t near = window + lane >= 1 ? slot_at(window + lane - 1) : -1;
-    const uint64_t marks = __ballot(begins(window + lane - 1, near, __shfl_up(near, 1))) & ~1ull;
+    const Split near_place = split_by((uint64_t)near < a.pool_tokens ? (uint64_t)near : 0, a.block_tokens, a.by_block);
+    const uint64_t marks = __ballot(begins(window + lane - 1, near, __shfl_up(near, 1), near_place.rest)) & ~1ull;
     // ... and its position; what is asked for here is there when the runs are known
     const uint32_t near_from = window - 1;
     const int32_t near_position = a.rope != nullptr && near_from + lane < a.tokens ? a.positions[near_from + lane] : 0;
@@ -493,23 +488,26 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
     const uint64_t in_pool = __ballot((uint64_t)near < a.pool_tokens && window + lane - 1 < a.tokens);
     uint64_t in_window = (marks & in_pool) >> 1 & ((1ull << kWindow) - 1);
     const uint32_t tasks = (uint32_t)__builtin_popcountll(in_window) * a.kv_heads;   // heads of all runs
-    const uint32_t from = (uint32_t)((uint64_t)tasks * blockIdx.y / a.kv_ways), to = (uint32_t)((uint64_t)tasks * (blockIdx.y + 1) / a.kv_ways);
+    const uint32_t share = (tasks + a.kv_ways - 1) / a.kv_ways, from = share * blockIdx.y;
+    const uint32_t to = from + share < tasks ? from + share : tasks;
+    if (from >= tasks) return;
     for (uint32_t task = 0; in_window != 0 && task < to; in_window &= in_window - 1, task += a.kv_heads) {
         if (task + a.kv_heads <= from) continue;
         const uint32_t at = __builtin_ctzll(in_window), first = window + at;
-        const uint64_t slot = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)((uint64_t)near >> 32), at + 1) << 32 |
-                              (uint32_t)__builtin_amdgcn_readlane((uint32_t)near, at + 1);
         uint32_t m = 0;
         if (const uint64_t later = marks >> 1 & ~((2ull << at) - 1); later != 0) {
             m = __builtin_ctzll(later) - at;
         } else {
             for (uint32_t t = window + 63; m == 0; t += 64) {
-                const uint64_t next = __ballot(begins(t + lane, slot_at(t + lane), slot_at(t + lane - 1)));
+                const int64_t slot = slot_at(t + lane);
+                const uint32_t rest = split_by((uint64_t)slot < a.pool_tokens ? (uint64_t)slot : 0, a.block_tokens, a.by_block).rest;
+                const uint64_t next = __ballot(begins(t + lane, slot, slot_at(t + lane - 1), rest));
                 if (next != 0) m = t + __builtin_ctzll(next) - first;
             }
         }
-        const Split place = split_by(slot, a.block_tokens, a.by_block);
-        append_run<H, C, kHeld>(a, turn, shared, first, m, of_first_lane(place.whole), __builtin_amdgcn_readfirstlane(place.rest),
+        const uint32_t low = __builtin_amdgcn_readlane((uint32_t)near_place.whole, at + 1);
+        const uint32_t high = __builtin_amdgcn_readlane((uint32_t)(near_place.whole >> 32), at + 1);
+        append_run<H, C, kHeld>(a, turn, shared, first, m, (uint64_t)high << 32 | low, __builtin_amdgcn_readlane(near_place.rest, at + 1),
                                 from > task ? from - task : 0, to - task < a.kv_heads ? to - task : a.kv_heads, raw, near_position, near_from);
     }
 }
