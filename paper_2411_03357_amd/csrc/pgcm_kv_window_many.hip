@@ -103,8 +103,7 @@ struct Rows {
 // Sixteen bytes a lane from base + at to LDS, without a register.  As an instruction of its own, since of the compiler's it waits
 // for all that are under way before it reads anything from LDS; who reads what it brings waits for it.  (Nothing else of these
 // kernels is compiled to use m0.)
-__device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t at, uint8_t* to) {
-    const uint32_t place = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)to);
+__device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t at, uint32_t place) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(place), "v"(at), "s"(base) : "memory");
 }
 
@@ -172,40 +171,63 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
         k_at[n] = (n * R::kRowsAtOnce + t) * (uint32_t)a.k_token + 16 * (pk < there ? pk : 0);
         v_at[n] = (n * R::kRowsAtOnce + t) * (uint32_t)a.v_token + 16 * (pv < there ? pv : 0);
     }
-    // Sixteen tiles' pieces at a time, lane by lane: their blocks
+    // Sixteen tiles' pieces at a time, lane by lane: where they lie, and, as bits, which of them are on the device, which do not all
+    // of the item's or of the wavefront's rows see whole, and which does any of the wavefront's see.
     constexpr uint32_t kBatch = 64 / kTilePieces;
+    auto token_of = [&](uint32_t tile) { return seen.piece(tile * kTilePieces + lane) * kPiece; };
     auto find = [&](uint32_t tile) {
-        const uint32_t t = tile + lane / kTilePieces, n = t * kTilePieces + lane % kTilePieces;
-        if (t >= to || n >= split.pieces) return ~0u;
-        return (uint32_t)a.tables[x.request * a.table_row + seen.piece(n) * kPiece / a.block_tokens];
+        if (tile + lane / kTilePieces >= to || tile * kTilePieces + lane >= split.pieces) return ~0u;
+        return (uint32_t)a.tables[x.request * a.table_row + token_of(tile) / a.block_tokens];
     };
-    uint32_t ahead = from, next = find(ahead), batch = from, block = ~0u;
-    uint64_t live = 0;
+    const uint32_t all_end = x.end_of(x.first / a.group), all_low = low_of(a, x.end_of((x.first + x.rows - 1) / a.group));
+    uint32_t ahead = from, next = find(ahead), piece_at = 0;
+    uint64_t live = 0, hidden_all = 0, hidden_mine = 0, seen_mine = 0, piece_k = 0, piece_v = 0;
+    auto use = [&]() {
+        piece_at = token_of(ahead);
+        const bool there = next < a.blocks;
+        const uint32_t block = there ? next : 0, inside = there ? piece_at % a.block_tokens : 0;   // (else any that is there)
+        piece_k = (uint64_t)(uintptr_t)a.k + x.kv_head * a.k_head + block * a.k_block + inside * a.k_token;
+        piece_v = (uint64_t)(uintptr_t)a.v + x.kv_head * a.v_head + block * a.v_block + inside * a.v_token;
+        const uint32_t piece_end = piece_at + kPiece;
+        live = __ballot(there);
+        hidden_all = __ballot(!there || piece_end > all_end || (piece_at < all_low && piece_end > a.sinks));
+        hidden_mine = __ballot(!there || piece_end > least_end || (piece_at < most_low && piece_end > a.sinks));
+        seen_mine = __ballot(there && piece_at < most_end && (piece_end > least_low || piece_at < a.sinks));
+        ahead += kBatch;
+        next = find(ahead);
+    };
+    auto lane_of = [](uint64_t x, uint32_t j) {
+        const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, j), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), j);
+        return (const uint8_t*)(uintptr_t)((uint64_t)hi << 32 | lo);   // (what comes from a lane is an int)
+    };
     struct Tile {
-        uint32_t piece, here;   // its first piece; which of its four are on the device
+        uint32_t here, hidden_all, hidden_mine, seen_mine;   // bits of its four pieces
+        uint32_t at[kTilePieces];                            // their first tokens, where any is hidden
     };
+    // where the wavefront's piece goes in LDS
+    const uint32_t rows_at = __builtin_amdgcn_readfirstlane(
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&shared.rows[0][0][0] + wave * 16 * R::kBytes);
     // the next tile of which any piece is there; its rows are asked for
     auto ask = [&](Tile& t, uint32_t turn) {
         while (live == 0) {
             if (ahead >= to) return false;
-            batch = ahead, block = next;
-            live = __ballot(block < a.blocks);
-            ahead += kBatch;
-            next = find(ahead);
+            use();
         }
         const uint32_t n = __builtin_ctzll(live) / kTilePieces * kTilePieces;
-        t.piece = batch * kTilePieces + n;
         t.here = (uint32_t)(live >> n) & 15;
+        t.hidden_all = (uint32_t)(hidden_all >> n) & 15;
+        t.hidden_mine = (uint32_t)(hidden_mine >> n) & 15;
+        t.seen_mine = (uint32_t)(seen_mine >> n) & 15;
         live &= ~(15ull << n);
-        const bool there = t.here >> wave & 1;
-        const uint64_t from_block = there ? (uint32_t)__builtin_amdgcn_readlane(block, n + wave) : 0;   // (else any that is there)
-        const uint32_t inside = there ? seen.piece(t.piece + wave) * kPiece % a.block_tokens : 0;
-        const uint8_t* const k = a.k + x.kv_head * a.k_head + from_block * a.k_block + inside * a.k_token;
-        const uint8_t* const v = a.v + x.kv_head * a.v_head + from_block * a.v_block + inside * a.v_token;
+        if (t.hidden_all != 0)
 #pragma unroll
-        for (uint32_t i = 0; i < R::kAsked; ++i) to_lds(k, k_at[i], shared.rows[turn][0] + wave * 16 * R::kBytes + i * 1024);
+            for (uint32_t p = 0; p < kTilePieces; ++p) t.at[p] = __builtin_amdgcn_readlane(piece_at, n + p);
+        const uint8_t* const k = lane_of(piece_k, n + wave);
+        const uint8_t* const v = lane_of(piece_v, n + wave);
 #pragma unroll
-        for (uint32_t i = 0; i < R::kAsked; ++i) to_lds(v, v_at[i], shared.rows[turn][1] + wave * 16 * R::kBytes + i * 1024);
+        for (uint32_t i = 0; i < R::kAsked; ++i) to_lds(k, k_at[i], rows_at + turn * 2 * kTile * R::kBytes + i * 1024);
+#pragma unroll
+        for (uint32_t i = 0; i < R::kAsked; ++i) to_lds(v, v_at[i], rows_at + (turn * 2 + 1) * kTile * R::kBytes + i * 1024);
         return true;
     };
 
@@ -219,16 +241,6 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
 #pragma unroll
     for (uint32_t n = 0; n < kOut; ++n) v_from[n] = v_token * R::kBytes + 16 * v_place(n) + 8 * (lane % 2);
 
-    // whether any of these rows does not see all of a tile's tokens
-    auto hidden_of = [&](const Tile& t, uint32_t least_end, uint32_t most_low) {
-        uint32_t hidden = 0;
-#pragma unroll
-        for (uint32_t p = 0; p < kTilePieces; ++p) {
-            const uint32_t at = seen.piece(t.piece + p) * kPiece, to_end = at + kPiece;
-            hidden |= (t.here >> p & 1 ^ 1) | (to_end > least_end) | ((at < most_low) & (to_end > a.sinks));
-        }
-        return hidden != 0;
-    };
     // Tokens that a row does not see have a weight of zero, and zero times what is no number is none.  So where there are such
     // tokens, the wavefront that asked for a piece of V takes what is not finite out of it, and writes down where that was.
     auto clean = [&](uint32_t turn) {
@@ -265,14 +277,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
     };
     uint32_t spoilt[kOut] = {};   // of the lane's row: the channels that saw such a value, bit 8 i + 4 hh + r (as in a row of odd)
 
-    auto work = [&](const Tile& t, uint32_t turn, bool cleaned) {
-        uint32_t some = 0;
-#pragma unroll
-        for (uint32_t p = 0; p < kTilePieces; ++p) {
-            const uint32_t at = seen.piece(t.piece + p) * kPiece;
-            some |= (t.here >> p & 1) & (at < most_end) & ((at + kPiece > least_low) | (at < a.sinks));
-        }
-        if (some == 0) return;
+    auto work = [&](const Tile& t, uint32_t turn) {
+        if (t.seen_mine == 0) return;
         const uint8_t* const k_rows = shared.rows[turn][0];
         const uint8_t* const v_rows = shared.rows[turn][1];
         f32x16 w[2];
@@ -288,12 +294,12 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
                 if (kDim == 256 && c % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (reads made far ahead have no registers)
             }
         }
-        if (cleaned && (hidden_of(t, least_end, most_low) || (shared.any[turn][0] | shared.any[turn][1] | shared.any[turn][2] | shared.any[turn][3]) != 0)) {
+        if (t.hidden_all != 0 && (t.hidden_mine != 0 || (shared.any[turn][0] | shared.any[turn][1] | shared.any[turn][2] | shared.any[turn][3]) != 0)) {
             // bit 16 b + r: whether the lane's row sees the token of w[b][r]
             uint32_t sees = 0;
 #pragma unroll
             for (uint32_t p = 0; p < kTilePieces; ++p) {
-                const uint32_t at = seen.piece(t.piece + p) * kPiece;
+                const uint32_t at = t.at[p];
                 auto below = [&](uint32_t x) {   // tokens of the piece before x
                     return x <= at ? 0u : x - at < kPiece ? (1u << (x - at)) - 1 : 0xFFFFu;
                 };
@@ -355,17 +361,15 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
     };
 
     {
-        const uint32_t all_end = x.end_of(x.first / a.group), all_low = low_of(a, x.end_of((x.first + x.rows - 1) / a.group));
         Tile now{}, after{};
         uint32_t turn = 0;
         bool more = ask(now, 0);
         while (more) {
-            const bool hidden = hidden_of(now, all_end, all_low);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the wavefront's rows are in LDS
-            if (hidden) clean(turn);
+            if (now.hidden_all != 0) clean(turn);
             __syncthreads();                                   // ... and the others', and all have left the tile before
             more = ask(after, turn ^ 1);
-            work(now, turn, hidden);
+            work(now, turn);
             now = after;
             turn ^= 1;
         }
