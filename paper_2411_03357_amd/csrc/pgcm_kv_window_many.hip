@@ -334,6 +334,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
             for (uint32_t n = 0; n < kOut; ++n) sum[n] *= keep;
         }
         const float down = top == -INFINITY ? 0.f : -top;
+        __builtin_amdgcn_s_setprio(1);
         typedef __attribute__((address_space(3))) s16x4* Lds;
 #pragma unroll
         for (uint32_t b = 0; b < 2; ++b)
@@ -358,6 +359,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
                 }
                 if (kDim == 256) __builtin_amdgcn_sched_barrier(0);
             }
+        __builtin_amdgcn_s_setprio(0);
     };
 
     {
