@@ -110,17 +110,25 @@ struct Codes {
         f16x8 x[2 * kSteps];
         float by;
     };
+    struct Raw {
+        uint4 x[2 * kSteps];
+    };
     template <bool kExact>
-    static __device__ __forceinline__ void query(Query& q, const WindowArgs& a, const uint8_t* row, bool there, uint32_t g) {
+    static __device__ __forceinline__ void ask_query(Raw& q, const WindowArgs& a, const uint8_t* row, bool there, uint32_t g) {
+#pragma unroll
+        for (uint32_t c = 0; c < 2 * kSteps; ++c) {
+            const uint32_t d = 64 * (c / 2) + 16 * g + 8 * (c % 2);
+            q.x[c] = make_uint4(0, 0, 0, 0);
+            if (there && (kExact || d < a.head_dim)) q.x[c] = *(const uint4*)(row + 2 * d);
+        }
+    }
+    static __device__ __forceinline__ void make_query(Query& q, const Raw& raw) {
         float x[2 * kSteps][8];
         float most = 0.f;
         bool odd = false;
 #pragma unroll
         for (uint32_t c = 0; c < 2 * kSteps; ++c) {
-            const uint32_t d = 64 * (c / 2) + 16 * g + 8 * (c % 2);
-            uint4 words = make_uint4(0, 0, 0, 0);
-            if (there && (kExact || d < a.head_dim)) words = *(const uint4*)(row + 2 * d);
-            const typename H::eight y = as_eight<H>(words);
+            const typename H::eight y = as_eight<H>(raw.x[c]);
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) {
                 x[c][e] = (float)y[e];
@@ -235,8 +243,9 @@ struct Halves {
         uint4 x[kSteps];
         static constexpr float by = 1.f;
     };
+    typedef Query Raw;
     template <bool kExact>
-    static __device__ __forceinline__ void query(Query& q, const WindowArgs& a, const uint8_t* row, bool there, uint32_t g) {
+    static __device__ __forceinline__ void ask_query(Raw& q, const WindowArgs& a, const uint8_t* row, bool there, uint32_t g) {
 #pragma unroll
         for (uint32_t c = 0; c < kSteps; ++c) {
             const uint32_t d = 32 * c + 8 * g;
@@ -244,6 +253,7 @@ struct Halves {
             if (there && (kExact || d < a.head_dim)) q.x[c] = *(const uint4*)(row + 2 * d);
         }
     }
+    static __device__ __forceinline__ void make_query(Query& q, const Raw& raw) { q = raw; }
     static __device__ __forceinline__ f32x4 scores(const Held& held, uint32_t p, const Query& q, const Here&) {
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -368,7 +378,8 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
             before = __builtin_amdgcn_readlane(upto, 63);
         }
         if (!found) return;
-    } else {
+    }
+    if constexpr (!kCut) {
         of = row_of(a, row);
         of.request = __builtin_amdgcn_readfirstlane(of.request), of.end = __builtin_amdgcn_readfirstlane(of.end);
         if (of.request == ~0u) return;
@@ -379,8 +390,8 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
     const uint32_t pieces = seen.pieces(), tiles = tiles_of<S>(a, of), low = low_of(a, of.end);
     const uint32_t from = tiles * part / parts, to = tiles * (part + 1) / parts;
 
-    typename S::Query query;
-    S::template query<kExact>(query, a, a.q + row * a.q_token + (first_head + (i < heads ? i : 0)) * a.q_head, i < heads, g);
+    typename S::Raw raw;
+    S::template ask_query<kExact>(raw, a, a.q + row * a.q_token + (first_head + (i < heads ? i : 0)) * a.q_head, i < heads, g);
 
     f32x4 sum[L::kParts][L::kRun];
 #pragma unroll
@@ -388,7 +399,6 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
 #pragma unroll
         for (uint32_t t = 0; t < L::kRun; ++t) sum[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, total = 0.f;
-    const float scale = a.scale * query.by;
 
     // Where the wavefront's pieces lie: lane l has the l-th of a batch, kPieces of each tile.
     constexpr uint32_t kBatch = 64 / kPieces;   // tiles
@@ -459,6 +469,8 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
 #pragma unroll
         for (uint32_t p = 0; p < kPieces; ++p) S::template load<kExact>(held, a, p, at[p], g, i);
     };
+    typename S::Query query;
+    float scale = 0.f;
     auto work = [&](typename S::Held& held, const Here (&at)[kPieces]) {
         float s[kPieces][4];
         float most = -INFINITY;
@@ -503,6 +515,8 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
         Here at[2][kPieces];
         if (seek(at[0])) {
             load(held[0], at[0]);
+            S::make_query(query, raw);
+            scale = a.scale * query.by;
             while (true) {
                 const bool more = seek(at[1]);
                 if (more) load(held[1], at[1]);
