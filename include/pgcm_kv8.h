@@ -45,7 +45,8 @@ typedef struct {
     uint32_t block_tokens;
     uint32_t kv_heads;
     uint32_t head_dim;           /* a multiple of 16 up to 256 */
-    int64_t k_block, k_token, k_head; /* strides in codes; those of tokens in [0, 2^25] for pgcm_kv8_attend */
+    int64_t k_block, k_token, k_head; /* strides in codes; those of tokens in [0, 2^25] for pgcm_kv8_attend (and, in halves,
+                                         for pgcm_kv_window) */
     int64_t v_block, v_token, v_head;
     int64_t k_scale_block, k_scale_head, v_scale_block, v_scale_head; /* in floats */
 } pgcm_kv8_cache;
@@ -55,7 +56,8 @@ typedef struct {
  * in `slots`, each slot one more than the one before; a call names each block in one such run.  A run that begins with its
  * block's first token starts the block anew; any other raises the block's scales, where its values need that, from what they
  * are (never lowers them), and then the codes of the tokens before the run are rounded to the new scale.  What the block holds
- * behind the run no longer counts.  A slot outside the pool is not written.
+ * behind the run no longer counts.  A slot outside the pool is not written.  Strides of tokens of k, v and of the cache are in
+ * [0, 2^23].
  */
 int pgcm_kv8_append(const pgcm_kv8_cache *cache, const pgcm_kv_append_args *args, void *hip_stream);
 

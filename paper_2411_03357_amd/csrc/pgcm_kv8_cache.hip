@@ -680,7 +680,7 @@ int pgcm_kv8_append(const pgcm_kv8_cache* cache, const pgcm_kv_append_args* args
     a.eps = args->eps, a.by_dim = 1.f / (float)dim, a.by_block = 1.0 / cache->block_tokens;
     const uint32_t windows = (args->tokens + kWindow - 1) / kWindow, in_window = args->tokens < kWindow ? args->tokens : kWindow;
     // about kGroups workgroups of either kind where there is that much to do
-    constexpr uint32_t kGroups = 1024;
+    constexpr uint32_t kGroups = 1024, kMostWays = 16384;
     auto ways = [&](uint64_t most) {   // of so many wavefronts' work
         const uint64_t groups = (most + kWaves - 1) / kWaves;
         return windows >= kGroups || groups <= 1 ? 1u : (uint32_t)(kGroups / windows < groups ? kGroups / windows : groups);
@@ -688,7 +688,8 @@ int pgcm_kv8_append(const pgcm_kv8_cache* cache, const pgcm_kv_append_args* args
     // (a prompt's runs begin in as many windows as there are blocks: the others' workgroups have nothing to do)
     const uint64_t of_kv = (uint64_t)in_window * a.kv_heads;
     a.spread = cache->block_tokens / kWindow < windows ? cache->block_tokens / kWindow : windows;
-    const uint64_t most_ways = (of_kv + kWaves - 1) / kWaves, some_ways = (uint64_t)ways(of_kv) * a.spread;
+    const uint64_t most_ways = (of_kv + kWaves - 1) / kWaves < kMostWays ? (of_kv + kWaves - 1) / kWaves : kMostWays;
+    const uint64_t some_ways = (uint64_t)ways(of_kv) * a.spread;
     a.kv_ways = (uint32_t)(some_ways < most_ways ? some_ways : most_ways);
     const uint32_t at_once = 64u >> a.row_power, of_q = (a.heads + at_once - 1) / at_once;
     uint32_t q_ways = of_q == 0 ? 0 : ways((uint64_t)kWindow * of_q);

@@ -85,12 +85,15 @@ def test_append_refuses():
     assert lib.pgcm_kv8_append(at, None, None) == ARG and lib.pgcm_kv8_append(None, C.byref(_append()), None) == ARG
     for bad in (dict(q=None), dict(q_out=None), dict(k=None), dict(v=None), dict(slots=None), dict(positions=None),
                 dict(heads=3), dict(heads=0), dict(heads=70000), dict(eps=-1.0), dict(eps=math.nan), dict(rope_dim=0),
-                dict(rope_dim=24), dict(rope_dim=144), dict(rope_positions=0), dict(tokens=1 << 31), dict(tokens=1 << 25)):
+                dict(rope_dim=24), dict(rope_dim=144), dict(rope_positions=0), dict(tokens=1 << 31), dict(tokens=(1 << 31) - 1),
+                dict(k_token=-256), dict(v_token=(1 << 23) + 8)):
         assert lib.pgcm_kv8_append(at, C.byref(_append(**bad)), None) == ARG, bad
     for bad in (dict(q=AT + 2), dict(k=AT + 2), dict(v=AT + 2), dict(q_out=AT + 2), dict(q_token=3), dict(q_head=3),
                 dict(k_token=3), dict(k_head=3), dict(v_token=3), dict(v_head=3), dict(q_out_token=3), dict(q_out_head=3),
                 dict(q_weight=AT + 2), dict(k_weight=AT + 2), dict(rope=AT + 4)):
         assert lib.pgcm_kv8_append(at, C.byref(_append(**bad)), None) == ALIGN, bad
+    for bad in (dict(k_token=(1 << 23) + 16), dict(v_token=-16)):
+        assert lib.pgcm_kv8_append(C.byref(_cache8(**bad)), C.byref(_append()), None) == ARG, bad
     assert lib.pgcm_kv8_append(at, C.byref(_append(tokens=0, k=None)), None) == 0
 
 
