@@ -11,6 +11,7 @@ namespace {
 constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kRowsHeld = 16;   // a unit's tokens in registers; of longer ones, so many at a time, twice
 constexpr int64_t kMostAppendStride = 1 << 23;
+constexpr uint32_t kFewUnits = 1024;
 constexpr uint32_t kTogether = 4;    // tokens whose loads are under way together
 constexpr uint32_t kStepsAtOnce = 3; // of queries
 
@@ -219,8 +220,10 @@ struct To {
     bool wanted;       // the lane has channels of a head
 };
 // A unit of halves, m tokens from `from` on: their codes, and the scale's bits
-template <class H, class C>
-__device__ __forceinline__ uint32_t convert_unit(const uint8_t* from, int64_t from_token, uint32_t m, const To& to, uint32_t row_power) {
+// join: of the largest values of those that share it
+template <class H, class C, class Join>
+__device__ __forceinline__ uint32_t convert_unit(const uint8_t* from, int64_t from_token, uint32_t m, const To& to, uint32_t row_power,
+                                                 Join join) {
     uint4 held[kRowsHeld];
     auto take = [&](uint32_t j0) {
 #pragma unroll
@@ -239,7 +242,7 @@ __device__ __forceinline__ uint32_t convert_unit(const uint8_t* from, int64_t fr
             largest = larger(largest, held[n]);
         }
     }
-    const uint32_t scale = scale_for<C>(over_row(as_float_bits<H>(largest), row_power), 0);
+    const uint32_t scale = scale_for<C>(join(over_row(as_float_bits<H>(largest), row_power)), 0);
     const float by = float_of(0x7F000000u - scale);   // (a power of two, or NaN)
     const bool lost = is_lost(scale);
     for (uint32_t j0 = 0; j0 < m; j0 += kRowsHeld) {
@@ -529,9 +532,8 @@ struct Unit {
     float* scale;
     uint32_t part;
 };
-__device__ __forceinline__ bool unit_of(const MoveArgs& a, Unit& u) {
+__device__ __forceinline__ bool unit_of(const MoveArgs& a, uint32_t task, Unit& u) {
     const uint32_t lane = threadIdx.x % 64, at_once = 64u >> a.row_power, of_kv = (a.kv_heads + at_once - 1) / at_once;
-    uint32_t task = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / 64);
     const uint32_t groups = 2 * of_kv * a.parts, i = task / groups;
     if (i >= a.n) return false;
     task -= i * groups;
@@ -557,18 +559,33 @@ __device__ __forceinline__ bool unit_of(const MoveArgs& a, Unit& u) {
     return true;
 }
 
-template <class H, class C>
+__device__ __forceinline__ uint32_t wave_of_grid() { return __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / 64); }
+
+// kShared: a unit is a workgroup's, a quarter of its tokens a wavefront's; else a wavefront's.
+template <class H, class C, bool kShared>
 __global__ __launch_bounds__(kThreads) void store8_kernel(MoveArgs a) {
+    __shared__ uint32_t largest[kShared ? kWaves : 1][64];
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     Unit u;
-    if (!unit_of(a, u)) return;
-    const uint32_t scale = convert_unit<H, C>(u.half, u.half_token, u.count, To{u.codes, u.code_token, u.wanted}, a.row_power);
-    if (u.part == 0 && u.there) *u.scale = float_of(scale);
+    if (!unit_of(a, kShared ? blockIdx.x : wave_of_grid(), u)) return;
+    const uint32_t from = kShared ? u.count * wave / kWaves : 0, to = kShared ? u.count * (wave + 1) / kWaves : u.count;
+    const uint32_t scale = convert_unit<H, C>(u.half + from * u.half_token, u.half_token, to - from,
+                                              To{u.codes + from * u.code_token, u.code_token, u.wanted}, a.row_power, [&](uint32_t most) {
+        if constexpr (kShared) {
+            largest[wave][lane] = most;
+            __syncthreads();
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; ++w) most = most > largest[w][lane] ? most : largest[w][lane];
+        }
+        return most;
+    });
+    if (u.part == 0 && u.there && (!kShared || wave == 0)) *u.scale = float_of(scale);
 }
 
 template <class H, class C>
 __global__ __launch_bounds__(kThreads) void load8_kernel(MoveArgs a) {
     Unit u;
-    if (!unit_of(a, u)) return;
+    if (!unit_of(a, wave_of_grid(), u)) return;
     const float scale = u.there ? *u.scale : 0.f;
     constexpr float kNearEnd = sizeof(typename H::one) == 2 && H::kInfinity == 0x7C00 ? 64.f : 0x1p118f;   // 448 times that is in range
     const bool near_end = scale > kNearEnd;
@@ -632,11 +649,9 @@ int move_args(const pgcm_kv8_cache* c8, const pgcm_kv_cache* c, uint32_t n, cons
     a->pool8 = c8->blocks, a->pool = c->blocks, a->row_power = row_power_of(c->head_dim), a->parts = 1;
     return PGCM_OK;
 }
-// workgroups, or 0: more than a launch holds
-uint32_t move_groups(const MoveArgs& a) {
-    const uint32_t at_once = 64u >> a.row_power, of_kv = (a.kv_heads + at_once - 1) / at_once;
-    const uint64_t waves = (uint64_t)a.n * 2 * of_kv * a.parts, groups = (waves + kWaves - 1) / kWaves;
-    return launchable(groups, kThreads) ? (uint32_t)groups : 0;
+uint64_t move_units(const MoveArgs& a) {
+    const uint32_t at_once = 64u >> a.row_power;
+    return (uint64_t)a.n * 2 * ((a.kv_heads + at_once - 1) / at_once) * a.parts;
 }
 
 }  // namespace
@@ -720,17 +735,22 @@ int pgcm_kv8_store(const pgcm_kv8_cache* to, const pgcm_kv_cache* from, uint32_t
     MoveArgs a{};
     if (const int rc = move_args(to, from, n, blocks, counts, from_blocks, &a)) return rc;
     if (n == 0) return PGCM_OK;
-    const uint32_t groups = move_groups(a);
-    if (groups == 0) return PGCM_ERR_ARG;
+    // A wavefront a unit, or four, where one would take its tokens twice, or units are few.  Microseconds with one and with four,
+    // read-back included: 16 blocks of 40 heads (320 units) 12.6 and 11.9, 64 (1280) 18.1 and 18.2, 256 41.5 and 47.3, 2048 398 and
+    // 419; 1024 blocks of 32 tokens 444 and 388, 512 of 64 499 and 386.
+    const bool shared = a.block_tokens > kRowsHeld || move_units(a) <= kFewUnits;
+    const uint64_t units = move_units(a), groups = shared ? units : (units + kWaves - 1) / kWaves;
+    if (!launchable(groups, kThreads)) return PGCM_ERR_ARG;
+    const uint32_t n_groups = (uint32_t)groups;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const bool f16 = from->half == PGCM_KV_F16;
-    if (to->code == PGCM_KV8_INT8) {
-        if (f16) store8_kernel<F16, Int8><<<groups, kThreads, 0, stream>>>(a);
-        else store8_kernel<Bf16, Int8><<<groups, kThreads, 0, stream>>>(a);
-    } else {
-        if (f16) store8_kernel<F16, E4m3><<<groups, kThreads, 0, stream>>>(a);
-        else store8_kernel<Bf16, E4m3><<<groups, kThreads, 0, stream>>>(a);
-    }
+    auto launch = [&](auto half, auto code) {
+        typedef decltype(half) H;
+        typedef decltype(code) C;
+        if (shared) store8_kernel<H, C, true><<<n_groups, kThreads, 0, stream>>>(a);
+        else store8_kernel<H, C, false><<<n_groups, kThreads, 0, stream>>>(a);
+    };
+    if (from->half == PGCM_KV_F16) to->code == PGCM_KV8_INT8 ? launch(F16(), Int8()) : launch(F16(), E4m3());
+    else to->code == PGCM_KV8_INT8 ? launch(Bf16(), Int8()) : launch(Bf16(), E4m3());
     return hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 
@@ -740,8 +760,9 @@ int pgcm_kv8_load(const pgcm_kv8_cache* from, const pgcm_kv_cache* to, uint32_t 
     if (const int rc = move_args(from, to, n, blocks, counts, to_blocks, &a)) return rc;
     if (n == 0) return PGCM_OK;
     a.parts = (from->block_tokens + 15) / 16;   // sixteen tokens a wavefront
-    const uint32_t groups = move_groups(a);
-    if (groups == 0) return PGCM_ERR_ARG;
+    const uint64_t waves = move_units(a);
+    if (!launchable((waves + kWaves - 1) / kWaves, kThreads)) return PGCM_ERR_ARG;
+    const uint32_t groups = (uint32_t)((waves + kWaves - 1) / kWaves);
     const hipStream_t stream = (hipStream_t)hip_stream;
     const bool f16 = to->half == PGCM_KV_F16;
     if (from->code == PGCM_KV8_INT8) {
