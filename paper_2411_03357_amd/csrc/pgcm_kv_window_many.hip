@@ -14,6 +14,7 @@ constexpr uint32_t kWaves = 4, kThreads = kWaves * 64, kRows = 32 * kWaves;
 constexpr uint32_t kTile = 64, kTilePieces = kTile / kPiece;
 constexpr uint32_t kManyGroups = 512;    // workgroups that the chip holds at once
 constexpr uint32_t kLeastTiles = 8;      // of a part
+constexpr uint32_t kMostParts = 1024;    // of all items, where they are cut
 static_assert(kTilePieces == kWaves, "a wavefront asks for a piece of a tile");
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -417,8 +418,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
             total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.693147180559945f;
 }
 
-// The parts of an item as one: blockIdx.y takes an eighth of its rows, a thread four channels of one at a time.
-constexpr uint32_t kJoins = 8;
+// The parts of an item as one: blockIdx.y takes a sixteenth of its rows, a thread four channels of one at a time.
+constexpr uint32_t kJoins = 16, kTogether = 8;   // parts whose loads are under way together
 template <class H, uint32_t kDim>
 __global__ __launch_bounds__(kThreads) void join_kernel(WindowArgs a, uint32_t ranks, uint32_t most_parts) {
     const uint32_t item = blockIdx.x;
@@ -432,16 +433,32 @@ __global__ __launch_bounds__(kThreads) void join_kernel(WindowArgs a, uint32_t r
     for (uint32_t n = threadIdx.x; n < kRows / kJoins * kQuads; n += kThreads) {
         const uint32_t r = blockIdx.y * (kRows / kJoins) + n / kQuads, d = n % kQuads * 4;
         if (r >= x.rows) return;
-        float most = -INFINITY;
-        for (uint32_t p = 0; p < parts; ++p) most = fmaxf(most, first[p * kPart + kRows * kDim + 2 * r]);
+        // (sums to the largest top so far, as in the walk)
+        float most = -INFINITY, total = 0.f;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        float total = 0.f;
-        for (uint32_t p = 0; p < parts; ++p) {
-            const float2 of = *(const float2*)(first + p * kPart + kRows * kDim + 2 * r);
-            const float4 y = *(const float4*)(first + p * kPart + r * kDim + d);
-            const float by = exp2_from(of.x, most);
-            total += of.y * by;
-            sum.x += y.x * by, sum.y += y.y * by, sum.z += y.z * by, sum.w += y.w * by;
+        for (uint32_t p0 = 0; p0 < parts; p0 += kTogether) {
+            float2 of[kTogether];
+            float4 y[kTogether];
+#pragma unroll
+            for (uint32_t e = 0; e < kTogether; ++e) {
+                const float* const part = first + (p0 + e < parts ? p0 + e : p0) * kPart;
+                of[e] = *(const float2*)(part + kRows * kDim + 2 * r);
+                y[e] = *(const float4*)(part + r * kDim + d);
+            }
+            float now = most;
+#pragma unroll
+            for (uint32_t e = 0; e < kTogether; ++e) now = fmaxf(now, of[e].x);
+            const float keep = exp2_from(most, now);
+            most = now;
+            total *= keep;
+            sum.x *= keep, sum.y *= keep, sum.z *= keep, sum.w *= keep;
+#pragma unroll
+            for (uint32_t e = 0; e < kTogether; ++e) {
+                if (p0 + e >= parts) break;
+                const float by = exp2_from(of[e].x, most);
+                total += of[e].y * by;
+                sum.x += y[e].x * by, sum.y += y[e].y * by, sum.z += y[e].z * by, sum.w += y[e].w * by;
+            }
         }
         const uint32_t row = x.first + r, token = row / a.group, head = x.kv_head * a.group + row - token * a.group;
         const float by = total == 0.f ? 0.f : 1.f / total;   // (a NaN stays one)
@@ -481,20 +498,27 @@ size_t part_bytes(uint32_t head_dim) { return 4 * (size_t)kRows * ((head_dim <= 
 
 }  // namespace
 
-Room window_many_room(uint32_t head_dim) { return Room{0, part_bytes(head_dim) * kManyGroups}; }
+Room window_many_room(uint32_t head_dim) { return Room{0, part_bytes(head_dim) * kMostParts}; }
 
 int window_many(pgcm_kv* kv, WindowArgs& a, uint32_t half, hipStream_t stream) {
-    // runs of kRows rows, at most: what the requests' last ones leave is one more for each
+    // runs of kRows rows, at most: each request's last one may be short of that
     const uint64_t some = a.requests < a.tokens ? a.requests : a.tokens;
-    const uint64_t ranks = (uint64_t)a.tokens * a.group / kRows + some, items = ranks * a.kv_heads;
+    const uint64_t ranks = ((uint64_t)a.tokens * a.group + some * (kRows - 1)) / kRows, items = ranks * a.kv_heads;
     if (!launchable(items, kThreads) || items > 0x7FFFFFFFull) return PGCM_ERR_ARG;
     uint64_t walked = (uint64_t)a.row_blocks * a.block_tokens;
     const uint64_t seen = (uint64_t)a.window + a.sinks + kRows / a.group + 4 * kPiece;
     if (a.window != 0 && walked > seen) walked = seen;
     const uint64_t tiles = (walked + kTile - 1) / kTile, useful = (tiles + kLeastTiles - 1) / kLeastTiles;
-    uint64_t parts = kManyGroups / items;
-    if (parts > useful) parts = useful;
-    if (parts < 1) parts = 1;
+    // As many parts as take the least time, in tiles: rounds of as many workgroups as the chip holds, two tiles' time at a part's
+    // start and end each, and the join's.
+    const uint64_t at_once = a.head_dim > 128 ? kManyGroups / 2 : kManyGroups;
+    uint64_t parts = 1;
+    double least = 0;
+    for (uint64_t p = 1; p == 1 || (p <= useful && items * p <= kMostParts); ++p) {
+        const double time = (double)((items * p + at_once - 1) / at_once) * ((double)tiles / (double)p + 2) +
+                            (p == 1 ? 0 : 1.5 + 0.007 * (double)(items * p));
+        if (p == 1 || time < least) least = time, parts = p;
+    }
     if (parts > 1) {
         const Room room = window_many_room(a.head_dim);
         if (const int rc = kv_ensure(kv, room.counters, room.scratch, stream)) return rc;
