@@ -19,6 +19,7 @@
  * So reading back is exact in binary32, and in halves but for the ends of their range; and a scale that has to grow while a
  * block fills doubles, so that the codes that are there are rounded again at most once for each doubling, which adds up to
  * less than one step of the last scale in int8, and in e4m3 changes only codes that fall below its least normal number.
+ * A cache may hold other scales above zero; append keeps the larger of what is there and what its values need, and 0 for none.
  * If a value is infinite or NaN the head's scale of that block is NaN, and the codes that come with it are zero: nothing that is
  * read from there is taken for a number.
  *

@@ -240,6 +240,75 @@ def test_append_with_norms_and_rotation(dim, rope_dim, adjacent, weighted, half,
                 assert bool(((got - rows[:, h]).abs() <= step + slack * a).all())
 
 
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("block, kv, dim, tokens, first", [
+    (16, 8, 128, 8191, 0), (16, 300, 16, 17000, 5), (512, 150, 16, 20000, 100), (64, 40, 128, 3000, 63), (32, 2, 256, 5000, 31),
+    (4096, 3, 64, 9000, 4000), (48, 5, 80, 1000, 47), (16, 1, 256, 300, 1), (128, 700, 32, 1500, 1), (80, 4, 112, 257, 0)])
+def test_an_append_makes_the_blocks_that_a_store_makes(block, kv, dim, tokens, first, code):
+    """of tokens from inside a block on, over blocks in any order, some of them elsewhere: whole blocks as store has them"""
+    half = torch.bfloat16
+    blocks = -(-(first + tokens) // block)
+    g = torch.Generator(device="cuda").manual_seed(block + kv)
+    x = torch.randn(blocks * block, 2, kv, dim, generator=g, device="cuda")
+    x = (x * (torch.randn(blocks * block, 1, kv, 1, generator=g, device="cuda") * 2).exp()).to(half)
+    order = torch.randperm(blocks, generator=g, device="cuda")
+    pool = torch.zeros(blocks, 2, block, kv, dim, dtype=half, device="cuda")
+    pool[order] = x.view(blocks, block, 2, kv, dim).transpose(1, 2)
+    sides = []
+    for _ in range(2):
+        codes = torch.zeros(blocks, 2, block, kv, dim, dtype=torch.uint8, device="cuda").view(code)
+        scales = torch.zeros(blocks, 2, kv, device="cuda")
+        sides.append((codes, scales, pgcm.KV8Cache(codes[:, 0], codes[:, 1], scales[:, 0], scales[:, 1], half)))
+    at = torch.arange(first + tokens, device="cuda")
+    slots = order[at // block] * block + at % block
+    if first:
+        pgcm.kv8_append(sides[0][2], None, x[:first, 0], x[:first, 1], None, slots[:first].contiguous(), None)
+    absent = order[blocks // 2]     # its tokens go nowhere
+    slots = torch.where(slots // block == absent, -1, slots)[first:].contiguous()
+    pgcm.kv8_append(sides[0][2], None, x[first:first + tokens, 0], x[first:first + tokens, 1], None, slots, None)
+    counts = torch.full((blocks,), block, dtype=torch.int32, device="cuda")
+    counts[order[-1]] = (first + tokens - 1) % block + 1
+    every = torch.arange(blocks, dtype=torch.int32, device="cuda")
+    pgcm.kv8_store(sides[1][2], pgcm.KVCache(pool[:, 0], pool[:, 1]), every, counts)
+    # all but the block that tokens were left out of, and the one that was filled in two steps, which may be off by a step
+    same = torch.ones(blocks, dtype=torch.bool, device="cuda")
+    same[absent] = False
+    if first:
+        same[order[(first - 1) // block]] = False
+    assert torch.equal(sides[0][1][same], sides[1][1][same])
+    assert torch.equal(sides[0][0].view(torch.uint8)[same], sides[1][0].view(torch.uint8)[same])
+    if first and int(order[(first - 1) // block]) != int(absent):
+        b = order[(first - 1) // block]
+        assert torch.equal(sides[0][1][b], sides[1][1][b])      # the largest of both steps
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+def test_scales_of_others(code):
+    """not a power of two, and zero, where an append goes on"""
+    half, block, kv, dim = torch.bfloat16, 16, 2, 64
+    cpu = list(ref.pool8(9, 2, block, kv, dim, code))
+    for s in cpu[2:]:
+        s[0] = torch.tensor([0.37, 1e-9])
+        s[1] = 0.0
+    gpu = ref.on_gpu(cpu, block, kv, dim, code, True)
+    _, k, v = _packed(50, 6, 2, kv, dim, half)
+    k, v = k.sign() * k.abs().clamp(2.0 ** -9, 30), v.sign() * v.abs().clamp(2.0 ** -9, 30)
+    slots = torch.tensor([5, 6, 7, 16 + 9, 16 + 10, 16 + 11])
+    pgcm.kv8_append(_cache8(gpu, half), None, k.cuda(), v.cuda(), None, slots.cuda(), None)
+    for i, x in enumerate((k.double(), v.double())):
+        for b, inside, rows in ((0, 5, x[:3]), (1, 9, x[3:])):
+            for h in range(kv):
+                scale, old = float(gpu[2 + i][b, h]), float(cpu[2 + i][b, h])
+                assert scale == max(old, 2.0 ** ref.power(float(rows[:, h].abs().max()), code))
+                got = gpu[i][b, inside:inside + 3, h].cpu().double() * scale
+                step = scale / 2 if code == torch.int8 else torch.maximum(rows[:, h].abs() / 16, torch.tensor(scale * 2.0 ** -10))
+                assert bool(((got - rows[:, h]).abs() <= step * (1 + 2.0 ** -20)).all())
+                kept = cpu[i][b, :inside, h].double() if code == torch.int8 else cpu[i][b, :inside, h].float().double()
+                now = gpu[i][b, :inside, h].cpu().double() * scale
+                step = scale / 2 if code == torch.int8 else torch.maximum((kept * old).abs() / 16, torch.tensor(scale * 2.0 ** -10))
+                assert bool(((now - kept * old).abs() <= (step * (1 + 2.0 ** -20) if scale != old else 0)).all())
+
+
 def test_a_captured_append_and_load():
     """replayed several times with other values, between eager work, against the eager results"""
     half, code, block, kv, dim, n = torch.bfloat16, torch.int8, 16, 4, 128, 40

@@ -108,6 +108,56 @@ def test_rows_in_parts(half, lens, news, kv, group, dim, window, sinks):
 
 
 @kinds
+def test_lengths_out_of_range(kind):
+    """beyond the row's blocks: cut to them; below zero: none"""
+    b = _blocks(kind, 45, [47, 31, 16], 2, 64)      # rows of three blocks and one more
+    for news in ([1, 1, 1], [20, 3, 2]):
+        q = _q(46, sum(news), 4, 64, kind[0]).cuda()
+        starts = torch.tensor([0, *torch.tensor(news).cumsum(0).tolist()], dtype=torch.int32).cuda()
+        tables = torch.from_numpy(b.tables).cuda()
+        tables[:, 3:] = -1
+        outs = []
+        for lens in ([1 << 30, -7, 16], [64, 0, 16]):
+            out = torch.zeros_like(q)
+            b.call(pgcm)(b.cache(pgcm), q, tables, torch.tensor(lens, dtype=torch.int32).cuda(), out, window=20, sinks=3,
+                         starts=starts, most=max(news))
+            outs.append(out)
+        assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
+        assert bool((outs[0][news[0]:news[0] + news[1]] == 0).all())
+
+
+@kinds
+def test_on_another_stream(kind):
+    b = _blocks(kind, 47, [3000, 200], 2, 128)
+    stream = torch.cuda.Stream()
+    for news in ([1, 1], [30, 4]):
+        q = _q(48, sum(news), 8, 128, kind[0])
+        want = ref.run(pgcm, b, q, news, 1000, 4)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            got = ref.run(pgcm, b, q, news, 1000, 4)
+        stream.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("half", HALVES)
+def test_random_shapes_of_many_rows(half):
+    """requests, rows, windows, sinks and holes at random, against the definition"""
+    import random
+    rng = random.Random(49)
+    for case in range(14):
+        kv, group = rng.choice([(1, 1), (2, 4), (1, 7), (3, 2), (1, 16)])
+        dim, block = rng.choice([64, 80, 128, 128, 256]), rng.choice([16, 32, 64])
+        lens = [rng.choice([0, 1, rng.randint(1, 80), rng.randint(1, 700)]) for _ in range(rng.randint(1, 5))]
+        news = [rng.choice([0, 1, min(t + 2, rng.randint(1, 60)), min(t, 130)]) for t in lens]
+        if max(news) < 2:
+            news[0] = 2
+        b = ref.Blocks(100 + case, lens, kv, dim, half, block=block, holes=rng.choice([0.0, 0.0, 0.3]))
+        q = _q(200 + case, sum(news), kv * group, dim, half, 1.5)
+        ref.check(pgcm, b, q, news, rng.choice([0, 1, rng.randint(2, 40), rng.randint(40, 500)]), rng.choice([0, 4, 33]), spare=2)
+
+
+@kinds
 def test_one_row_of_some_requests(kind):
     lens, news = [300, 5, 0, 129, 64], [1, 0, 1, 1, 0]
     b = _blocks(kind, 15, lens, 2, 128)
