@@ -275,50 +275,50 @@ __device__ __forceinline__ Split split_by(uint64_t x, uint32_t by, double one_by
     return Split{q, (uint32_t)r};
 }
 
-// Keys and values of a run, m tokens from `first` on, to `block` from place `inside` on: heads [head_from, head_to), a wavefront
-// of the workgroup one at a time.  A lane's rows are tokens side by side, kHeld times as many held in registers (a "chunk"): so a
-// head's largest value is found in the wavefront.  The factors that norm and rotation multiply a chunk's tokens with are made once
-// for all heads, in LDS.  Runs of several chunks are taken twice, for their largest values and for their codes.
-constexpr uint32_t kHeadsAtOnce = 32;    // of a wavefront, whose largest values are kept over a run
+// Keys and values of a run, m tokens from `first` on, to `block` from place `inside` on: the workgroup's share of the run's sides
+// (keys of head 0, 1, ..., then values of head 0, 1, ...), [from, to), a wavefront one at a time.  A lane's rows are tokens side by
+// side, kHeld times as many held in registers (a "chunk"): so a side's largest value is found in the wavefront.  The factors that norm and
+// rotation multiply a chunk's tokens with are made once for all heads, in LDS.  Runs of several chunks are taken twice, for their
+// largest values and for their codes.
+constexpr uint32_t kSidesAtOnce = 64;    // of a wavefront, whose largest values are kept over a run
 template <uint32_t kHeld>
 struct AppendShared {
     float4 factors[kHeld][4][64];        // of a lane's row: own, then other
-    uint32_t largest[kWaves][kHeadsAtOnce][2];
+    uint32_t largest[kWaves][kSidesAtOnce];
 };
 template <class H, class C, uint32_t kHeld>
 __device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& turn, AppendShared<kHeld>& shared, uint32_t first,
-                                           uint32_t m, uint64_t block, uint32_t inside, uint32_t head_from, uint32_t head_to,
+                                           uint32_t m, uint64_t block, uint32_t inside, uint32_t from, uint32_t to,
                                            const typename Turn<H>::Raw& raw, int32_t near_position, uint32_t near_from) {
     const uint32_t lane = turn.lane, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t rows = 64u >> a.row_power, in_step = lane >> a.row_power, chunk = kHeld * rows;
     const bool worked = a.k_weight != nullptr || a.rope != nullptr, normed = a.k_weight != nullptr;
     const bool once = m <= chunk;
-    // where the lane's channels lie from a step's first token on
-    const uint32_t k_off = in_step * (uint32_t)a.k_token + 2 * turn.d, v_off = in_step * (uint32_t)a.v_token + 2 * turn.d;
-    const uint32_t code_off[2] = {in_step * (uint32_t)a.side[0].token + turn.d, in_step * (uint32_t)a.side[1].token + turn.d};
-    for (uint32_t group = head_from; group < head_to; group += kHeadsAtOnce * kWaves) {
+    for (uint32_t group = from; group < to; group += kSidesAtOnce * kWaves) {
         // twice: the largest values alone, then the codes
         for (uint32_t x = once ? m : 0; x < 2 * m; x = x < m && x + chunk > m ? m : x + chunk) {
             const bool writes = x >= m;
             const uint32_t j0 = once ? 0 : writes ? x - m : x, left = m - j0;
-            uint4 k[kHeld], v[kHeld];
-            float old_at[2] = {0.f, 0.f};   // the scales that were there
-            auto take = [&](uint32_t h) {
+            uint4 rows_of[kHeld];
+            float old_at = 0.f;   // the scale that was there
+            auto take = [&](uint32_t n_side) {
+                const bool is_v = n_side >= a.kv_heads;
+                const uint32_t h = is_v ? n_side - a.kv_heads : n_side;
+                const Side8& side = a.side[is_v];
+                // (where the lane's channels lie from a step's first token on: in 32 bits)
+                const int64_t stride = is_v ? a.v_token : a.k_token;
+                const uint32_t off = in_step * (uint32_t)stride + 2 * turn.d;
+                const uint8_t* at = (is_v ? a.v + h * a.v_head : a.k + h * a.k_head) + (first + j0) * stride;
 #pragma unroll
                 for (uint32_t n = 0; n < kHeld; ++n) {
-                    k[n] = v[n] = make_uint4(0, 0, 0, 0);
-                    if (n * rows < left && turn.mine && n * rows + in_step < left) {
-                        const uint32_t t = first + j0 + n * rows;
-                        k[n] = *(const uint4*)(a.k + h * a.k_head + t * a.k_token + k_off);
-                        v[n] = *(const uint4*)(a.v + h * a.v_head + t * a.v_token + v_off);
-                    }
+                    rows_of[n] = make_uint4(0, 0, 0, 0);
+                    if (n * rows < left && turn.mine && n * rows + in_step < left) rows_of[n] = *(const uint4*)(at + off);
+                    at += rows * stride;
                 }
-#pragma unroll
-                for (uint32_t e = 0; e < 2; ++e)
-                    if (writes && inside != 0) old_at[e] = a.side[e].scales[block * a.side[e].scale_block + h * a.side[e].scale_head];
+                if (writes && inside != 0) old_at = side.scales[block * side.scale_block + h * side.scale_head];
             };
-            if (group + wave < head_to) take(group + wave);     // under way while the factors are made
-            if (worked) {
+            if (group + wave < to) take(group + wave);     // under way while the factors are made
+            if (worked && group < a.kv_heads) {
                 __syncthreads();   // (all have left those of before)
                 for (uint32_t n = wave; n < kHeld && n * rows < left; n += kWaves) {
                     const uint32_t j = n * rows + in_step, t = first + j0 + j;
@@ -333,90 +333,75 @@ __device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& 
                 }
                 __syncthreads();
             }
-            for (uint32_t i = 0; i < kHeadsAtOnce; ++i) {
-                const uint32_t h = group + i * kWaves + wave;
-                if (h >= head_to) break;
-                if (i != 0) take(h);
-                uint32_t old[2];
-#pragma unroll
-                for (uint32_t e = 0; e < 2; ++e) old[e] = __builtin_amdgcn_readfirstlane(bits_of(old_at[e]));
+            for (uint32_t i = 0; i < kSidesAtOnce; ++i) {
+                const uint32_t n_side = group + i * kWaves + wave;
+                if (n_side >= to) break;
+                if (i != 0) take(n_side);
+                const bool is_v = n_side >= a.kv_heads, turned = worked && !is_v;
                 float z[kHeld][8], by[kHeld];
-                uint32_t most[2] = {0, 0};
-                u16x2 most_v = (u16x2)(unsigned short)0;
+                uint32_t most = 0;
 #pragma unroll
                 for (uint32_t n = 0; n < kHeld; ++n) {
                     by[n] = 1.f;
                     if (n * rows >= left) continue;   // (the same for all lanes)
-                    if (worked) {
+                    if (turned) {
                         const float4 f0 = shared.factors[n][0][lane], f1 = shared.factors[n][1][lane];
                         const float4 f2 = shared.factors[n][2][lane], f3 = shared.factors[n][3][lane];
                         const typename Turn<H>::Weights f{{f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w},
                                                           {f2.x, f2.y, f2.z, f2.w, f3.x, f3.y, f3.z, f3.w}};
-                        by[n] = turn.apply(a, k[n], f, normed, z[n]);
+                        by[n] = turn.apply(a, rows_of[n], f, normed, z[n]);
                     } else {
-                        floats_of<H>(k[n], z[n]);
+                        floats_of<H>(rows_of[n], z[n]);
                     }
                     const uint32_t of_row = bits_of(float_of(larger(0, z[n])) * by[n]) & 0x7FFFFFFFu;
-                    if (turn.mine && n * rows + in_step < left && of_row > most[0]) most[0] = of_row;
-                    most_v = larger(most_v, v[n]);
+                    if (turn.mine && n * rows + in_step < left && of_row > most) most = of_row;
                 }
-                most[1] = as_float_bits<H>(most_v);
-#pragma unroll
-                for (uint32_t e = 0; e < 2; ++e) {
-                    most[e] = over_wave(most[e], [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-                    if (once) continue;
-                    uint32_t* const kept = &shared.largest[wave][i][e];   // (the wavefront's own)
-                    if (!writes) *kept = j0 != 0 && *kept > most[e] ? *kept : most[e];
-                    else most[e] = *kept;
+                most = over_wave(most, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+                if (!once) {
+                    uint32_t* const kept = &shared.largest[wave][i];   // (the wavefront's own)
+                    if (!writes) *kept = j0 != 0 && *kept > most ? *kept : most;
+                    else most = *kept;
                 }
                 if (!writes) continue;
+                const uint32_t h = is_v ? n_side - a.kv_heads : n_side;
+                const Side8& side = a.side[is_v];
+                const uint32_t old = __builtin_amdgcn_readfirstlane(bits_of(old_at));
+                const uint32_t scale = scale_for<C>(__builtin_amdgcn_readfirstlane(most), old);
+                const float inv = inverse(scale);
+                const bool lost = is_lost(scale);
+                const uint32_t off = in_step * (uint32_t)side.token + turn.d;
+                uint8_t* const at = side.at + block * side.block + h * side.head;
 #pragma unroll
-                for (uint32_t e = 0; e < 2; ++e) {
-                    const Side8& side = a.side[e];
-                    const uint32_t scale = scale_for<C>(__builtin_amdgcn_readfirstlane(most[e]), old[e]);
-                    const float inv = inverse(scale);
-                    const bool lost = is_lost(scale);
-                    uint8_t* const at = side.at + block * side.block + h * side.head;
-#pragma unroll
-                    for (uint32_t n = 0; n < kHeld; ++n) {
-                        if (n * rows >= left) continue;
-                        float y[8];
-                        if (e == 0) {
-#pragma unroll
-                            for (uint32_t c = 0; c < 8; ++c) y[c] = z[n][c];
-                        } else {
-                            floats_of<H>(v[n], y);
-                        }
-                        uint2 codes = eight_codes<C>(y, e == 0 ? by[n] * inv : inv);
-                        if (lost) codes = make_uint2(0, 0);
-                        if (turn.mine && n * rows + in_step < left)
-                            *(uint2*)(at + (inside + j0 + n * rows) * side.token + code_off[e]) = codes;
-                    }
-                    // with the first chunk: the codes that are there to the new scale
-                    if (j0 == 0 && inside != 0 && !lost && scale != old[e]) {
-                        const float ratio = float_of(old[e]) * inv;
-                        for (uint32_t t = 0; t < inside; t += kTogether * rows) {
-                            uint2 words[kTogether];
-#pragma unroll
-                            for (uint32_t n = 0; n < kTogether; ++n) {
-                                words[n] = make_uint2(0, 0);
-                                if (turn.mine && t + n * rows + in_step < inside)
-                                    words[n] = *(const uint2*)(at + (t + n * rows) * side.token + code_off[e]);
-                            }
-#pragma unroll
-                            for (uint32_t n = 0; n < kTogether; ++n) {
-                                float low[4], high[4];
-                                C::values(words[n].x, low), C::values(words[n].y, high);
-                                const uint2 codes = make_uint2(C::codes(low[0], low[1], low[2], low[3], ratio),
-                                                               C::codes(high[0], high[1], high[2], high[3], ratio));
-                                if (turn.mine && t + n * rows + in_step < inside)
-                                    *(uint2*)(at + (t + n * rows) * side.token + code_off[e]) = codes;
-                            }
-                        }
-                    }
-                    // ... and the scale with the last, as each reads what it was
-                    if (left <= chunk && lane == 0) side.scales[block * side.scale_block + h * side.scale_head] = float_of(scale);
+                for (uint32_t n = 0; n < kHeld; ++n) {
+                    if (n * rows >= left) continue;
+                    uint2 codes = eight_codes<C>(z[n], by[n] * inv);
+                    if (lost) codes = make_uint2(0, 0);
+                    if (turn.mine && n * rows + in_step < left) *(uint2*)(at + (inside + j0 + n * rows) * side.token + off) = codes;
                 }
+                // with the first chunk: the codes that are there to the new scale
+                if (j0 == 0 && inside != 0 && !lost && scale != old) {
+                    const float ratio = float_of(old) * inv;
+                    for (uint32_t t = 0; t < inside; t += kTogether * rows) {
+                        uint2 words[kTogether];
+#pragma unroll
+                        for (uint32_t n = 0; n < kTogether; ++n) {
+                            words[n] = make_uint2(0, 0);
+                            if (turn.mine && t + n * rows + in_step < inside)
+                                words[n] = *(const uint2*)(at + (t + n * rows) * side.token + off);
+                        }
+#pragma unroll
+                        for (uint32_t n = 0; n < kTogether; ++n) {
+                            float low[4], high[4];
+                            C::values(words[n].x, low), C::values(words[n].y, high);
+                            const uint2 codes = make_uint2(C::codes(low[0], low[1], low[2], low[3], ratio),
+                                                           C::codes(high[0], high[1], high[2], high[3], ratio));
+                            if (turn.mine && t + n * rows + in_step < inside)
+                                *(uint2*)(at + (t + n * rows) * side.token + off) = codes;
+                        }
+                    }
+                }
+                // ... and the scale with the last, as each reads what it was
+                if (left <= chunk && lane == 0) side.scales[block * side.scale_block + h * side.scale_head] = float_of(scale);
             }
         }
     }
@@ -426,7 +411,7 @@ __device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& 
 // lanes for each head instead of each token, as the append of halves has them, sixteen tokens' factors were made for every four
 // heads: 142 us instead of 103 for the prompt).
 //
-// The runs that begin in a window of tokens are taken by its kv_ways workgroups, whole, their heads in equal shares; the window's
+// The runs that begin in a window of tokens are taken by its kv_ways workgroups, whole, their sides in equal shares; the window's
 // queries by the workgroups of blockIdx.y >= kv_ways, a token and some of its heads a wavefront.
 constexpr uint32_t kWindow = 16;
 template <class H, class C, uint32_t kHeld>
@@ -496,12 +481,12 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
     // bit i: token window + i begins a run that is stored
     const uint64_t in_pool = __ballot((uint64_t)near < a.pool_tokens && window + lane - 1 < a.tokens);
     uint64_t in_window = (marks & in_pool) >> 1 & ((1ull << kWindow) - 1);
-    const uint32_t tasks = (uint32_t)__builtin_popcountll(in_window) * a.kv_heads;   // heads of all runs
+    const uint32_t tasks = (uint32_t)__builtin_popcountll(in_window) * 2 * a.kv_heads;   // sides of all runs
     const uint32_t share = (tasks + a.kv_ways - 1) / a.kv_ways, from = share * blockIdx.y;
     const uint32_t to = from + share < tasks ? from + share : tasks;
     if (from >= tasks) return;
-    for (uint32_t task = 0; in_window != 0 && task < to; in_window &= in_window - 1, task += a.kv_heads) {
-        if (task + a.kv_heads <= from) continue;
+    for (uint32_t task = 0; in_window != 0 && task < to; in_window &= in_window - 1, task += 2 * a.kv_heads) {
+        if (task + 2 * a.kv_heads <= from) continue;
         const uint32_t at = __builtin_ctzll(in_window), first = window + at;
         uint32_t m = 0;
         if (const uint64_t later = marks >> 1 & ~((2ull << at) - 1); later != 0) {
@@ -517,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
         const uint32_t low = __builtin_amdgcn_readlane((uint32_t)near_place.whole, at + 1);
         const uint32_t high = __builtin_amdgcn_readlane((uint32_t)(near_place.whole >> 32), at + 1);
         append_run<H, C, kHeld>(a, turn, shared, first, m, (uint64_t)high << 32 | low, __builtin_amdgcn_readlane(near_place.rest, at + 1),
-                                from > task ? from - task : 0, to - task < a.kv_heads ? to - task : a.kv_heads, raw, near_position, near_from);
+                                from > task ? from - task : 0, to - task < 2 * a.kv_heads ? to - task : 2 * a.kv_heads, raw, near_position, near_from);
     }
 }
 
@@ -707,7 +692,7 @@ int pgcm_kv8_append(const pgcm_kv8_cache* cache, const pgcm_kv_append_args* args
         return windows >= kGroups || groups <= 1 ? 1u : (uint32_t)(kGroups / windows < groups ? kGroups / windows : groups);
     };
     // (a prompt's runs begin in as many windows as there are blocks: the others' workgroups have nothing to do)
-    const uint64_t of_kv = (uint64_t)in_window * a.kv_heads;
+    const uint64_t of_kv = (uint64_t)in_window * 2 * a.kv_heads;
     a.spread = cache->block_tokens / kWindow < windows ? cache->block_tokens / kWindow : windows;
     const uint64_t most_ways = (of_kv + kWaves - 1) / kWaves < kMostWays ? (of_kv + kWaves - 1) / kWaves : kMostWays;
     const uint64_t some_ways = (uint64_t)ways(of_kv) * a.spread;
