@@ -5,8 +5,6 @@
 
 namespace pgcm_kv_impl {
 
-constexpr uint32_t kTargetGroups = 1024;   // workgroups that a call's work is cut for
-
 struct WindowArgs {
     const uint8_t *k, *v, *q;
     uint8_t* out;

@@ -3,26 +3,35 @@
 // Per token, kv head and group of up to sixteen of its query heads (an "item"):
 //   s[t][h] = scale k_t . q_h,   m = max s,   out = sum 2^(s - m) v_t / sum 2^(s - m)     (s in units of log 2)
 // with running m and sums, one pass over K and V.  What bounds it is memory: two requests of 131 059 tokens in int8, 8 kv heads of
-// 128 and 8 query heads to each (537 MB): 126 us, 4.3 TB/s; 48 requests of up to 16384 tokens in e4m3 with a window of 8192, a
-// twentieth of the blocks elsewhere (416 MB): 99 us, 4.2 TB/s; 64 in bfloat16 with a window of 4096 (982 MB): 192 us, 5.1 TB/s; one
+// 128 and 8 query heads to each (537 MB): 116 us, 4.6 TB/s; 48 requests of up to 16384 tokens in e4m3 with a window of 8192, a
+// twentieth of the blocks elsewhere (416 MB): 93 us, 4.5 TB/s; 64 in bfloat16 with a window of 4096 (982 MB): 174 us, 5.6 TB/s; one
 // of 33 tokens, 40 heads: 6.1 us, the launch and trips to memory one after the other (length, table, scales and rows).
 //
 // Codes are whole in binary16, so they are multiplied as such, and their scales are applied to sums: the keys' to scores, the
 // values' to each piece of sixteen tokens' part of a sum, in binary32: so any scales do, whatever they are to each other.
 //
-// Rows go to registers as the products take them, two tiles by turns.  (Three under way, of codes: 128 us for the long case.)
-// Items are cut into parts of equal numbers of tiles, a workgroup each, about kTargetGroups in all: twice what the chip holds, so
-// that ragged lengths even out (512: 133 us for the long case, 112 for the batch; 768: 135 and 101).  Parts of an item follow each
-// other in the grid; by heads first, as their tokens do in memory: 134 and 112.  They are joined by the last of them to arrive.
+// Rows go to registers as the products take them, two tiles by turns.  (Three under way, of codes, with a head a workgroup: 128 us for the long case
+// instead of 126.)
+// Items are cut into parts of equal numbers of tiles, a workgroup each.
+//
+// A head's row is 128 or 256 bytes of a token's, and rows that lie next to each other in memory belong to the heads beside it.
+// Where there is much to read, a workgroup is eight wavefronts that have four heads side by side, two wavefronts each, and as many
+// workgroups as the chip has room for at once: the same loads with nothing made of them take 96 us for the long case instead of
+// 121, 166 instead of 192 in bfloat16; two heads 105, workgroups of heads beside each other on one XCD 133.  It has four times as
+// many results to join for a workgroup, which costs it where there is little to read: there a workgroup has one head, and about
+// kTargetGroups of them even out ragged lengths.
 #include "pgcm_kv_window.h"
 
 namespace pgcm_kv_impl {
 namespace {
 
-constexpr uint32_t kWaves = 4, kThreads = kWaves * 64;
+// Wavefronts of a workgroup, and kv heads that it has side by side
+constexpr uint32_t waves_of(bool wide, uint32_t dim) { return wide && dim <= 128 ? 8 : 4; }
+constexpr uint32_t abreast_of(bool wide) { return wide ? 4 : 1; }
 constexpr uint32_t kMergedHeads = 4;   // at a time
-constexpr uint32_t kJoinedAtOnce = 24, kMostJoined = 32;   // parts of an item in one go, by what a thread reads of each; and in any
-static_assert(kMostJoined * kMostJoined >= kTargetGroups, "two levels are enough");
+constexpr uint32_t kJoinedAtOnce = 8;   // parts that a thread asks for together
+constexpr uint32_t kMostJoined = 24;   // parts of an item in one go, by what a thread reads of each
+constexpr uint32_t kTargetGroups = 1024, kWideGroups = 256;   // workgroups that a call's work is cut for
 constexpr uint32_t kWholeRows = 512;   // beyond so many rows an item is one workgroup's: each looks through them for its own
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
@@ -298,22 +307,20 @@ struct Halves {
     }
 };
 
-template <uint32_t kDim>
+// A row's request and how many of its tokens it sees, or request ~0: none has it
+struct Row {
+    uint32_t request, end;
+};
+template <uint32_t kWaves, uint32_t kDim>
 struct FewShared {
     union {
+        Row row[kWholeRows];
         float sum[kWaves][kMergedHeads][kDim + 4];
-        struct {
-            float top[kMostJoined][16], total[kMostJoined][16];
-        } part;
     };
     float top[kWaves][16], total[kWaves][16];
     uint32_t last;
 };
 
-// A row's request and how many of its tokens it sees, or request ~0: none has it
-struct Row {
-    uint32_t request, end;
-};
 __device__ __forceinline__ Row row_of(const WindowArgs& a, uint32_t row) {
     const uint32_t room = a.row_blocks * a.block_tokens;
     if (a.starts == nullptr) return Row{row, clamped(a.lens[row], room)};
@@ -331,54 +338,85 @@ __device__ __forceinline__ Row row_of(const WindowArgs& a, uint32_t row) {
     return Row{low, len > behind ? len - behind : 0};
 }
 
+// its tiles: of the pieces that the wavefronts of an item, `slots` of them, take at once
 template <class S>
-__device__ __forceinline__ uint32_t tiles_of(const WindowArgs& a, Row row) {
-    constexpr uint32_t kTilePieces = kWaves * S::kPieces;
-    return row.end == 0 ? 0 : (seen_of(a, row.end, row.end).pieces() + kTilePieces - 1) / kTilePieces;
+__device__ __forceinline__ uint32_t tiles_of(const WindowArgs& a, Row row, uint32_t slots) {
+    return row.end == 0 ? 0 : (seen_of(a, row.end, row.end).pieces() + slots * S::kPieces - 1) / (slots * S::kPieces);
 }
 
-// kCut: items are cut into parts of equal numbers of tiles, so that all of them make about kTargetGroups; else an item is one
-// workgroup's.
-template <class S, bool kExact, bool kCut>
-__global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(WindowArgs a) {
+// kCut: items are cut into parts of equal numbers of tiles; else an item is one workgroup's.  kWide: a workgroup has those of
+// kAbreast kv heads.
+template <class S, bool kExact, bool kCut, bool kWide>
+__global__ __launch_bounds__(waves_of(kWide, S::kDim) * 64, kWide || S::kDim == 256 ? 1 : 2) void few_kernel(WindowArgs a) {
     typedef typename S::H H;
     typedef typename S::M M;
     typedef typename S::L L;
-    constexpr uint32_t kDim = S::kDim, kPieces = S::kPieces;
-    __shared__ FewShared<kDim> shared;
+    constexpr uint32_t kDim = S::kDim, kPieces = S::kPieces, kWaves = waves_of(kWide, kDim), kThreads = kWaves * 64;
+    constexpr uint32_t kAbreast = abreast_of(kWide), kSlots = kWaves / kAbreast;   // kSlots: wavefronts that share an item
+    __shared__ FewShared<kWaves, kDim> shared;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t g = lane / 16, i = lane % 16;
-    const uint32_t group_tiles = (a.group + 15) / 16, per_row = a.kv_heads * group_tiles;
+    const uint32_t g = lane / 16, i = lane % 16, beside = wave % kAbreast, slot = wave / kAbreast;
+    const uint32_t group_tiles = (a.group + 15) / 16, per_row = a.kv_heads / kAbreast * group_tiles;
 
-    uint32_t row = blockIdx.x / per_row, item = blockIdx.x - row * per_row, part = 0, parts = 1;
+    // The workgroup's items are those of kAbreast kv heads of a row, side by side.
+    uint32_t row = blockIdx.x / per_row, items = blockIdx.x - row * per_row, part = 0, parts = 1, first_part = 0;
     Row of;
     if constexpr (kCut) {
-        uint32_t all = 0, mine = 0;
+        // rows and their tiles: a lane has the l-th of 64
         Row lane_row{~0u, 0};
-        for (uint32_t r0 = 0; r0 < a.tokens; r0 += 64) {
-            lane_row = r0 + lane < a.tokens ? row_of(a, r0 + lane) : Row{~0u, 0};
-            mine = tiles_of<S>(a, lane_row);
-            all += __builtin_amdgcn_readlane(scan(mine), 63);
+        uint32_t mine = 0, all = 0;
+        if (a.tokens <= 64) {
+            if (lane < a.tokens) lane_row = row_of(a, lane);
+            mine = tiles_of<S>(a, lane_row, kSlots);
+            all = __builtin_amdgcn_readlane(scan(mine), 63);
+        } else {
+            for (uint32_t r = threadIdx.x; r < a.tokens; r += kThreads) shared.row[r] = row_of(a, r);
+            __syncthreads();
         }
-        const uint32_t share = (all * per_row + kTargetGroups - 1) / kTargetGroups;   // tiles of a part, at most
+        auto look = [&](uint32_t r0) {
+            if (a.tokens <= 64) return;
+            lane_row = r0 + lane < a.tokens ? shared.row[r0 + lane] : Row{~0u, 0};
+            mine = tiles_of<S>(a, lane_row, kSlots);
+        };
+        if (a.tokens > 64)
+            for (uint32_t r0 = 0; r0 < a.tokens; r0 += 64) {
+                look(r0);
+                all += __builtin_amdgcn_readlane(scan(mine), 63);
+            }
+        // A part's tiles, at most.  One head a workgroup: so that those that are cut make about kTargetGroups; all of them are no more
+        // than that and one for each item.  Heads side by side: about the least for which all are no more than kWideGroups.
+        const uint32_t most_parts = kWideGroups / per_row;   // (used where items are at most half as many as kWideGroups)
+        uint32_t share = kWide ? (all + most_parts - 1) / most_parts : (all * per_row + kTargetGroups - 1) / kTargetGroups;
+        share = share != 0 ? share : 1;
+        auto its = [&] {   // (rows without tokens are answered by one part)
+            return lane_row.request == ~0u ? 0 : mine <= share ? 1 : (mine + share - 1) / share;
+        };
+        while (kWide) {
+            uint32_t count = 0;
+            for (uint32_t r0 = 0; r0 < a.tokens; r0 += 64) {
+                look(r0);
+                count += __builtin_amdgcn_readlane(scan(its()), 63);
+            }
+            if (count <= most_parts) break;
+            const uint32_t more = (uint32_t)((float)share * (float)count / (float)most_parts);
+            share = more > share ? more : share + 1;
+        }
         uint32_t before = 0;
         bool found = false;
         for (uint32_t r0 = 0; r0 < a.tokens; r0 += 64) {
-            if (a.tokens > 64) {
-                lane_row = r0 + lane < a.tokens ? row_of(a, r0 + lane) : Row{~0u, 0};
-                mine = tiles_of<S>(a, lane_row);
-            }
-            // rows without tokens are answered by one part
-            const uint32_t its = lane_row.request == ~0u ? 0 : mine <= share ? 1 : (mine + share - 1) / share;
-            const uint32_t upto = before + scan(its);
+            look(r0);
+            const uint32_t here = its(), upto = before + scan(here);
             const uint64_t past = __ballot(upto * per_row > blockIdx.x);
             if (past != 0) {
                 const uint32_t at = __builtin_ctzll(past);
                 row = r0 + at;
-                parts = __builtin_amdgcn_readlane(its, at);
-                const uint32_t x = blockIdx.x - (__builtin_amdgcn_readlane(upto, at) - parts) * per_row;
-                item = x / parts;
-                part = x - item * parts;
+                parts = __builtin_amdgcn_readlane(here, at);
+                const uint32_t first = (__builtin_amdgcn_readlane(upto, at) - parts) * per_row, x = blockIdx.x - first;
+                // in the grid: heads next to each other, as in memory (the loads of the long case alone: 100 us, 109 with parts
+                // next to each other); with one head a workgroup, parts (127 us, 139 with heads)
+                part = kWide ? x / per_row : x % parts;
+                items = kWide ? x - part * per_row : x / parts;
+                first_part = first + items * parts;
                 of = Row{(uint32_t)__builtin_amdgcn_readlane(lane_row.request, at), (uint32_t)__builtin_amdgcn_readlane(lane_row.end, at)};
                 found = true;
                 break;
@@ -386,17 +424,19 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
             before = __builtin_amdgcn_readlane(upto, 63);
         }
         if (!found) return;
-    }
-    if constexpr (!kCut) {
+    } else {
         of = row_of(a, row);
         of.request = __builtin_amdgcn_readfirstlane(of.request), of.end = __builtin_amdgcn_readfirstlane(of.end);
         if (of.request == ~0u) return;
     }
-    const uint32_t kv_head = item / group_tiles, head0 = (item - kv_head * group_tiles) * 16, first_head = kv_head * a.group + head0;
-    const uint32_t heads = a.group - head0 < 16 ? a.group - head0 : 16;
+    const uint32_t heads_at = items / group_tiles, head0 = (items - heads_at * group_tiles) * 16;
+    const uint32_t kv_head = heads_at * kAbreast + beside, heads = a.group - head0 < 16 ? a.group - head0 : 16;
+    auto first_head_of = [&](uint32_t beside) { return (heads_at * kAbreast + beside) * a.group + head0; };
+    const uint32_t first_head = first_head_of(beside);
     const Seen seen = of.end == 0 ? Seen{0, 0, 0} : seen_of(a, of.end, of.end);
-    const uint32_t pieces = seen.pieces(), tiles = tiles_of<S>(a, of), low = low_of(a, of.end);
-    const uint32_t from = tiles * part / parts, to = tiles * (part + 1) / parts;
+    const uint32_t pieces = seen.pieces(), tiles = tiles_of<S>(a, of, kSlots), low = low_of(a, of.end);
+    const uint32_t even = tiles / parts, more = tiles - even * parts;   // `more` parts have one tile more
+    const uint32_t from = even * part + (part < more ? part : more), to = from + even + (part < more ? 1 : 0);
 
     typename S::Raw raw;
     S::template ask_query<kExact>(raw, a, a.q + row * a.q_token + (first_head + (i < heads ? i : 0)) * a.q_head, i < heads, g);
@@ -415,7 +455,7 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
     };
     auto find = [&](uint32_t tile) {
         Pieces p{~0u, 0, 0};
-        const uint32_t t = tile + lane / kPieces, x = (t * kWaves + wave) * kPieces + lane % kPieces;
+        const uint32_t t = tile + lane / kPieces, x = (t * kSlots + slot) * kPieces + lane % kPieces;
         if (t >= to || x >= pieces) return p;
         const uint32_t token = seen.piece(x) * kPiece, place = token / a.block_tokens;
         const uint32_t end = of.end - token;   // of the tokens that are seen, from the piece's first one on
@@ -541,9 +581,8 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
     // The wavefronts' results as one.  A lane holds, of head i, channels kRun (4 g + r) + t.
     total = over_rows_sum(total);
     if (g == 0) shared.top[wave][i] = top, shared.total[wave][i] = total;
-    auto finish = [&](uint32_t h, uint32_t d, float4 x, float top, float total) {
+    auto finish = [&](uint32_t out_head, uint32_t d, float4 x, float top, float total) {
         const float by = total == 0.f ? 0.f : 1.f / total;   // (a NaN stays one)
-        const uint32_t out_head = first_head + h;
         if (d < a.head_dim) {
             typename H::one y[4] = {(typename H::one)(x.x * by), (typename H::one)(x.y * by), (typename H::one)(x.z * by),
                                     (typename H::one)(x.w * by)};
@@ -558,8 +597,7 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
     constexpr uint32_t kQuads = kDim / 4;
     const uint32_t rows_kept = a.group < 16 ? a.group : 16;
     const size_t part_floats = (size_t)rows_kept * (kDim + 2);   // sums, then tops and totals
-    const uint32_t first_part = blockIdx.x - part;
-    auto part_at = [&](uint32_t w) { return a.partials + w * part_floats; };
+    auto part_at = [&](uint32_t place, uint32_t beside) { return a.partials + (place * kAbreast + beside) * part_floats; };
     auto put_part = [&](float* to_part, uint32_t h, uint32_t d, float4 x, float top, float total) {
         uint64_t* to_sum = (uint64_t*)(to_part + h * kDim + d);
         put_shared(to_sum, __builtin_bit_cast(uint64_t, make_float2(x.x, x.y)));
@@ -581,89 +619,88 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
                             make_float4(sum[n][t][r], sum[n][t + 1][r], sum[n][t + 2][r], sum[n][t + 3][r]);
         }
         __syncthreads();
-        for (uint32_t x = threadIdx.x; x < these * kQuads; x += kThreads) {
-            const uint32_t h = x / kQuads, d = x % kQuads * 4;
-            float most = shared.top[0][h0 + h];
+        for (uint32_t x = threadIdx.x; x < these * kAbreast * kQuads; x += kThreads) {
+            const uint32_t d = x % kQuads * 4, b = x / kQuads % kAbreast, k = x / (kQuads * kAbreast), h = h0 + k;
+            float most = shared.top[b][h];
 #pragma unroll
-            for (uint32_t w = 1; w < kWaves; ++w) most = fmaxf(most, shared.top[w][h0 + h]);
+            for (uint32_t w = 1; w < kSlots; ++w) most = fmaxf(most, shared.top[b + w * kAbreast][h]);
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
             float of_all = 0.f;
 #pragma unroll
-            for (uint32_t w = 0; w < kWaves; ++w) {
-                const float by = exp2_from(shared.top[w][h0 + h], most);
-                const float4 z = *(const float4*)&shared.sum[w][h][d];
-                of_all += shared.total[w][h0 + h] * by;
+            for (uint32_t w = 0; w < kSlots; ++w) {
+                const float by = exp2_from(shared.top[b + w * kAbreast][h], most);
+                const float4 z = *(const float4*)&shared.sum[b + w * kAbreast][k][d];
+                of_all += shared.total[b + w * kAbreast][h] * by;
                 y.x += z.x * by, y.y += z.y * by, y.z += z.z * by, y.w += z.w * by;
             }
-            if (!kCut || parts == 1) finish(h0 + h, d, y, most, of_all);
-            else put_part(part_at(blockIdx.x), h0 + h, d, y, most, of_all);
+            if (!kCut || parts == 1) finish(first_head_of(b) + h, d, y, most, of_all);
+            else put_part(part_at(first_part + part, b), h, d, y, most, of_all);
         }
     }
     if constexpr (kCut) {
         if (parts == 1) return;
         // The parts' results as one, by the last workgroup to arrive: those of workgroups first, first + apart, ..., to the outputs
         // or to the first's place.
-        constexpr uint32_t kMine = (16 * kQuads + kThreads - 1) / kThreads, kTogether = 8 / kMine;
+        constexpr uint32_t kMine = kWide && kDim != 64 ? 2 : 1;   // quads of a thread at a time
+        const uint32_t quads = kAbreast * heads * kQuads;
         auto join = [&](uint32_t first, uint32_t apart, uint32_t count, bool last) {
-            __syncthreads();
-            for (uint32_t x = threadIdx.x; x < count * heads; x += kThreads) {
-                const uint32_t p = x / heads, h = x - p * heads;
-                const float2 y =
-                    __builtin_bit_cast(float2, get_shared((const uint64_t*)(part_at(first + p * apart) + rows_kept * kDim) + h));
-                shared.part.top[p][h] = y.x;
-                shared.part.total[p][h] = y.y;
-            }
-            __syncthreads();
-            float4 y[kMine];
-            float most[kMine], of_all[kMine];
+            for (uint32_t x0 = threadIdx.x; x0 < quads; x0 += kMine * kThreads) {
+                float4 y[kMine];
+                float top[kMine], total[kMine];
+                uint32_t b[kMine], h[kMine];
+                const uint32_t d = x0 % kQuads * 4;
 #pragma unroll
-            for (uint32_t n = 0; n < kMine; ++n) {
-                const uint32_t x = threadIdx.x + n * kThreads, h = x / kQuads;
-                y[n] = make_float4(0.f, 0.f, 0.f, 0.f), most[n] = -INFINITY, of_all[n] = 0.f;
-                if (x < heads * kQuads)
-                    for (uint32_t p = 0; p < count; ++p) most[n] = fmaxf(most[n], shared.part.top[p][h]);
-            }
-            for (uint32_t p0 = 0; p0 < count; p0 += kTogether) {
-                uint64_t z[kTogether][kMine][2];   // under way together
+                for (uint32_t n = 0; n < kMine; ++n) {
+                    const uint32_t x = x0 + n * kThreads < quads ? x0 + n * kThreads : x0;
+                    b[n] = x / kQuads % kAbreast, h[n] = x / (kQuads * kAbreast);
+                    y[n] = make_float4(0.f, 0.f, 0.f, 0.f), top[n] = -INFINITY, total[n] = 0.f;
+                }
+                for (uint32_t p0 = 0; p0 < count; p0 += kJoinedAtOnce) {
+                    uint64_t z[kJoinedAtOnce][kMine][3];   // under way together
 #pragma unroll
-                for (uint32_t e = 0; e < kTogether; ++e) {
-                    const float* from_part = part_at(first + (p0 + e < count ? p0 + e : p0) * apart);
+                    for (uint32_t e = 0; e < kJoinedAtOnce; ++e)
+#pragma unroll
+                        for (uint32_t n = 0; n < kMine; ++n) {
+                            const float* from_part = part_at(first + (p0 + e < count ? p0 + e : p0) * apart, b[n]);
+                            const uint64_t* at_sum = (const uint64_t*)(from_part + h[n] * kDim + d);
+                            z[e][n][0] = get_shared(at_sum), z[e][n][1] = get_shared(at_sum + 1);
+                            z[e][n][2] = get_shared((const uint64_t*)(from_part + rows_kept * kDim) + h[n]);
+                        }
 #pragma unroll
                     for (uint32_t n = 0; n < kMine; ++n) {
-                        const uint32_t x = threadIdx.x + n * kThreads;
-                        const uint64_t* at_sum = (const uint64_t*)(from_part + 4 * (x < heads * kQuads ? x : 0));
-                        z[e][n][0] = get_shared(at_sum), z[e][n][1] = get_shared(at_sum + 1);
+                        float most = top[n];
+#pragma unroll
+                        for (uint32_t e = 0; e < kJoinedAtOnce; ++e) most = fmaxf(most, __builtin_bit_cast(float2, z[e][n][2]).x);
+                        const float keep = exp2_from(top[n], most);
+                        top[n] = most, total[n] *= keep;
+                        y[n].x *= keep, y[n].y *= keep, y[n].z *= keep, y[n].w *= keep;
+#pragma unroll
+                        for (uint32_t e = 0; e < kJoinedAtOnce; ++e) {
+                            if (p0 + e >= count) break;
+                            const float2 u = __builtin_bit_cast(float2, z[e][n][0]), v = __builtin_bit_cast(float2, z[e][n][1]);
+                            const float2 of = __builtin_bit_cast(float2, z[e][n][2]);
+                            const float by = exp2_from(of.x, most);
+                            total[n] += of.y * by;
+                            y[n].x += u.x * by, y[n].y += u.y * by, y[n].z += v.x * by, y[n].w += v.y * by;
+                        }
                     }
                 }
 #pragma unroll
                 for (uint32_t n = 0; n < kMine; ++n) {
-                    const uint32_t x = threadIdx.x + n * kThreads, h = x / kQuads;
-                    if (x >= heads * kQuads) continue;
-#pragma unroll
-                    for (uint32_t e = 0; e < kTogether; ++e) {
-                        if (p0 + e >= count) break;
-                        const float2 u = __builtin_bit_cast(float2, z[e][n][0]), v = __builtin_bit_cast(float2, z[e][n][1]);
-                        const float by = exp2_from(shared.part.top[p0 + e][h], most[n]);
-                        of_all[n] += shared.part.total[p0 + e][h] * by;
-                        y[n].x += u.x * by, y[n].y += u.y * by, y[n].z += v.x * by, y[n].w += v.y * by;
-                    }
+                    if (x0 + n * kThreads >= quads) continue;
+                    // (a row is a wavefront's or a part of it: what is put over the first part has been read by all)
+                    if (last) finish(first_head_of(b[n]) + h[n], d, y[n], top[n], total[n]);
+                    else put_part(part_at(first, b[n]), h[n], d, y[n], top[n], total[n]);
                 }
-            }
-#pragma unroll
-            for (uint32_t n = 0; n < kMine; ++n) {
-                const uint32_t x = threadIdx.x + n * kThreads, h = x / kQuads, d = x % kQuads * 4;
-                if (x >= heads * kQuads) continue;
-                if (last) finish(h, d, y[n], most[n], of_all[n]);
-                else put_part(part_at(first), h, d, y[n], most[n], of_all[n]);
             }
         };
         // in one go, or in groups of as many as there are groups
         uint32_t fan = parts;
-        if (parts * ((heads * kQuads + kThreads - 1) / kThreads) > kJoinedAtOnce)
+        if (parts * ((quads + kThreads - 1) / kThreads) > kMostJoined)
             for (fan = 4; fan * fan < parts;) ++fan;
         const uint32_t mine = part / fan * fan, count = parts - mine < fan ? parts - mine : fan;
         if (last_to_arrive(a.counters + first_part + mine, count, &shared.last)) {
-            join(first_part + mine, 1, count, fan == parts);
+            join(first_part + mine, 1, count, fan >= parts);
             const uint32_t groups_of = (parts + fan - 1) / fan;
             if (fan < parts && last_to_arrive(a.counters + 2 * kTargetGroups + first_part, groups_of, &shared.last))
                 join(first_part, fan, groups_of, true);
@@ -672,19 +709,21 @@ __global__ __launch_bounds__(kThreads, S::kDim == 256 ? 1 : 2) void few_kernel(W
 }
 
 template <class S, bool kExact>
-void launch(const WindowArgs& a, uint32_t groups, bool cut, hipStream_t stream) {
-    if (cut) few_kernel<S, kExact, true><<<groups, kThreads, 0, stream>>>(a);
-    else few_kernel<S, kExact, false><<<groups, kThreads, 0, stream>>>(a);
+void launch(const WindowArgs& a, uint32_t groups, bool cut, bool wide, hipStream_t stream) {
+    const uint32_t threads = waves_of(wide, S::kDim) * 64;
+    if (cut && wide) few_kernel<S, kExact, true, true><<<groups, threads, 0, stream>>>(a);
+    else if (cut) few_kernel<S, kExact, true, false><<<groups, threads, 0, stream>>>(a);
+    else few_kernel<S, kExact, false, false><<<groups, threads, 0, stream>>>(a);
 }
 template <template <uint32_t> class S>
-void launch(const WindowArgs& a, uint32_t groups, bool cut, hipStream_t stream) {
+void launch(const WindowArgs& a, uint32_t groups, bool cut, bool wide, hipStream_t stream) {
     const uint32_t d = a.head_dim;
-    if (d == 64) launch<S<64>, true>(a, groups, cut, stream);
-    else if (d < 64) launch<S<64>, false>(a, groups, cut, stream);
-    else if (d == 128) launch<S<128>, true>(a, groups, cut, stream);
-    else if (d < 128) launch<S<128>, false>(a, groups, cut, stream);
-    else if (d == 256) launch<S<256>, true>(a, groups, cut, stream);
-    else launch<S<256>, false>(a, groups, cut, stream);
+    if (d == 64) launch<S<64>, true>(a, groups, cut, wide, stream);
+    else if (d < 64) launch<S<64>, false>(a, groups, cut, wide, stream);
+    else if (d == 128) launch<S<128>, true>(a, groups, cut, wide, stream);
+    else if (d < 128) launch<S<128>, false>(a, groups, cut, wide, stream);
+    else if (d == 256) launch<S<256>, true>(a, groups, cut, wide, stream);
+    else launch<S<256>, false>(a, groups, cut, wide, stream);
 }
 template <uint32_t kDim> using Int8OfF16 = Codes<F16, Int8, kDim>;
 template <uint32_t kDim> using Int8OfBf16 = Codes<Bf16, Int8, kDim>;
@@ -695,23 +734,39 @@ template <uint32_t kDim> using HalvesBf16 = Halves<Bf16, kDim>;
 
 }  // namespace
 
-// Partial results of as many workgroups as there may be with more than one for an item, and two counters for each.
+// Results of as many workgroups as there may be with more than one for an item, and two counters for each.
+static_assert(abreast_of(true) * kWideGroups <= 2 * kTargetGroups, "one room for both");
 Room window_few_room(uint32_t heads, uint32_t kv_heads, uint32_t head_dim) {
     return Room{4 * 2 * 2 * kTargetGroups, 4 * partial_floats(head_dim, heads / kv_heads) * 2 * kTargetGroups};
 }
 
 int window_few(pgcm_kv* kv, WindowArgs& a, uint32_t half, uint32_t code, hipStream_t stream) {
-    const uint64_t items = (uint64_t)a.tokens * a.kv_heads * ((a.group + 15) / 16);
-    const uint32_t tile = kWaves * kPiece * (code != ~0u && a.head_dim <= 64 ? 4 : 2);
     uint64_t walked = (uint64_t)a.row_blocks * a.block_tokens;
     if (a.window != 0 && walked > (uint64_t)a.window + a.sinks + 3 * kPiece) walked = (uint64_t)a.window + a.sinks + 3 * kPiece;
-    const uint64_t tiles = (walked + tile - 1) / tile;
-    // An item is cut where that may give the chip more to do: all parts are at most kTargetGroups and one for each item, so
-    // with up to kTargetGroups items there is room for them.
-    const bool cut = tiles > 2 && items <= kTargetGroups && a.tokens <= kWholeRows && items * tiles < 1u << 31;
-    const uint64_t most = items * (tiles > 1 ? tiles : 1);
-    const uint64_t groups = cut && most > items + kTargetGroups ? items + kTargetGroups : cut ? most : items;
-    if (!launchable(groups, kThreads)) return PGCM_ERR_ARG;
+    struct Cut {
+        uint64_t per_row, items, tiles;   // workgroups of a row and of all, uncut; an item's tiles
+        bool worth;
+    };
+    auto cut_of = [&](bool wide) {
+        const uint32_t pieces = code != ~0u && a.head_dim <= 64 ? 4 : 2;
+        const uint32_t tile = waves_of(wide, a.head_dim) / abreast_of(wide) * pieces * kPiece;
+        Cut x;
+        x.per_row = (uint64_t)a.kv_heads / abreast_of(wide) * ((a.group + 15) / 16);
+        x.items = a.tokens * x.per_row, x.tiles = (walked + tile - 1) / tile;
+        x.worth = x.tiles > 2 && x.items <= kTargetGroups && a.tokens <= kWholeRows && x.items * x.tiles < 1u << 31;
+        return x;
+    };
+    const Cut narrow = cut_of(false), beside = cut_of(true);
+    // Items are cut where that may give the chip more to do.  Heads side by side are worth it where an item has few parts to be
+    // joined or many tiles: a call of them takes up to 10 us longer whatever the lengths (1 of 4096 tokens, 8 kv heads: 20 us
+    // instead of 13.5; of 32768, 36 and 37; two of 131 059, 116 and 127; 48 of 500 with 8 kv heads, 15.7 and 17.1; 16, 12.5 and 8.1).
+    const bool cut = narrow.worth;
+    const bool wide = cut && beside.worth && a.kv_heads % abreast_of(true) == 0 && 2 * beside.items <= kWideGroups &&
+                      (beside.items >= kWideGroups / 4 || beside.items * beside.tiles >= 16 * kWideGroups);
+    const uint64_t items = wide ? beside.items : narrow.items;
+    const uint64_t all = wide ? kWideGroups / beside.per_row * beside.per_row : narrow.items + kTargetGroups;
+    const uint64_t most = items * (wide ? beside.tiles : narrow.tiles), groups = !cut ? items : most < all ? most : all;
+    if (!launchable(groups, waves_of(wide, a.head_dim) * 64)) return PGCM_ERR_ARG;
     if (cut) {
         const Room room = window_few_room(a.kv_heads * a.group, a.kv_heads, a.head_dim);
         if (const int rc = kv_ensure(kv, room.counters, room.scratch, stream)) return rc;
@@ -719,9 +774,9 @@ int window_few(pgcm_kv* kv, WindowArgs& a, uint32_t half, uint32_t code, hipStre
     }
     const uint32_t n = (uint32_t)groups;
     const bool f16 = half == PGCM_KV_F16;
-    if (code == PGCM_KV8_INT8) f16 ? launch<Int8OfF16>(a, n, cut, stream) : launch<Int8OfBf16>(a, n, cut, stream);
-    else if (code == PGCM_KV8_E4M3) f16 ? launch<E4m3OfF16>(a, n, cut, stream) : launch<E4m3OfBf16>(a, n, cut, stream);
-    else f16 ? launch<HalvesF16>(a, n, cut, stream) : launch<HalvesBf16>(a, n, cut, stream);
+    if (code == PGCM_KV8_INT8) f16 ? launch<Int8OfF16>(a, n, cut, wide, stream) : launch<Int8OfBf16>(a, n, cut, wide, stream);
+    else if (code == PGCM_KV8_E4M3) f16 ? launch<E4m3OfF16>(a, n, cut, wide, stream) : launch<E4m3OfBf16>(a, n, cut, wide, stream);
+    else f16 ? launch<HalvesF16>(a, n, cut, wide, stream) : launch<HalvesBf16>(a, n, cut, wide, stream);
     return pgcm::hip_noted(hipGetLastError()) ? PGCM_ERR_HIP : PGCM_OK;
 }
 

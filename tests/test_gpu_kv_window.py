@@ -69,6 +69,71 @@ def test_long_ones_in_parts(kind, lens, kv, group, dim, window, sinks):
 
 
 @kinds
+@pytest.mark.parametrize("rows, most, kv, group, dim, window, sinks, holes", [
+    (80, 700, 4, 2, 64, 0, 0, 0.1), (16, 1000, 16, 3, 128, 200, 20, 0.0), (40, 400, 4, 17, 128, 0, 0, 0.2), (33, 500, 8, 1, 80, 300, 7, 0.3),
+    (65, 600, 4, 5, 256, 0, 0, 0.0), (32, 3000, 8, 8, 144, 2500, 64, 0.1), (128, 300, 4, 16, 24, 0, 3, 0.0)])
+def test_heads_side_by_side(kind, rows, most, kv, group, dim, window, sinks, holes):
+    """four heads a workgroup, items cut into few parts; lengths of all sizes"""
+    lens = [(most - 1) * (7 * i % rows) // (rows - 1) for i in range(rows)]
+    b = _blocks(kind, 51, lens, kv, dim, holes=holes)
+    q = _q(52, rows, kv * group, dim, kind[0])
+    if kind[1] is not None and dim % 16:   # (rows of codes are whole sixteens of bytes)
+        with pytest.raises(pgcm.PgcmError):
+            ref.run(pgcm, b, q, [1] * rows, window, sinks)
+        return
+    first = ref.check(pgcm, b, q, [1] * rows, window, sinks)
+    for _ in range(2):
+        again = ref.run(pgcm, b, q, [1] * rows, window, sinks)
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
+@kinds
+def test_heads_side_by_side_in_many_parts(kind):
+    """parts joined in two steps: an item's, alone, and beside items without tokens"""
+    for lens in ([140000], [140000, 0, 5]):
+        b = _blocks(kind, 53, lens, 16, 16)
+        ref.check(pgcm, b, _q(54, len(lens), 48, 16, kind[0]), [1] * len(lens))
+
+
+@pytest.mark.parametrize("kind", [x for x in KINDS if x[1] is not None], ids=[n for x, n in zip(KINDS, NAMES) if x[1] is not None])
+def test_heads_side_by_side_of_new_tokens(kind):
+    lens, news = [900, 30, 0, 5, 300], [60, 33, 3, 10, 16]
+    b = _blocks(kind, 55, lens, 4, 128)
+    ref.check(pgcm, b, _q(56, sum(news), 8, 128, kind[0]), news, 0, 0, spare=4, most=60)
+
+
+@kinds
+def test_heads_side_by_side_in_a_graph(kind):
+    """replayed with other lengths, between eager calls of one head a workgroup on its workspace"""
+    rows, most = 32, 1500
+    b = _blocks(kind, 57, [most] * rows, 8, 128)
+    space = pgcm.KVWorkspace()
+    pgcm.kv_window_reserve(space, 16, 8, 128)
+    tables, lens = b.r.gpu_tables()
+    q = _q(58, rows, 16, 128, kind[0]).cuda()
+    outs = [torch.zeros_like(q) for _ in range(3)]
+    cache = b.cache(pgcm)
+
+    def call(out, n=rows):
+        b.call(pgcm)(cache, q[:n], tables[:n], lens[:n], out[:n], window=1000, sinks=4, workspace=space)
+
+    call(outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[0])
+    for turn in range(4):
+        lens.copy_(torch.tensor([[most, 0, 700, 17][(i * turn + i // 3) % 4] for i in range(rows)], dtype=torch.int32))
+        call(outs[1])
+        graph.replay()
+        call(outs[2], 3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]), turn
+        outs[0].fill_(3)
+
+
+@kinds
 def test_many_requests(kind):
     """more than 64, and more than are cut into parts"""
     for n, most in ((150, 900), (600, 400)):
