@@ -10,9 +10,8 @@
 // Codes are whole in binary16, so they are multiplied as such, and their scales are applied to sums: the keys' to scores, the
 // values' to each piece of sixteen tokens' part of a sum, in binary32: so any scales do, whatever they are to each other.
 //
-// Rows go to registers as the products take them, two tiles by turns.  (Three under way, of codes, with a head a workgroup: 128 us for the long case
-// instead of 126.)
-// Items are cut into parts of equal numbers of tiles, a workgroup each.
+// Rows go to registers as the products take them, two tiles by turns.  (Three under way, of codes, with a head a workgroup: 128 us
+// for the long case instead of 126.)  Items are cut into parts of equal numbers of tiles, a workgroup each.
 //
 // A head's row is 128 or 256 bytes of a token's, and rows that lie next to each other in memory belong to the heads beside it.
 // Where there is much to read, a workgroup is eight wavefronts that have four heads side by side, two wavefronts each, and as many
