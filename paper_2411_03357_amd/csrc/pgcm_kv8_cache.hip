@@ -1,7 +1,7 @@
 // KV blocks in 8 bits: new keys and values into them, whole blocks to them and back (include/pgcm_kv8.h).  What bounds all is
 // memory.  2048 blocks of 16 tokens and 40 heads of 128 (1.0 GB each way): stored in 217 us, 4.6 TB/s, read back in 182, 5.5; a
-// prompt of 8191 tokens, 40 heads, 40 kv heads (420 MB): appended in 103 us, 4.1 TB/s; 64 tokens of 32 and 8 heads: 7.9 us, of
-// which instructions are most, some 1100 a wavefront that its launch has to fetch.
+// prompt of 8191 tokens, 40 heads, 40 kv heads (420 MB): appended in 98 us, 4.3 TB/s; 64 tokens of 32 and 8 heads: 5.7 us, of
+// which instructions are most, that its launch has to fetch.
 //
 // Store and load: a wavefront takes, of a block, the keys or the values of 64 / 2^row_power heads (a "unit"): a lane eight channels
 // of one head in every token, so that a token's codes are written in one piece and a head's largest value is found by its lanes alone.
@@ -275,11 +275,20 @@ __device__ __forceinline__ Split split_by(uint64_t x, uint32_t by, double one_by
     return Split{q, (uint32_t)r};
 }
 
+// The kernel's arguments, its only ones, read where they are used: kept in scalar registers from the start on, most went to lanes of
+// vector registers and back (64 tokens: 13.1 us with their read-back instead of 11.3).
+typedef const Append8Args __attribute__((address_space(4))) Constant;
+__device__ __forceinline__ const Append8Args& late_args() {
+    Constant* at = (Constant*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const Append8Args*)at;
+}
+
 // Keys and values of a run, m tokens from `first` on, to `block` from place `inside` on: the workgroup's share of the run's sides
 // (keys of head 0, 1, ..., then values of head 0, 1, ...), [from, to), a wavefront one at a time.  A lane's rows are tokens side by
-// side, kHeld times as many held in registers (a "chunk"): so a side's largest value is found in the wavefront.  The factors that norm and
-// rotation multiply a chunk's tokens with are made once for all heads, in LDS.  Runs of several chunks are taken twice, for their
-// largest values and for their codes.
+// side, kHeld times as many held in registers (a "chunk"): so a side's largest value is found in the wavefront.  The factors that
+// norm and rotation multiply a chunk's tokens with are made once for all heads, in LDS.  Runs of several chunks are taken twice, for
+// their largest values and for their codes.
 constexpr uint32_t kSidesAtOnce = 64;    // of a wavefront, whose largest values are kept over a run
 template <uint32_t kHeld>
 struct AppendShared {
@@ -287,9 +296,10 @@ struct AppendShared {
     uint32_t largest[kWaves][kSidesAtOnce];
 };
 template <class H, class C, uint32_t kHeld>
-__device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& turn, AppendShared<kHeld>& shared, uint32_t first,
+__device__ __forceinline__ void append_run(const Turn<H>& turn, AppendShared<kHeld>& shared, uint32_t first,
                                            uint32_t m, uint64_t block, uint32_t inside, uint32_t from, uint32_t to,
                                            const typename Turn<H>::Raw& raw, int32_t near_position, uint32_t near_from) {
+    const Append8Args& a = late_args();
     const uint32_t lane = turn.lane, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t rows = 64u >> a.row_power, in_step = lane >> a.row_power, chunk = kHeld * rows;
     const bool worked = a.k_weight != nullptr || a.rope != nullptr, normed = a.k_weight != nullptr;
@@ -304,6 +314,7 @@ __device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& 
             auto take = [&](uint32_t n_side) {
                 const bool is_v = n_side >= a.kv_heads;
                 const uint32_t h = is_v ? n_side - a.kv_heads : n_side;
+                const Append8Args& a = late_args();
                 const Side8& side = a.side[is_v];
                 // (where the lane's channels lie from a step's first token on: in 32 bits)
                 const int64_t stride = is_v ? a.v_token : a.k_token;
@@ -364,6 +375,7 @@ __device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& 
                 }
                 if (!writes) continue;
                 const uint32_t h = is_v ? n_side - a.kv_heads : n_side;
+                const Append8Args& a = late_args();
                 const Side8& side = a.side[is_v];
                 const uint32_t old = __builtin_amdgcn_readfirstlane(bits_of(old_at));
                 const uint32_t scale = scale_for<C>(__builtin_amdgcn_readfirstlane(most), old);
@@ -414,8 +426,9 @@ __device__ __forceinline__ void append_run(const Append8Args& a, const Turn<H>& 
 // The runs that begin in a window of tokens are taken by its kv_ways workgroups, whole, their sides in equal shares; the window's
 // queries by the workgroups of blockIdx.y >= kv_ways, a token and some of its heads a wavefront.
 constexpr uint32_t kWindow = 16;
+// Four workgroups a compute unit (three: a prompt of 8191 tokens of 8 kv heads and its read-back in 47 us instead of 45).
 template <class H, class C, uint32_t kHeld>
-__global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
+__global__ __launch_bounds__(kThreads, kHeld == 4 ? 4 : 2) void append8_kernel(Append8Args a) {
     __shared__ AppendShared<kHeld> shared;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     // windows a block apart follow each other, so that those in which a prompt's runs begin are spread over all XCDs
@@ -501,8 +514,9 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
         }
         const uint32_t low = __builtin_amdgcn_readlane((uint32_t)near_place.whole, at + 1);
         const uint32_t high = __builtin_amdgcn_readlane((uint32_t)(near_place.whole >> 32), at + 1);
-        append_run<H, C, kHeld>(a, turn, shared, first, m, (uint64_t)high << 32 | low, __builtin_amdgcn_readlane(near_place.rest, at + 1),
-                                from > task ? from - task : 0, to - task < 2 * a.kv_heads ? to - task : 2 * a.kv_heads, raw, near_position, near_from);
+        append_run<H, C, kHeld>(turn, shared, first, m, (uint64_t)high << 32 | low, __builtin_amdgcn_readlane(near_place.rest, at + 1),
+                                from > task ? from - task : 0, to - task < 2 * a.kv_heads ? to - task : 2 * a.kv_heads, raw, near_position,
+                                near_from);
     }
 }
 
