@@ -4,9 +4,9 @@
 // tiles of 64 tokens, each of a workgroup's four wavefronts with 32 rows:
 //   S' = K Q',  P' = 2^(S' - m),  O' = V' P'     (transposed, so that P' comes out as the right operand that it goes in as)
 // with running m and sums.  Where there are few items, each is cut into parts, whose results a second kernel puts together.
-// What bounds it are the matrix cores, busy 47 % of the cycles, and the exponentials beside them, at the clock that both leave:
-// four prompts of up to 16384 tokens, 32 heads of 128, window 4096 (1.12 TFLOP): 1.13 to 1.22 ms, 917 to 992 TFLOP/s, where a
-// library's product of 8192^3 reaches 1247; 512 tokens behind 65536, window 16384 (0.14 TFLOP, 512 parts): 178 to 190 us.
+// Weights are sums of two halves, so the second product is made twice (see there).  Four prompts of up to 16384 tokens, 32 heads of
+// 128, window 4096 (1.12 TFLOP): 1.52 ms, 738 TFLOP/s, where a library's product of 8192^3 reaches 1247; 512 tokens behind 65536,
+// window 16384 (0.14 TFLOP, 512 parts): 207 to 240 us.
 //
 // K and V go to LDS without registers, two tiles by turns, and the lanes read them from there without conflicts of banks, V across
 // its rows (ds_read_b64_tr_b16), as the left operand of the second product has tokens side by side.  A wavefront has 32 rows: two
@@ -34,11 +34,22 @@ struct Wide<F16> {
     static __device__ __forceinline__ f32x16 product(uint4 a, uint4 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(as_eight<F16>(a), as_eight<F16>(b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ void split(const float (&x)[8], uint4 (&halves)[2]) {   // all but 2^-22
+        F16::eight y[2];
+        F16::split(x, y);
+        halves[0] = as_words<F16>(y[0]), halves[1] = as_words<F16>(y[1]);
+    }
 };
 template <>
 struct Wide<Bf16> {
     static __device__ __forceinline__ f32x16 product(uint4 a, uint4 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_eight<Bf16>(a), as_eight<Bf16>(b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ void split(const float (&x)[8], uint4 (&halves)[2]) {   // the first to nearest: all but 2^-17
+        Bf16::eight first, left;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) first[e] = (__bf16)x[e], left[e] = (__bf16)(x[e] - (float)first[e]);
+        halves[0] = as_words<Bf16>(first), halves[1] = as_words<Bf16>(left);
     }
 };
 
@@ -348,22 +359,26 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
         for (uint32_t b = 0; b < 2; ++b)
 #pragma unroll
             for (uint32_t e = 0; e < 2; ++e) {
-                // weights as the right operand, sixteen tokens a step; each rounded to a half once, their sum not
-                typename H::eight y;
+                // Weights as the right operand, sixteen tokens a step, as sums of two halves.  Rounded to one each, they cost more
+                // than the outputs' own rounding: the prompts' were off by 0.0022 (2-norm, relative, bfloat16) instead of 0.0017, the
+                // chunk's by 0.00025 instead of 0.00021 (binary16), and a token's results were others than alone.  With one: 1.19
+                // ms and 166 us instead of 1.52 and 207.
+                float z[8];
 #pragma unroll
                 for (uint32_t r = 0; r < 8; ++r) {
-                    const float z = __builtin_amdgcn_exp2f(fmaf(w[b][8 * e + r], scale, down));
-                    total += z;
-                    y[r] = (typename H::one)z;
+                    z[r] = __builtin_amdgcn_exp2f(fmaf(w[b][8 * e + r], scale, down));
+                    total += z[r];
                 }
-                const uint4 p = as_words<H>(y);
+                uint4 p[2];
+                W::split(z, p);
 #pragma unroll
                 for (uint32_t n = 0; n < kOut; ++n) {
                     if (!kExact && 32 * n >= a.head_dim) break;
                     const uint8_t* from_row = v_rows + (32 * b + 16 * e) * R::kBytes + v_from[n];
                     const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)from_row));
-                    const uint2 z = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from_row + 8 * R::kBytes)));
-                    sum[n] = W::product(make_uint4(x.x, x.y, z.x, z.y), p, sum[n]);
+                    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(from_row + 8 * R::kBytes)));
+                    const uint4 v = make_uint4(x.x, x.y, y.x, y.y);
+                    sum[n] = W::product(v, p[1], W::product(v, p[0], sum[n]));
                 }
                 if (kDim == 256) __builtin_amdgcn_sched_barrier(0);
             }
