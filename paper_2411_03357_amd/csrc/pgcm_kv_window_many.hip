@@ -149,7 +149,9 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
     const Parts split = parts_of(a, x, kCut ? most_parts : 1);
     if (part >= split.parts) return;
     const Seen seen = split.seen;
-    const uint32_t from = split.tiles * part / split.parts, to = split.tiles * (part + 1) / split.parts;
+    // (`longer` parts have one tile more; a product of tiles and parts would pass 32 bits)
+    const uint32_t even = split.tiles / split.parts, longer = split.tiles - even * split.parts;
+    const uint32_t from = even * part + (part < longer ? part : longer), to = from + even + (part < longer ? 1 : 0);
 
     // the wavefront's rows, and the lane's
     const uint32_t row0 = 32 * wave, mine = x.rows <= row0 ? 0 : x.rows - row0 < 32 ? x.rows - row0 : 32;
