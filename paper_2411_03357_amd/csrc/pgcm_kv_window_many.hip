@@ -120,11 +120,14 @@ struct Rows {
 };
 
 // Sixteen bytes a lane from base + at to LDS, without a register.  As an instruction of its own, since of the compiler's it waits
-// for all that are under way before it reads anything from LDS; who reads what it brings waits for it.  (Nothing else of these
-// kernels is compiled to use m0.)
+// for all that are under way before it reads anything from LDS; who reads what it brings waits for it.
+// (m0 is reserved: the compiler sees that it changes here, and warns that it will not restore it, which nothing needs.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t at, uint32_t place) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(place), "v"(at), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(place), "v"(at), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 template <uint32_t kDim>
 struct ManyShared {
