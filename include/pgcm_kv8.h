@@ -109,7 +109,9 @@ typedef struct {
  */
 int pgcm_kv8_attend(pgcm_kv_t *kv, const pgcm_kv8_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);
 int pgcm_kv_window(pgcm_kv_t *kv, const pgcm_kv_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);
-/* Room of a workspace for calls of both with at most these sizes. */
+/* Room of a workspace for any calls of both with at most these sizes: what many new tokens may take, 35 MB with up to 64 channels,
+ * 68 with up to 128, 135 with more, and half as much again.  A call by itself asks for what it takes, single tokens for a quarter of
+ * that at most (1 MB for each query head of a kv head, with 128 channels). */
 int pgcm_kv_window_reserve(pgcm_kv_t *kv, uint32_t heads, uint32_t kv_heads, uint32_t head_dim, void *hip_stream);
 
 #ifdef __cplusplus

@@ -525,6 +525,7 @@ size_t part_bytes(uint32_t head_dim) { return 4 * (size_t)kRows * ((head_dim <= 
 
 }  // namespace
 
+// (of any call; one takes as much as it has parts)
 Room window_many_room(uint32_t head_dim) { return Room{0, part_bytes(head_dim) * kMostParts}; }
 
 int window_many(pgcm_kv* kv, WindowArgs& a, uint32_t half, hipStream_t stream) {
@@ -548,8 +549,7 @@ int window_many(pgcm_kv* kv, WindowArgs& a, uint32_t half, hipStream_t stream) {
         if (p == 1 || time < least) least = time, parts = p;
     }
     if (parts > 1) {
-        const Room room = window_many_room(a.head_dim);
-        if (const int rc = kv_ensure(kv, room.counters, room.scratch, stream)) return rc;
+        if (const int rc = kv_ensure(kv, 0, part_bytes(a.head_dim) * items * parts, stream)) return rc;
         a.partials = (float*)kv->scratch.at;
     }
     if (half == PGCM_KV_F16) launch<F16>(a, (uint32_t)items, (uint32_t)ranks, (uint32_t)parts, stream);
