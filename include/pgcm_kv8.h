@@ -66,8 +66,11 @@ int pgcm_kv8_append(const pgcm_kv8_cache *cache, const pgcm_kv_append_args *args
  * n blocks' first tokens, from `from` (block from_blocks[i], or blocks[i] if NULL) to `to` (block blocks[i]).  counts: DEVICE
  * [n], tokens of each (cut to [0, block_tokens]), or NULL: all.  Both caches have the same sizes but for the number of blocks, and
  * one `half`.  A block outside its pool is passed over; no block of `to` is named twice.  Store starts each block anew, with the
- * scales of those tokens; places behind them are left as they are, in both directions.  Load rounds once to a half; what
- * would exceed its range, at most by that rounding, becomes its largest number.
+ * scales of those tokens; places behind them are left as they are, in both directions.  Load rounds once to a half; a finite
+ * product beyond its range becomes its largest number, however far beyond it is.  Of blocks that store made, only what rounding
+ * to a code has put there is (2^16 in binary16).  Append rounds values of 32 bits to codes, and scales of others may be any: such
+ * a value of a binary16 cache may be far beyond 65504.  pgcm_kv8_attend takes it as it is, load makes it 65504, where
+ * pgcm_kv_append would have made it infinite.
  */
 int pgcm_kv8_store(const pgcm_kv8_cache *to, const pgcm_kv_cache *from, uint32_t n, const int32_t *blocks, const int32_t *counts,
                    const int32_t *from_blocks, void *hip_stream);
