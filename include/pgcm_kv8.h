@@ -105,7 +105,7 @@ typedef struct {
  * makes its channel infinite or NaN in the rows that see it.
  * Softmax weights are multiplied with values as sums of halves, and added up as they are.  One new token of each request, and
  * always in pgcm_kv8_attend: they leave nothing out over bfloat16 blocks of halves, else 2^-22 of a weight at most, or 2^-38 of the
- * row's largest where that is more.  More of them over blocks of halves: 2^-17 of a weight at most in bfloat16, in binary16 as much
+ * row's largest where that is more.  More of them over blocks of halves: 2^-16 of a weight at most in bfloat16, in binary16 as much
  * as one does.
  * In pgcm_kv8_attend a query is multiplied as a power of two times binary16 numbers, its largest channel near 2^14: what of a
  * bfloat16 channel lies below 2^-38 of that one is rounded away, and a row whose largest is below 2^-126 counts as zero.

@@ -45,11 +45,17 @@ struct Wide<Bf16> {
     static __device__ __forceinline__ f32x16 product(uint4 a, uint4 b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_eight<Bf16>(a), as_eight<Bf16>(b), c, 0, 0, 0);
     }
-    static __device__ __forceinline__ void split(const float (&x)[8], uint4 (&halves)[2]) {   // the first to nearest: all but 2^-17
-        Bf16::eight first, left;
+    static __device__ __forceinline__ void split(const float (&x)[8], uint4 (&halves)[2]) {   // all but 2^-16
+        uint32_t first[4], left[4];
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) first[e] = (__bf16)x[e], left[e] = (__bf16)(x[e] - (float)first[e]);
-        halves[0] = as_words<Bf16>(first), halves[1] = as_words<Bf16>(left);
+        for (uint32_t e = 0; e < 8; e += 2) {   // (the upper half of a float is its bfloat16 towards zero)
+            const uint32_t a = __builtin_bit_cast(uint32_t, x[e]), b = __builtin_bit_cast(uint32_t, x[e + 1]);
+            first[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            typedef __bf16 two __attribute__((ext_vector_type(2)));   // (converted in pairs: the prompts in 1.52 ms, by one 1.58)
+            left[e / 2] = __builtin_bit_cast(uint32_t, two{(__bf16)(x[e] - __builtin_bit_cast(float, a & 0xFFFF0000u)),
+                                                           (__bf16)(x[e + 1] - __builtin_bit_cast(float, b & 0xFFFF0000u))});
+        }
+        halves[0] = make_uint4(first[0], first[1], first[2], first[3]), halves[1] = make_uint4(left[0], left[1], left[2], left[3]);
     }
 };
 
@@ -537,7 +543,7 @@ int window_many(pgcm_kv* kv, WindowArgs& a, uint32_t half, hipStream_t stream) {
     const uint64_t seen = (uint64_t)a.window + a.sinks + kRows / a.group + 4 * kPiece;
     if (a.window != 0 && walked > seen) walked = seen;
     const uint64_t tiles = (walked + kTile - 1) / kTile, useful = (tiles + kLeastTiles - 1) / kLeastTiles;
-    // (512 tokens, 128 items: 4 parts 187 us, 3 205, 8 205; 1200, 304 items: 3 parts 410, 1 473; 8 tokens, 8 items: 33 parts 35, 16 43)
+    // (512 tokens, 128 items: 4 parts 236 us, 3 262, 8 253; 1200, 304 items: 3 parts 530, 1 619; 8 tokens, 8 items: 33 parts 37, 16 48)
     // As many parts as take the least time, in tiles: rounds of as many workgroups as the chip holds, two tiles' time at a part's
     // start and end each, and the join's.
     const uint64_t at_once = a.head_dim > 128 ? kManyGroups / 2 : kManyGroups;

@@ -14,8 +14,9 @@ import kv_window_reference as ref
 
 pytestmark = pytest.mark.gpu
 
-# of a weight, what its halves leave out: two, the first of 11 bits towards zero, or of 8 bits to nearest
-LEFT_OUT = {torch.float16: 2.0 ** -22, torch.bfloat16: 2.0 ** -17}
+# of a weight in [1, 2), what its two halves leave out: the first, towards zero, less than its last bit (2^-10; 2^-7), and the second,
+# to nearest, half of the last bit of a number below that (2^-22; 2^-16)
+LEFT_OUT = {torch.float16: 2.0 ** -22, torch.bfloat16: 2.0 ** -16}
 SCALE = 0.125
 
 
