@@ -163,7 +163,7 @@ struct Codes {
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) q.x[c][e] = (_Float16)(exponent == 255 ? 0.f : x[c][e] * first * second);
     }
-    static __device__ __forceinline__ f32x4 scores(const Held& held, uint32_t p, const Query& q, const Here& at) {
+    static __device__ __forceinline__ f32x4 scores(const Held& held, uint32_t p, const Query& q) {
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (uint32_t c = 0; c < kSteps; ++c) {
@@ -174,7 +174,7 @@ struct Codes {
                 s[n] = F16::product(__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7), q.x[2 * c + n], s[n]);
             }
         }
-        return (s[0] + s[1]) * at.k_scale;
+        return s[0] + s[1];
     }
     // sums += values by the weights of pieces p and p + 1
     static __device__ __forceinline__ void add(Held& held, uint32_t p, const float (&w)[8], const Here (&at)[kPieces],
@@ -270,7 +270,7 @@ struct Halves {
         }
     }
     static __device__ __forceinline__ void make_query(Query& q, const Raw& raw) { q = raw; }
-    static __device__ __forceinline__ f32x4 scores(const Held& held, uint32_t p, const Query& q, const Here&) {
+    static __device__ __forceinline__ f32x4 scores(const Held& held, uint32_t p, const Query& q) {
         f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (uint32_t c = 0; c < kSteps; ++c) s[c % 2] = H::product(as_eight<H>(held.k[p][c]), as_eight<H>(q.x[c]), s[c % 2]);
@@ -517,13 +517,14 @@ __global__ __launch_bounds__(waves_of(kWide, S::kDim) * 64, kWide || S::kDim == 
         for (uint32_t p = 0; p < kPieces; ++p) S::template load<kExact>(held, a, p, at[p], g, i);
     };
     typename S::Query query;
-    float scale = 0.f;
     auto work = [&](typename S::Held& held, const Here (&at)[kPieces]) {
         float s[kPieces][4];
         float most = -INFINITY;
 #pragma unroll
         for (uint32_t p = 0; p < kPieces; ++p) {
-            const f32x4 x = S::scores(held, p, query, at[p]);
+            const f32x4 x = S::scores(held, p, query);
+            // (the powers of two of keys and query first: either may be near the ends of the range, and their product not)
+            const float scale = S::kScaled ? at[p].k_scale * query.by * a.scale : a.scale;
 #pragma unroll
             for (uint32_t r = 0; r < 4; ++r) {
                 s[p][r] = x[r] * scale;
@@ -563,7 +564,6 @@ __global__ __launch_bounds__(waves_of(kWide, S::kDim) * 64, kWide || S::kDim == 
         if (seek(at[0])) {
             load(held[0], at[0]);
             S::make_query(query, raw);
-            scale = a.scale * query.by;
             while (true) {
                 const bool more = seek(at[1]);
                 if (more) load(held[1], at[1]);

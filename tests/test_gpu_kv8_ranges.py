@@ -1,4 +1,5 @@
-"""KV blocks in 8 bits of binary16 values whose norm's weight or rotation takes them beyond what a half holds."""
+"""KV blocks in 8 bits at the ends of ranges: binary16 values that a norm's weight or a rotation takes beyond what a half holds,
+keys and queries of opposite sizes."""
 import math
 
 import pytest
@@ -7,6 +8,7 @@ import torch
 import paper_2411_03357_amd as pgcm
 import kv8_reference as ref
 import kv_reference as ref16
+import kv_window_reference as window
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +64,15 @@ def test_what_append_takes_beyond_a_half_is_kept_in_codes_and_cut_by_load(weight
     assert abs(float(lse[0, 0]) - score) <= abs(score) * 2.0 ** -20
     if weighted:
         assert abs(score) > 70000 * 2.0 ** -12
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+@pytest.mark.parametrize("up", [112, -112])
+def test_scores_of_keys_and_queries_at_opposite_ends_of_the_range(up, code):
+    """keys of 2^112 and queries of 2^-112, and the other way round: their products are as any"""
+    half = torch.bfloat16
+    b = window.Blocks8(94, [300, 40, 1], 2, 128, half, code)
+    b.parts[2] *= 2.0 ** up if up > 0 else 2.0 ** -90       # (scales of this library are 2^-100 at least)
+    b.k *= 2.0 ** up if up > 0 else 2.0 ** -90
+    q = (ref16.numbers(95, 3, 8, 128).clamp(-3, 3) * 2.0 ** (-up if up > 0 else 90)).to(half)
+    window.check(pgcm, b, q, [1, 1, 1])
