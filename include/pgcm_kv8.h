@@ -108,7 +108,9 @@ typedef struct {
  * row's largest where that is more.  More of them over blocks of halves: 2^-16 of a weight at most in bfloat16, in binary16 as much
  * as one does.
  * In pgcm_kv8_attend a query is multiplied as a power of two times binary16 numbers, its largest channel near 2^14: what of a
- * bfloat16 channel lies below 2^-38 of that one is rounded away, and a row whose largest is below 2^-126 counts as zero.
+ * bfloat16 channel lies below 2^-38 of that one is rounded away, and a row whose largest is below 2^-126 counts as zero.  One with
+ * a channel that is not finite makes its results NaN where it sees a token that is on the device, whatever its scores are.
+ * Sums of values are held in binary32 times 2^15 and less: values beyond 2^88 may leave its range.
  */
 int pgcm_kv8_attend(pgcm_kv_t *kv, const pgcm_kv8_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);
 int pgcm_kv_window(pgcm_kv_t *kv, const pgcm_kv_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);

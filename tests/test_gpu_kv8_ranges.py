@@ -1,5 +1,5 @@
 """KV blocks in 8 bits at the ends of ranges: binary16 values that a norm's weight or a rotation takes beyond what a half holds,
-keys and queries of opposite sizes."""
+keys and queries of opposite sizes, queries that are not finite."""
 import math
 
 import pytest
@@ -76,3 +76,19 @@ def test_scores_of_keys_and_queries_at_opposite_ends_of_the_range(up, code):
     b.k *= 2.0 ** up if up > 0 else 2.0 ** -90
     q = (ref16.numbers(95, 3, 8, 128).clamp(-3, 3) * 2.0 ** (-up if up > 0 else 90)).to(half)
     window.check(pgcm, b, q, [1, 1, 1])
+
+
+@pytest.mark.parametrize("code", ref.CODES)
+def test_a_query_that_is_not_finite_makes_its_row_nan(code):
+    """... where it sees any token, and in no other row"""
+    for half in (torch.float16, torch.bfloat16):
+        b = window.Blocks8(96, [50, 0, 20, 33], 2, 64, half, code)
+        q = ref16.numbers(97, 4, 4, 64).to(half)
+        clean, clean_lse = window.run(pgcm, b, q, [1] * 4)
+        q[0, 1, 5], q[1, 0, 3], q[2, 3, 0] = math.inf, math.nan, -math.inf
+        out, lse = window.run(pgcm, b, q, [1] * 4)
+        lost = torch.zeros(4, 4, dtype=torch.bool, device="cuda")
+        lost[0, 1] = lost[2, 3] = True
+        assert bool(torch.isnan(out[lost]).all()) and bool(torch.isnan(lse[lost]).all())
+        assert torch.equal(out[~lost], clean[~lost]) and torch.equal(lse[~lost], clean_lse[~lost])
+        assert bool((out[1] == 0).all())
