@@ -179,10 +179,14 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void many_kernel(Win
             const uint32_t d = 16 * c + 8 * hh;
             q[c] = make_uint4(0, 0, 0, 0);
             if (mine != 0 && (kExact || d < a.head_dim)) q[c] = *(const uint4*)(at + 2 * d);
-            // (a factor below zero turns the signs of q, one of zero makes it zero: the factor left is more than zero)
+            // (a factor below zero turns the signs of q, one of zero makes it zero, or NaN: the factor left is more than zero)
             if (a.scale <= 0.f) {
-                const uint32_t kept = a.scale == 0.f ? 0u : ~0u, sign = kept & 0x80008000u;
-                q[c] = make_uint4((q[c].x & kept) ^ sign, (q[c].y & kept) ^ sign, (q[c].z & kept) ^ sign, (q[c].w & kept) ^ sign);
+                auto with = [&](uint32_t w) {
+                    constexpr uint32_t kInf = H::kInfinity;
+                    if (a.scale != 0.f) return w ^ 0x80008000u;
+                    return ((w & kInf) == kInf ? 0x7FFFu : 0u) | ((w & kInf << 16) == kInf << 16 ? 0x7FFF0000u : 0u);
+                };
+                q[c] = make_uint4(with(q[c].x), with(q[c].y), with(q[c].z), with(q[c].w));
             }
         }
     }
