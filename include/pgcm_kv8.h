@@ -111,6 +111,8 @@ typedef struct {
  * bfloat16 channel lies below 2^-38 of that one is rounded away, and a row whose largest is below 2^-126 counts as zero.  One with
  * a channel that is not finite makes its results NaN where it sees a token that is on the device, whatever its scores are.
  * Sums of values are held in binary32 times 2^15 and less: values beyond 2^88 may leave its range.
+ * One new token of each request without a window is also what pgcm_kv_attend does, which takes 3 % less time in large batches, 30 %
+ * less in small ones of some 1000 tokens, and 5 to 25 % more for one request of some 4000 tokens or a few of 100000.
  */
 int pgcm_kv8_attend(pgcm_kv_t *kv, const pgcm_kv8_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);
 int pgcm_kv_window(pgcm_kv_t *kv, const pgcm_kv_cache *cache, const pgcm_kv_window_args *args, void *hip_stream);

@@ -3,7 +3,7 @@
 // Per token, kv head and group of up to sixteen of its query heads (an "item"):
 //   s[t][h] = scale k_t . q_h,   m = max s,   out = sum 2^(s - m) v_t / sum 2^(s - m)     (s in units of log 2)
 // with running m and sums, one pass over K and V.  What bounds it is memory: two requests of 131 059 tokens in int8, 8 kv heads of
-// 128 and 8 query heads to each (537 MB): 116 us, 4.6 TB/s; 48 requests of up to 16384 tokens in e4m3 with a window of 8192, a
+// 128 and 8 query heads to each (537 MB): 113 us, 4.8 TB/s; 48 requests of up to 16384 tokens in e4m3 with a window of 8192, a
 // twentieth of the blocks elsewhere (416 MB): 93 us, 4.5 TB/s; 64 in bfloat16 with a window of 4096 (982 MB): 174 us, 5.6 TB/s; one
 // of 33 tokens, 40 heads: 6.1 us, the launch and trips to memory one after the other (length, table, scales and rows).
 //

@@ -4,9 +4,11 @@
 // tiles of 64 tokens, each of a workgroup's four wavefronts with 32 rows:
 //   S' = K Q',  P' = 2^(S' - m),  O' = V' P'     (transposed, so that P' comes out as the right operand that it goes in as)
 // with running m and sums.  Where there are few items, each is cut into parts, whose results a second kernel puts together.
-// Weights are sums of two halves, so the second product is made twice (see there).  Four prompts of up to 16384 tokens, 32 heads of
-// 128, window 4096 (1.12 TFLOP): 1.52 ms, 738 TFLOP/s, where a library's product of 8192^3 reaches 1247; 512 tokens behind 65536,
-// window 16384 (0.14 TFLOP, 512 parts): 207 to 240 us.
+// Weights are sums of two halves, so the second product is made twice (see there).  What bounds it are the matrix cores, busy 60 % of
+// the cycles, and vector instructions, under way in 49 %: the two wavefronts of a SIMD hide little more of one behind the other, at
+// a clock that falls to 1.8 GHz.  (LDS: 50 % of the cycles by the bytes, 4 % of all waits.)  Four prompts of up to 16384 tokens, 32
+// heads of 128, window 4096 (1.12 TFLOP): 1.52 to 1.54 ms, 727 to 738 TFLOP/s, where a library's product of 8192^3 reaches 1247; 512
+// tokens behind 65536, window 16384 (0.14 TFLOP, 512 parts): 207 to 240 us.
 //
 // K and V go to LDS without registers, two tiles by turns, and the lanes read them from there without conflicts of banks, V across
 // its rows (ds_read_b64_tr_b16), as the left operand of the second product has tokens side by side.  A wavefront has 32 rows: two
